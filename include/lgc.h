@@ -328,6 +328,125 @@ lgc_status lgc_average(lgc_ctx *ctx, const float *x, uint64_t len, int batch, fl
 lgc_status lgc_reserve(lgc_ctx *ctx, const lgc_ae *ae /* nullable */, uint64_t k, int batch,
                        const lgc_segments *seg /* nullable */);
 
+/* ---- the training step that the gradient comes from ----
+ *
+ * Layer norm, the non-linearity and the products of a linear layer, forward and
+ * backward, with the activations kept for the backward pass in 8 bits: the
+ * array that a product reads is also the checkpoint that the weights' gradient
+ * and the non-linearity's gradient read.  The weights' gradients come out in
+ * fp32, wherever in a flat gradient their place is, for lgc_accumulate_topk.
+ *
+ * Plain matrices: row-major, fp32 or bf16 (lgc_type), `ld` ELEMENTS from row to
+ * row (ld >= columns), at any address that an element's size divides.  One call's
+ * plain matrices have one type.  Vectors (gamma, beta, mean, rstd, bias and their
+ * gradients) are fp32.
+ *
+ * Matrices in 8 bits: two arrays.
+ *   codes  [rows][lgc_codes_stride(cols)]: e4m3 (OCP: 4 exponent bits, bias 7, 3
+ *          of mantissa; 0x7f and 0xff are NaN, the largest number is 448), the
+ *          columns padded with zeros to a multiple of 128.  16-byte aligned.
+ *   exps   one byte E per block of columns, [rows][lgc_exps_stride(cols)]; or, for
+ *          weights, one per 128 x 128, [ceil(rows / 128)][lgc_exps_stride(cols)].
+ *          4-byte aligned; bytes past the last block are never looked at.
+ *   value = code * 2^(E - 127).  E is the least for which the block's largest
+ *          finite magnitude is at most 448 * 2^(E - 127), and at least 10 (so that
+ *          every value is zero or a normal number of bf16 and fp32).  Codes are
+ *          rounded to nearest, ties to even: an element is off by at most 2^-4 of
+ *          itself or 2^-17 of the block's largest (2^-127 absolute in a block
+ *          below 448 * 2^-117).  Infinities and NaNs become NaN.
+ *
+ * Limits: columns (cols, n, k) from 1 to 2^20; rows below 2^31, and rows times
+ * blocks of 128 columns below 2^30.  rows == 0 is valid: nothing is computed, and
+ * sums over the rows are zeros.  Sums and statistics are in fp32, products' as
+ * lgc_product says, and in a fixed order: equal calls give equal bits.
+ */
+
+typedef enum { LGC_FP32 = 0, LGC_BF16 = 1 } lgc_type;
+typedef enum { LGC_RELU = 0, LGC_GELU = 1 /* with the normal distribution's function */, LGC_SILU = 2 } lgc_act;
+
+/* bytes from row to row of the codes and of the exponents of a matrix of `cols` columns (0 for 0) */
+uint64_t lgc_codes_stride(uint64_t cols);
+uint64_t lgc_exps_stride(uint64_t cols);
+
+/*
+ * Reserves the scratch (64 MB) where lgc_layer_norm_grad, lgc_product and
+ * lgc_weight_grad put partial sums, whatever their sizes.  Without it they return
+ * LGC_EINVAL and say so; the other calls need none.  May allocate; a second call
+ * does nothing.  The context's max_n, max_k and max_batch do not limit these
+ * calls, and none of them touches the state of the selection.
+ */
+lgc_status lgc_reserve_training(lgc_ctx *ctx);
+
+/* codes, exps <- x, with an exponent per row and 128 columns */
+lgc_status lgc_quantize(lgc_ctx *ctx, const void *x, lgc_type type, uint64_t rows, uint64_t cols, uint64_t ld,
+                        uint8_t *codes, uint8_t *exps, void *stream);
+
+/* codes, exps <- w, with an exponent per 128 x 128; codes_t, exps_t (both or
+ * neither NULL) <- the transpose [cols][rows], of the same numbers: what the
+ * product of the backward pass reads.  rows: 1 to 2^20. */
+lgc_status lgc_quantize_weights(lgc_ctx *ctx, const void *w, lgc_type type, uint64_t rows, uint64_t cols, uint64_t ld,
+                                uint8_t *codes, uint8_t *exps, uint8_t *codes_t, uint8_t *exps_t, void *stream);
+
+/* x <- codes, exps; exp_rows: 1 (an exponent per row) or 128 (per 128 x 128).
+ * Exact in both types. */
+lgc_status lgc_dequantize(lgc_ctx *ctx, const uint8_t *codes, const uint8_t *exps, int exp_rows, uint64_t rows, uint64_t cols,
+                          void *x, lgc_type type, uint64_t ld, void *stream);
+
+/*
+ * Layer norm of every row: mean = sum x / cols, rstd = (sum (x - mean)^2 / cols +
+ * eps)^(-1/2), y = (x - mean) rstd gamma + beta, in fp32 and rounded once.
+ * gamma, beta: [cols] (NULL: 1, 0).  Any of the outputs may be NULL: y, mean and
+ * rstd [rows], and y in 8 bits (codes and exps both or neither).  eps >= 0.
+ */
+lgc_status lgc_layer_norm(lgc_ctx *ctx, const void *x, lgc_type type, uint64_t rows, uint64_t cols, uint64_t ld,
+                          const float *gamma, const float *beta, float eps, void *y, uint64_t ld_y, float *mean, float *rstd,
+                          uint8_t *codes, uint8_t *exps, void *stream);
+
+/*
+ * Its gradient, from lgc_layer_norm's mean and rstd: with h = (x - mean) rstd and
+ * q = dy gamma,  dx = rstd (q - mean(q) - h mean(q h)) (means over the row),
+ * dgamma = sum over rows of dy h,  dbeta = sum over rows of dy.  Any of dx, dgamma
+ * and dbeta may be NULL.
+ */
+lgc_status lgc_layer_norm_grad(lgc_ctx *ctx, const void *dy, uint64_t ld_dy, const void *x, uint64_t ld, lgc_type type,
+                               uint64_t rows, uint64_t cols, const float *gamma, const float *mean, const float *rstd, void *dx,
+                               uint64_t ld_dx, float *dgamma, float *dbeta, void *stream);
+
+/* z <- f(a) elementwise; a in 8 bits (the checkpoint) and z in 8 bits (for the next
+ * product).  Any of the three outputs may be NULL (codes with its exps). */
+lgc_status lgc_activate(lgc_ctx *ctx, lgc_act act, const void *a, lgc_type type, uint64_t rows, uint64_t cols, uint64_t ld,
+                        void *z, uint64_t ld_z, uint8_t *a_codes, uint8_t *a_exps, uint8_t *z_codes, uint8_t *z_exps,
+                        void *stream);
+
+/* da <- dz f'(a), a from its 8 bits (f' of LGC_RELU at 0 is 0); da plain and in 8
+ * bits, either may be NULL. */
+lgc_status lgc_activate_grad(lgc_ctx *ctx, lgc_act act, const void *dz, lgc_type type, uint64_t rows, uint64_t cols,
+                             uint64_t ld, const uint8_t *a_codes, const uint8_t *a_exps, void *da, uint64_t ld_da,
+                             uint8_t *da_codes, uint8_t *da_exps, void *stream);
+
+/*
+ * y[m][n] = sum_k a[m][k] b[n][k] + bias[n] (bias may be NULL), a with an exponent
+ * per row and 128 columns, b (weights) with one per 128 x 128.  Forward: a = the
+ * layer's input, b = w [out][in]; gradient of the input: a = dy, b = the transpose
+ * that lgc_quantize_weights makes.  Precision by the type of y.  LGC_BF16: the
+ * matrix cores' products of 8-bit codes, which add eight neighbouring products with
+ * some 14 bits below the largest and go on in fp32; about 2^-16 of the result for
+ * inputs of one size, below what rounding to bf16 costs.  LGC_FP32: exact products,
+ * added in fp32, at a lower rate.
+ */
+lgc_status lgc_product(lgc_ctx *ctx, const uint8_t *a_codes, const uint8_t *a_exps, uint64_t m, const uint8_t *b_codes,
+                       const uint8_t *b_exps, uint64_t n, uint64_t k, const float *bias, void *y, lgc_type type, uint64_t ld,
+                       void *stream);
+
+/*
+ * dw[n][k] = sum over rows t of dy[t][n] x[t][k] and db[n] = sum over rows of dy[t][n]
+ * (NULL: not wanted): the gradient of a linear layer's weights and bias, from dy as it
+ * is and the layer's input in 8 bits (an exponent per row and 128 columns).  dw is
+ * contiguous.  Products are exact and added in fp32.
+ */
+lgc_status lgc_weight_grad(lgc_ctx *ctx, const void *dy, lgc_type type, uint64_t rows, uint64_t n, uint64_t ld,
+                           const uint8_t *x_codes, const uint8_t *x_exps, uint64_t k, float *dw, float *db, void *stream);
+
 /* ---- diagnostics (never needed on the hot path) ---- */
 
 /* LGC_OPT_SELECT_PATH: how lgc_topk / lgc_accumulate_topk select (the results

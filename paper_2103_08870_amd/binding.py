@@ -17,6 +17,8 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "liblgc.so")
 
 LGC_OK, LGC_EINVAL, LGC_ENOMEM, LGC_EHIP, LGC_EDEVICE = range(5)
+LGC_FP32, LGC_BF16 = 0, 1
+LGC_RELU, LGC_GELU, LGC_SILU = 0, 1, 2
 LGC_OPT_SELECT_PATH, LGC_OPT_PROFILE, LGC_OPT_CARRY_THRESHOLD = 0, 1, 2
 
 EXPORTS = [
@@ -28,6 +30,10 @@ EXPORTS = [
     "lgc_segments_create", "lgc_segments_destroy", "lgc_segments_total_k",
     "lgc_topk_segmented", "lgc_accumulate_topk_segmented",
     "lgc_innovation", "lgc_decode_innovation",
+    "lgc_codes_stride", "lgc_exps_stride", "lgc_reserve_training",
+    "lgc_quantize", "lgc_quantize_weights", "lgc_dequantize",
+    "lgc_layer_norm", "lgc_layer_norm_grad", "lgc_activate", "lgc_activate_grad",
+    "lgc_product", "lgc_weight_grad",
 ]
 
 
@@ -113,6 +119,21 @@ def lib() -> C.CDLL:
     l.lgc_stats_carried.restype = i32
     l.lgc_profile_read.argtypes = [vp, C.POINTER(C.c_double), C.POINTER(u64)]
     l.lgc_profile_read.restype = i32
+    l.lgc_codes_stride.argtypes = l.lgc_exps_stride.argtypes = [u64]
+    l.lgc_codes_stride.restype = l.lgc_exps_stride.restype = u64
+    for name, args in (
+            ("lgc_reserve_training", [vp]),
+            ("lgc_quantize", [vp, vp, i32, u64, u64, u64, vp, vp, vp]),
+            ("lgc_quantize_weights", [vp, vp, i32, u64, u64, u64, vp, vp, vp, vp, vp]),
+            ("lgc_dequantize", [vp, vp, vp, i32, u64, u64, vp, i32, u64, vp]),
+            ("lgc_layer_norm", [vp, vp, i32, u64, u64, u64, vp, vp, f32, vp, u64, vp, vp, vp, vp, vp]),
+            ("lgc_layer_norm_grad", [vp, vp, u64, vp, u64, i32, u64, u64, vp, vp, vp, vp, u64, vp, vp, vp]),
+            ("lgc_activate", [vp, i32, vp, i32, u64, u64, u64, vp, u64, vp, vp, vp, vp, vp]),
+            ("lgc_activate_grad", [vp, i32, vp, i32, u64, u64, u64, vp, vp, vp, u64, vp, vp, vp]),
+            ("lgc_product", [vp, vp, vp, u64, vp, vp, u64, u64, vp, vp, i32, u64, vp]),
+            ("lgc_weight_grad", [vp, vp, i32, u64, u64, u64, vp, vp, u64, vp, vp, vp])):
+        entry = getattr(l, name)
+        entry.argtypes, entry.restype = args, i32
     _lib = l
     return l
 
@@ -234,6 +255,22 @@ class Segments:
             self.close()
         except Exception:
             pass
+
+
+class Blocks:
+    """A matrix [rows][cols] in 8 bits: e4m3 codes (columns padded to a multiple of 128) and one exponent byte per row and
+    128 columns or, with ``tiles`` (weights), per 128 x 128.  Makes the two arrays, or takes a caller's."""
+
+    def __init__(self, rows: int, cols: int, tiles: bool = False, device="cuda", codes: Optional[torch.Tensor] = None,
+                 exps: Optional[torch.Tensor] = None):
+        wide = (cols + 127) // 128
+        self.rows, self.cols, self.tiles = rows, cols, tiles
+        shape = (rows, 128 * wide), ((rows + 127) // 128 if tiles else rows, (wide + 3) // 4 * 4)
+        self.codes = torch.empty(shape[0], dtype=torch.uint8, device=device) if codes is None else codes
+        self.exps = torch.empty(shape[1], dtype=torch.uint8, device=device) if exps is None else exps
+        for t, s in zip((self.codes, self.exps), shape):
+            _require(t.is_contiguous() and tuple(t.shape) == s and t.dtype == torch.uint8, f"an array of a Blocks is contiguous uint8 of shape {s}")
+        self.at = _ptr(self.codes), _ptr(self.exps)
 
 
 # ---------------------------------------------------------------------------- entry points
@@ -407,3 +444,143 @@ def lgc_profile_read(ctx: Context) -> Tuple[float, int]:
     ms, cnt = C.c_double(), C.c_uint64()
     _check(lib().lgc_profile_read(ctx.h, C.byref(ms), C.byref(cnt)), ctx.h)
     return ms.value, cnt.value
+
+
+# ------------------------------------------------------------- the training step's operators
+
+_TYPES = {torch.float32: LGC_FP32, torch.bfloat16: LGC_BF16}
+_ACTS = {"relu": LGC_RELU, "gelu": LGC_GELU, "silu": LGC_SILU}
+_NONE = None, None
+
+
+def _matrix(t: Optional[torch.Tensor], shape, dtype, what: str):
+    """(pointer, elements from row to row) of a plain matrix, None: (None, 0)."""
+    if t is None:
+        return None, 0
+    _require(t.dim() == 2 and t.shape == shape and t.dtype == dtype, f"{what} must be {tuple(shape)} of {dtype}")
+    _require(t.stride(1) == 1 or shape[1] <= 1 or shape[0] == 0, f"{what} must have contiguous rows")
+    return _ptr(t), t.stride(0) if shape[0] > 1 else max(1, shape[1])
+
+
+def _vector(t: Optional[torch.Tensor], n: int, what: str) -> Optional[int]:
+    _require(t is None or t.is_contiguous() and t.numel() == n, f"{what} must be contiguous with {n} elements")
+    return _ptr(t, torch.float32)
+
+
+def _blocks(b: Optional[Blocks], shape, what: str, tiles: bool = False):
+    if b is None:
+        return _NONE
+    _require((b.rows, b.cols) == tuple(shape) and b.tiles == tiles, f"{what} must be Blocks of {tuple(shape)} with an exponent per "
+                                                                    + ("128 x 128" if tiles else "row and 128 columns"))
+    return b.at
+
+
+def _type(t: torch.Tensor, what: str) -> int:
+    _require(t.dim() == 2 and t.dtype in _TYPES, f"{what} must be a matrix of float32 or bfloat16")
+    return _TYPES[t.dtype]
+
+
+def lgc_codes_stride(cols: int) -> int:
+    return int(lib().lgc_codes_stride(cols))
+
+
+def lgc_exps_stride(cols: int) -> int:
+    return int(lib().lgc_exps_stride(cols))
+
+
+def lgc_reserve_training(ctx: Context) -> None:
+    """Reserves the scratch of lgc_layer_norm_grad, lgc_product and lgc_weight_grad (64 MB, whatever the sizes)."""
+    _check(lib().lgc_reserve_training(ctx.h), ctx.h)
+
+
+def lgc_quantize(ctx: Context, x: torch.Tensor, out: Blocks) -> None:
+    """out <- x [rows][cols], an exponent per row and 128 columns."""
+    kind = _type(x, "x")
+    at, ld = _matrix(x, x.shape, x.dtype, "x")
+    codes, exps = _blocks(out, x.shape, "out")
+    _check(lib().lgc_quantize(ctx.h, at, kind, x.shape[0], x.shape[1], ld, codes, exps, _stream()), ctx.h)
+
+
+def lgc_quantize_weights(ctx: Context, w: torch.Tensor, out: Blocks, transposed: Optional[Blocks] = None) -> None:
+    """out <- w [rows][cols], transposed <- its transpose, an exponent per 128 x 128; the same numbers in both."""
+    kind = _type(w, "w")
+    at, ld = _matrix(w, w.shape, w.dtype, "w")
+    codes, exps = _blocks(out, w.shape, "out", True)
+    codes_t, exps_t = _blocks(transposed, w.shape[::-1], "transposed", True)
+    _check(lib().lgc_quantize_weights(ctx.h, at, kind, w.shape[0], w.shape[1], ld, codes, exps, codes_t, exps_t, _stream()), ctx.h)
+
+
+def lgc_dequantize(ctx: Context, blocks: Blocks, out: torch.Tensor) -> None:
+    """out [rows][cols] <- the values of blocks, exactly."""
+    kind = _type(out, "out")
+    at, ld = _matrix(out, (blocks.rows, blocks.cols), out.dtype, "out")
+    _check(lib().lgc_dequantize(ctx.h, *blocks.at, 128 if blocks.tiles else 1, blocks.rows, blocks.cols, at, kind, ld, _stream()), ctx.h)
+
+
+def lgc_layer_norm(ctx: Context, x: torch.Tensor, gamma: Optional[torch.Tensor], beta: Optional[torch.Tensor], eps: float,
+                   y: Optional[torch.Tensor] = None, mean: Optional[torch.Tensor] = None, rstd: Optional[torch.Tensor] = None,
+                   blocks: Optional[Blocks] = None) -> None:
+    """y, blocks (y in 8 bits), mean, rstd <- layer norm of the rows of x; what is None is left out."""
+    kind = _type(x, "x")
+    rows, cols = x.shape
+    at, ld = _matrix(x, x.shape, x.dtype, "x")
+    out, ld_y = _matrix(y, x.shape, x.dtype, "y")
+    codes, exps = _blocks(blocks, x.shape, "blocks")
+    _check(lib().lgc_layer_norm(ctx.h, at, kind, rows, cols, ld, _vector(gamma, cols, "gamma"), _vector(beta, cols, "beta"), eps, out, ld_y,
+                                _vector(mean, rows, "mean"), _vector(rstd, rows, "rstd"), codes, exps, _stream()), ctx.h)
+
+
+def lgc_layer_norm_grad(ctx: Context, dy: torch.Tensor, x: torch.Tensor, gamma: Optional[torch.Tensor], mean: torch.Tensor, rstd: torch.Tensor,
+                        dx: Optional[torch.Tensor] = None, dgamma: Optional[torch.Tensor] = None, dbeta: Optional[torch.Tensor] = None) -> None:
+    """Gradients of lgc_layer_norm from its mean and rstd; what is None is left out."""
+    kind = _type(x, "x")
+    rows, cols = x.shape
+    at, ld = _matrix(x, x.shape, x.dtype, "x")
+    at_dy, ld_dy = _matrix(dy, x.shape, x.dtype, "dy")
+    at_dx, ld_dx = _matrix(dx, x.shape, x.dtype, "dx")
+    _check(lib().lgc_layer_norm_grad(ctx.h, at_dy, ld_dy, at, ld, kind, rows, cols, _vector(gamma, cols, "gamma"), _vector(mean, rows, "mean"),
+                                     _vector(rstd, rows, "rstd"), at_dx, ld_dx, _vector(dgamma, cols, "dgamma"), _vector(dbeta, cols, "dbeta"),
+                                     _stream()), ctx.h)
+
+
+def _act(act) -> int:
+    _require(act in _ACTS, f"act is one of {', '.join(_ACTS)}")
+    return _ACTS[act]
+
+
+def lgc_activate(ctx: Context, act: str, a: torch.Tensor, z: Optional[torch.Tensor] = None, a_blocks: Optional[Blocks] = None,
+                 z_blocks: Optional[Blocks] = None) -> None:
+    """z, z_blocks (z in 8 bits), a_blocks (a in 8 bits, for lgc_activate_grad) <- f(a); act: "relu", "gelu" or "silu"."""
+    kind = _type(a, "a")
+    at, ld = _matrix(a, a.shape, a.dtype, "a")
+    out, ld_z = _matrix(z, a.shape, a.dtype, "z")
+    _check(lib().lgc_activate(ctx.h, _act(act), at, kind, a.shape[0], a.shape[1], ld, out, ld_z, *_blocks(a_blocks, a.shape, "a_blocks"),
+                              *_blocks(z_blocks, a.shape, "z_blocks"), _stream()), ctx.h)
+
+
+def lgc_activate_grad(ctx: Context, act: str, dz: torch.Tensor, a_blocks: Blocks, da: Optional[torch.Tensor] = None,
+                      da_blocks: Optional[Blocks] = None) -> None:
+    """da, da_blocks (da in 8 bits) <- dz f'(a), a as lgc_activate kept it."""
+    kind = _type(dz, "dz")
+    at, ld = _matrix(dz, dz.shape, dz.dtype, "dz")
+    out, ld_da = _matrix(da, dz.shape, dz.dtype, "da")
+    _check(lib().lgc_activate_grad(ctx.h, _act(act), at, kind, dz.shape[0], dz.shape[1], ld, *_blocks(a_blocks, dz.shape, "a_blocks"), out, ld_da,
+                                   *_blocks(da_blocks, dz.shape, "da_blocks"), _stream()), ctx.h)
+
+
+def lgc_product(ctx: Context, a: Blocks, b: Blocks, bias: Optional[torch.Tensor], y: torch.Tensor) -> None:
+    """y [m][n] <- a [m][k] b [n][k]^T + bias [n]; b with an exponent per 128 x 128."""
+    kind = _type(y, "y")
+    at, ld = _matrix(y, (a.rows, b.rows), y.dtype, "y")
+    a_codes, a_exps = _blocks(a, (a.rows, a.cols), "a")
+    b_codes, b_exps = _blocks(b, (b.rows, a.cols), "b", True)
+    _check(lib().lgc_product(ctx.h, a_codes, a_exps, a.rows, b_codes, b_exps, b.rows, a.cols, _vector(bias, b.rows, "bias"), at, kind, ld, _stream()), ctx.h)
+
+
+def lgc_weight_grad(ctx: Context, dy: torch.Tensor, x: Blocks, dw: torch.Tensor, db: Optional[torch.Tensor] = None) -> None:
+    """dw [n][k] <- dy [rows][n]^T x [rows][k], db [n] <- the columns' sums of dy; dw anywhere in a flat fp32 gradient."""
+    kind = _type(dy, "dy")
+    rows, n = dy.shape
+    at, ld = _matrix(dy, dy.shape, dy.dtype, "dy")
+    codes, exps = _blocks(x, (rows, x.cols), "x")
+    _check(lib().lgc_weight_grad(ctx.h, at, kind, rows, n, ld, codes, exps, x.cols, _vector(dw, n * x.cols, "dw"), _vector(db, n, "db"), _stream()), ctx.h)

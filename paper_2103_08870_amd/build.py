@@ -15,8 +15,9 @@ LIB = os.path.join(HERE, "liblgc.so")
 LIB_SHORT_WAIT = os.path.join(HERE, "liblgc_short_wait.so")
 ROOT = os.path.dirname(HERE)
 HBM_RATES = os.path.join(ROOT, "hbm_rates")
-SOURCES = ["api.hip", "streaming.hip", "topk.hip", "small.hip", "segmented.hip", "autoencoder.hip", "ae_mfma.hip", "ae_fused.hip"]
-HEADERS = [os.path.join(CSRC, "lgc_internal.h"), os.path.join(CSRC, "device_helpers.h"), os.path.join(CSRC, "carry.h"),
+SOURCES = ["api.hip", "streaming.hip", "topk.hip", "small.hip", "segmented.hip", "autoencoder.hip", "ae_mfma.hip", "ae_fused.hip",
+           "blocks.hip", "norm.hip", "product.hip", "weight_grad.hip"]
+HEADERS = [os.path.join(CSRC, "lgc_internal.h"), os.path.join(CSRC, "device_helpers.h"), os.path.join(CSRC, "carry.h"), os.path.join(CSRC, "blocks.h"),
            os.path.join(os.path.dirname(HERE), "include", "lgc.h")]
 
 FLAGS = ["-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC", "-ffp-contract=off",

@@ -45,6 +45,7 @@ struct lgc_ctx {
     // per-layer selection: thresholds [max_batch][n_seg] and a candidate list of its own, grown on demand
     uint32_t *seg_t = nullptr, *seg_cand = nullptr, *seg_row_prefix = nullptr;
     size_t seg_t_words = 0, seg_cand_words = 0;
+    float *training = nullptr;           // partial sums of the training step's operators (kTrainingFloats), or not reserved
     int opt_path = 0, opt_profile = 0, opt_carry = 1;
     // Thresholds carried from one selection to the next (one record per node, device memory, see Carry); for the
     // per-layer selection one record per layer and node, sized with the rest of its scratch by lgc_reserve
@@ -552,6 +553,7 @@ extern "C" void lgc_destroy(lgc_ctx *ctx) {
     if (ctx->seg_row_prefix) (void)hipFree(ctx->seg_row_prefix);
     if (ctx->scratch) (void)hipFree(ctx->scratch);
     if (ctx->row_rec) (void)hipFree(ctx->row_rec);
+    if (ctx->training) (void)hipFree(ctx->training);
     if (ctx->fell_back_host) (void)hipHostFree(ctx->fell_back_host);
     delete ctx;
 }
@@ -1441,6 +1443,174 @@ extern "C" lgc_status lgc_reserve(lgc_ctx *ctx, const lgc_ae *ae, uint64_t k, in
         if (ae && k > 0 && (s = ensure_act(ctx, act_need(ae, k, batch))) != LGC_OK) return s;
         if (seg && (s = ensure_seg_scratch(ctx, seg)) != LGC_OK) return s;
         return LGC_OK;
+    });
+}
+
+// ------------------------------------------------------------------ the training step's operators
+
+extern "C" uint64_t lgc_codes_stride(uint64_t cols) { return codes_stride(cols); }
+extern "C" uint64_t lgc_exps_stride(uint64_t cols) { return exps_stride(cols); }
+
+extern "C" lgc_status lgc_reserve_training(lgc_ctx *ctx) {
+    if (!ctx) return fail(nullptr, LGC_EINVAL, "ctx is NULL");
+    if (ctx->training) return LGC_OK;
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return fail(ctx, LGC_EHIP, "cannot select device %d", ctx->device);
+    float *p = nullptr;
+    HIP_TRY(ctx, hipMalloc((void **)&p, kTrainingFloats * 4));
+    ctx->training = p;
+    return LGC_OK;
+}
+
+namespace {
+
+constexpr uint64_t kMostCols = 1u << 20;
+
+// One call's arguments, checked in turn; the first that is wrong is what `status` reports.
+struct Check {
+    lgc_ctx *ctx;
+    lgc_status status = LGC_OK;
+    explicit Check(lgc_ctx *c) : ctx(c) {
+        if (!c) status = fail(nullptr, LGC_EINVAL, "ctx is NULL");
+    }
+    template <typename... A>
+    Check &need(bool good, const char *fmt, A... a) {
+        if (status == LGC_OK && !good) status = fail(ctx, LGC_EINVAL, fmt, a...);
+        return *this;
+    }
+    Check &type(lgc_type t) { return need(t == LGC_FP32 || t == LGC_BF16, "unknown type %d", (int)t); }
+    Check &act(lgc_act a) { return need(a == LGC_RELU || a == LGC_GELU || a == LGC_SILU, "unknown non-linearity %d", (int)a); }
+    Check &cols(const char *name, uint64_t n) {
+        return need(n >= 1 && n <= kMostCols, "%s = %llu outside [1, 2^20]", name, (unsigned long long)n);
+    }
+    Check &rows(const char *name, uint64_t r, uint64_t cols) {
+        return need(r < (1ull << 31) && (status != LGC_OK || r * block_count(cols) < (1ull << 30)),
+                    "%s = %llu: not below 2^31, or 2^30 blocks of 128 columns or more", name, (unsigned long long)r);
+    }
+    Check &plain(const char *name, const void *p, lgc_type t, uint64_t cols, uint64_t ld) {
+        need(p != nullptr, "%s is NULL", name);
+        need(aligned(p, t == LGC_FP32 ? 4 : 2), "%s is not aligned to its elements", name);
+        return need(ld >= cols && ld < (1ull << 40), "the rows of %s are %llu apart", name, (unsigned long long)ld);
+    }
+    Check &maybe(const char *name, const void *p, lgc_type t, uint64_t cols, uint64_t ld) { return p ? plain(name, p, t, cols, ld) : *this; }
+    Check &vector(const char *name, const void *p) { return need(p && aligned(p, 4), "%s is NULL or not 4-byte aligned", name); }
+    Check &maybe(const char *name, const void *p) { return need(aligned(p, 4), "%s is not 4-byte aligned", name); }
+    Check &blocks(const char *name, const void *codes, const void *exps) {
+        need(codes && exps, "the codes or exponents of %s are NULL", name);
+        return need(aligned(codes, 16) && aligned(exps, 4), "the codes of %s are not 16-byte aligned, or its exponents not 4-byte aligned", name);
+    }
+    Check &maybe_blocks(const char *name, const void *codes, const void *exps) { return codes || exps ? blocks(name, codes, exps) : *this; }
+    Check &reserved(const char *call) {
+        return need(ctx && ctx->training, "%s: scratch not reserved: call lgc_reserve_training(ctx) once beforehand", call);
+    }
+};
+
+// The launches of a call whose arguments are good
+template <typename F>
+lgc_status launch(const Check &c, F &&launches) {
+    if (c.status != LGC_OK) return c.status;
+    lgc_ctx *ctx = c.ctx;
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return fail(ctx, LGC_EHIP, "cannot select device %d", ctx->device);
+    launches();
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return fail(ctx, LGC_EHIP, "kernel launch: %s", hipGetErrorString(e));
+    return LGC_OK;
+}
+
+}  // namespace
+
+extern "C" lgc_status lgc_quantize(lgc_ctx *ctx, const void *x, lgc_type type, uint64_t rows, uint64_t cols, uint64_t ld, uint8_t *codes, uint8_t *exps, void *stream) {
+    Check c(ctx);
+    c.type(type).cols("cols", cols).rows("rows", rows, cols);
+    if (rows) c.plain("x", x, type, cols, ld).blocks("x", codes, exps);
+    return launch(c, [&] {
+        if (rows) launch_quantize(x, type, (uint32_t)rows, (uint32_t)cols, ld, codes, exps, (hipStream_t)stream);
+    });
+}
+
+extern "C" lgc_status lgc_quantize_weights(lgc_ctx *ctx, const void *w, lgc_type type, uint64_t rows, uint64_t cols, uint64_t ld, uint8_t *codes, uint8_t *exps,
+                                           uint8_t *codes_t, uint8_t *exps_t, void *stream) {
+    Check c(ctx);
+    c.type(type).cols("cols", cols).cols("rows", rows).rows("rows", rows, cols);
+    c.plain("w", w, type, cols, ld).blocks("w", codes, exps).maybe_blocks("w's transpose", codes_t, exps_t);
+    return launch(c, [&] { launch_quantize_tiles(w, type, (uint32_t)rows, (uint32_t)cols, ld, codes, exps, codes_t, exps_t, (hipStream_t)stream); });
+}
+
+extern "C" lgc_status lgc_dequantize(lgc_ctx *ctx, const uint8_t *codes, const uint8_t *exps, int exp_rows, uint64_t rows, uint64_t cols, void *x, lgc_type type,
+                                     uint64_t ld, void *stream) {
+    Check c(ctx);
+    c.type(type).cols("cols", cols).rows("rows", rows, cols).need(exp_rows == 1 || exp_rows == kBlockCols, "exp_rows = %d is neither 1 nor 128", exp_rows);
+    if (rows) c.plain("x", x, type, cols, ld).blocks("x", codes, exps);
+    return launch(c, [&] {
+        if (rows) launch_dequantize(codes, exps, exp_rows != 1, (uint32_t)rows, (uint32_t)cols, x, type, ld, (hipStream_t)stream);
+    });
+}
+
+extern "C" lgc_status lgc_layer_norm(lgc_ctx *ctx, const void *x, lgc_type type, uint64_t rows, uint64_t cols, uint64_t ld, const float *gamma, const float *beta,
+                                     float eps, void *y, uint64_t ld_y, float *mean, float *rstd, uint8_t *codes, uint8_t *exps, void *stream) {
+    Check c(ctx);
+    c.type(type).cols("cols", cols).rows("rows", rows, cols).need(eps >= 0.f && eps < INFINITY, "eps = %g", (double)eps);
+    c.maybe("gamma", gamma).maybe("beta", beta).maybe("mean", mean).maybe("rstd", rstd);
+    if (rows) c.plain("x", x, type, cols, ld).maybe("y", y, type, cols, ld_y).maybe_blocks("y", codes, exps);
+    return launch(c, [&] {
+        if (rows) launch_norm(x, type, (uint32_t)rows, (uint32_t)cols, ld, gamma, beta, eps, y, ld_y, mean, rstd, codes, exps, (hipStream_t)stream);
+    });
+}
+
+extern "C" lgc_status lgc_layer_norm_grad(lgc_ctx *ctx, const void *dy, uint64_t ld_dy, const void *x, uint64_t ld, lgc_type type, uint64_t rows, uint64_t cols,
+                                          const float *gamma, const float *mean, const float *rstd, void *dx, uint64_t ld_dx, float *dgamma, float *dbeta,
+                                          void *stream) {
+    Check c(ctx);
+    c.type(type).cols("cols", cols).rows("rows", rows, cols).maybe("gamma", gamma).maybe("dgamma", dgamma).maybe("dbeta", dbeta);
+    if (rows) c.plain("dy", dy, type, cols, ld_dy).plain("x", x, type, cols, ld).vector("mean", mean).vector("rstd", rstd).maybe("dx", dx, type, cols, ld_dx);
+    c.reserved("lgc_layer_norm_grad");
+    return launch(c, [&] {
+        launch_norm_grad(dy, ld_dy, x, ld, type, (uint32_t)rows, (uint32_t)cols, gamma, mean, rstd, dx, ld_dx, dgamma, dbeta, ctx->training, kTrainingFloats, ctx->cus,
+                         (hipStream_t)stream);
+    });
+}
+
+extern "C" lgc_status lgc_activate(lgc_ctx *ctx, lgc_act act, const void *a, lgc_type type, uint64_t rows, uint64_t cols, uint64_t ld, void *z, uint64_t ld_z,
+                                   uint8_t *a_codes, uint8_t *a_exps, uint8_t *z_codes, uint8_t *z_exps, void *stream) {
+    Check c(ctx);
+    c.act(act).type(type).cols("cols", cols).rows("rows", rows, cols);
+    if (rows) c.plain("a", a, type, cols, ld).maybe("z", z, type, cols, ld_z).maybe_blocks("a", a_codes, a_exps).maybe_blocks("z", z_codes, z_exps);
+    return launch(c, [&] {
+        if (rows) launch_activate(act, a, type, (uint32_t)rows, (uint32_t)cols, ld, z, ld_z, a_codes, a_exps, z_codes, z_exps, (hipStream_t)stream);
+    });
+}
+
+extern "C" lgc_status lgc_activate_grad(lgc_ctx *ctx, lgc_act act, const void *dz, lgc_type type, uint64_t rows, uint64_t cols, uint64_t ld, const uint8_t *a_codes,
+                                        const uint8_t *a_exps, void *da, uint64_t ld_da, uint8_t *da_codes, uint8_t *da_exps, void *stream) {
+    Check c(ctx);
+    c.act(act).type(type).cols("cols", cols).rows("rows", rows, cols);
+    if (rows) c.plain("dz", dz, type, cols, ld).blocks("a", a_codes, a_exps).maybe("da", da, type, cols, ld_da).maybe_blocks("da", da_codes, da_exps);
+    return launch(c, [&] {
+        if (rows) launch_activate_grad(act, dz, type, (uint32_t)rows, (uint32_t)cols, ld, a_codes, a_exps, da, ld_da, da_codes, da_exps, (hipStream_t)stream);
+    });
+}
+
+extern "C" lgc_status lgc_product(lgc_ctx *ctx, const uint8_t *a_codes, const uint8_t *a_exps, uint64_t m, const uint8_t *b_codes, const uint8_t *b_exps, uint64_t n,
+                                  uint64_t k, const float *bias, void *y, lgc_type type, uint64_t ld, void *stream) {
+    Check c(ctx);
+    c.type(type).cols("n", n).cols("k", k).rows("m", m, k).rows("m", m, n).rows("n", n, k).maybe("bias", bias);
+    if (m) c.blocks("a", a_codes, a_exps).blocks("b", b_codes, b_exps).plain("y", y, type, n, ld);
+    c.reserved("lgc_product");
+    return launch(c, [&] {
+        if (m) launch_product(a_codes, a_exps, b_codes, b_exps, (uint32_t)m, (uint32_t)n, (uint32_t)k, bias, y, type, ld, ctx->training, kTrainingFloats, ctx->cus,
+                              (hipStream_t)stream);
+    });
+}
+
+extern "C" lgc_status lgc_weight_grad(lgc_ctx *ctx, const void *dy, lgc_type type, uint64_t rows, uint64_t n, uint64_t ld, const uint8_t *x_codes,
+                                      const uint8_t *x_exps, uint64_t k, float *dw, float *db, void *stream) {
+    Check c(ctx);
+    c.type(type).cols("n", n).cols("k", k).rows("rows", rows, k).rows("rows", rows, n).rows("n", n, k).vector("dw", dw).maybe("db", db);
+    if (rows) c.plain("dy", dy, type, n, ld).blocks("x", x_codes, x_exps);
+    c.reserved("lgc_weight_grad");
+    return launch(c, [&] {
+        launch_weight_grad(dy, type, (uint32_t)rows, (uint32_t)n, ld, x_codes, x_exps, (uint32_t)k, dw, db, ctx->training, kTrainingFloats, ctx->cus, (hipStream_t)stream);
     });
 }
 

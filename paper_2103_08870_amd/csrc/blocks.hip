@@ -1,0 +1,286 @@
+// Matrices in 8 bits: storing and bringing back, weights with a scale per 128 x 128, and the non-linearities that keep
+// their input that way for the backward pass.
+#include "blocks.h"
+
+namespace lgc {
+namespace {
+
+constexpr int kUnits = 4;   // blocks of 128 columns that 16 lanes handle one after the other, with all loads queued first
+
+// One of the launch's blocks of 128 columns as 16 lanes see it: the lane's eight columns.
+struct Place {
+    uint32_t row, col;
+    int count;   // of the eight columns, how many exist
+};
+__device__ __forceinline__ Place place_of(uint32_t unit, const Divide &blocks, uint32_t cols) {
+    Place p;
+    p.row = quotient(unit, blocks);
+    p.col = (unit - p.row * blocks.by) * kBlockCols + (threadIdx.x & 15) * kChunkCols;
+    p.count = p.col >= cols ? 0 : cols - p.col >= 8 ? 8 : (int)(cols - p.col);
+    return p;
+}
+__device__ __forceinline__ uint32_t first_unit() { return blockIdx.x * (uint32_t)(kUnits * kBlock / 16) + threadIdx.x / 16; }
+
+template <typename T>
+__global__ __launch_bounds__(kBlock) void k_quantize(const T *x, uint64_t ld, uint32_t cols, Divide blocks, uint32_t units, uint8_t *codes, uint8_t *exps,
+                                                     uint32_t exp_stride) {
+    float v[kUnits][8];
+    const uint32_t u0 = first_unit();
+#pragma unroll
+    for (int i = 0; i < kUnits; ++i) {
+        const uint32_t u = u0 + i * (kBlock / 16);
+        if (u >= units) break;
+        const Place p = place_of(u, blocks, cols);
+        load_chunk(x + (uint64_t)p.row * ld + p.col, p.count, v[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < kUnits; ++i) {
+        const uint32_t u = u0 + i * (kBlock / 16);
+        if (u >= units) break;
+        const uint32_t row = quotient(u, blocks), b = u - row * blocks.by;
+        store_block(v[i], codes + (uint64_t)u * kBlockCols + (threadIdx.x & 15) * kChunkCols, exps + (uint64_t)row * exp_stride + b);
+    }
+}
+
+// tiles: 1: an exponent is shared by 128 rows
+template <typename T>
+__global__ __launch_bounds__(kBlock) void k_dequantize(const uint8_t *codes, const uint8_t *exps, uint32_t exp_stride, int tiles, uint32_t cols, Divide blocks,
+                                                       uint32_t units, T *x, uint64_t ld) {
+    u2 c[kUnits];
+    uint32_t e[kUnits];
+    const uint32_t u0 = first_unit();
+#pragma unroll
+    for (int i = 0; i < kUnits; ++i) {
+        const uint32_t u = u0 + i * (kBlock / 16);
+        if (u >= units) break;
+        const uint32_t row = quotient(u, blocks), b = u - row * blocks.by;
+        c[i] = *(const u2 *)(codes + (uint64_t)u * kBlockCols + (threadIdx.x & 15) * kChunkCols);
+        e[i] = exps[(uint64_t)(tiles ? row / kBlockCols : row) * exp_stride + b];
+    }
+#pragma unroll
+    for (int i = 0; i < kUnits; ++i) {
+        const uint32_t u = u0 + i * (kBlock / 16);
+        if (u >= units) break;
+        const Place p = place_of(u, blocks, cols);
+        float v[8];
+        values_of(c[i], exp_scale(e[i]), v);
+        store_chunk(x + (uint64_t)p.row * ld + p.col, p.count, v);
+    }
+}
+
+// One tile of 128 x 128 of a weight matrix per block: its codes, and (codes_t not null) those of the transposed matrix, which are the same numbers.
+template <typename T>
+__global__ __launch_bounds__(kBlock) void k_quantize_tiles(const T *w, uint64_t ld, uint32_t rows, uint32_t cols, uint8_t *codes, uint8_t *exps, uint32_t exp_stride,
+                                                           uint64_t code_stride, uint8_t *codes_t, uint8_t *exps_t, uint32_t exp_stride_t, uint64_t code_stride_t) {
+    constexpr int kPitch = kBlockCols + 8;   // bytes per column of the tile in LDS: rows of codes in eights
+    __shared__ __align__(16) uint8_t turned[kBlockCols * kPitch];
+    __shared__ uint32_t most[kWaves];
+    const uint32_t r0 = blockIdx.y * kBlockCols, c0 = blockIdx.x * kBlockCols, col = c0 + (threadIdx.x & 15) * kChunkCols;
+    const int count = col >= cols ? 0 : cols - col >= 8 ? 8 : (int)(cols - col);
+    float v[8][8];
+    uint32_t key = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const uint32_t row = r0 + threadIdx.x / 16 + 16 * i;
+        load_chunk(w + (uint64_t)row * ld + col, row < rows ? count : 0, v[i]);
+        const uint32_t k = finite_key(v[i]);
+        key = k > key ? k : key;
+    }
+    key = max_of_16(key);
+    uint32_t all = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t k = __builtin_amdgcn_readlane(key, 16 * i);
+        all = k > all ? k : all;
+    }
+    most[threadIdx.x / 64] = all;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i) all = most[i] > all ? most[i] : all;
+    const uint32_t e = block_exp(all);
+    const float inverse = exp_inverse(e);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const uint32_t r = threadIdx.x / 16 + 16 * i;
+        const u2 c = codes_of(v[i], inverse);
+        if (r0 + r < rows) *(u2 *)(codes + (uint64_t)(r0 + r) * code_stride + col) = c;
+        if (codes_t)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) turned[((threadIdx.x & 15) * 8 + j) * kPitch + r] = (uint8_t)(c[j / 4] >> (8 * (j % 4)));
+    }
+    if (threadIdx.x == 0) {
+        exps[(uint64_t)blockIdx.y * exp_stride + blockIdx.x] = (uint8_t)e;
+        if (codes_t) exps_t[(uint64_t)blockIdx.x * exp_stride_t + blockIdx.y] = (uint8_t)e;
+    }
+    if (!codes_t) return;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const uint32_t c = threadIdx.x / 16 + 16 * i, part = (threadIdx.x & 15) * 8;
+        if (c0 + c < cols) *(u2 *)(codes_t + (uint64_t)(c0 + c) * code_stride_t + r0 + part) = *(const u2 *)(turned + c * kPitch + part);
+    }
+}
+
+// ---------------------------------------------------------------- non-linearities
+
+// Normal distribution's function below -|x|, over exp(-x^2 / 2): t * (c0 + c1 t + .. + c6 t^6) with t = 1 / (1 + p |x|), fitted (least largest relative
+// error, by reweighted least squares) for 0 <= |x| <= 13.5, where it is off by 5.3e-7 at most; the tail keeps its relative precision, since nothing is
+// subtracted from 1.
+__device__ __forceinline__ float normal_below(float size, float gauss) {
+    const float t = __builtin_amdgcn_rcpf(1.f + 0.26390194744793544f * size);
+    float s = -0.0694093182682991f;
+    s = fmaf(s, t, 0.20417608320713043f);
+    s = fmaf(s, t, -0.07719594985246658f);
+    s = fmaf(s, t, 0.14925582706928253f);
+    s = fmaf(s, t, 0.08022129535675049f);
+    s = fmaf(s, t, 0.10782003402709961f);
+    s = fmaf(s, t, 0.10513176769018173f);
+    return s * t * gauss;
+}
+
+constexpr float kLog2e = 1.4426950408889634f;
+
+template <int kAct>
+__device__ __forceinline__ float act(float x) {
+    if constexpr (kAct == LGC_RELU) return x < 0.f ? 0.f : x;   // (a NaN stays)
+    if constexpr (kAct == LGC_SILU) return x * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-kLog2e * x));
+    const float below = normal_below(fabsf(x), __builtin_amdgcn_exp2f(-0.5f * kLog2e * x * x));
+    return x * (x < 0.f ? below : 1.f - below);
+}
+template <int kAct>
+__device__ __forceinline__ float act_slope(float x) {
+    if constexpr (kAct == LGC_RELU) return x > 0.f ? 1.f : x <= 0.f ? 0.f : x;
+    if constexpr (kAct == LGC_SILU) {
+        const float p = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-kLog2e * x));
+        return fmaf(x * p, 1.f - p, p);
+    }
+    const float gauss = __builtin_amdgcn_exp2f(-0.5f * kLog2e * x * x), below = normal_below(fabsf(x), gauss);
+    return fmaf(x * gauss, 0.3989422804014327f, x < 0.f ? below : 1.f - below);
+}
+
+// z = f(a), and a and z in 8 bits; what is null is left out
+template <typename T, int kAct>
+__global__ __launch_bounds__(kBlock) void k_activate(const T *a, uint64_t ld, uint32_t cols, Divide blocks, uint32_t units, T *z, uint64_t ld_z, uint8_t *a_codes,
+                                                     uint8_t *a_exps, uint8_t *z_codes, uint8_t *z_exps, uint32_t exp_stride) {
+    float v[kUnits][8];
+    const uint32_t u0 = first_unit();
+#pragma unroll
+    for (int i = 0; i < kUnits; ++i) {
+        const uint32_t u = u0 + i * (kBlock / 16);
+        if (u >= units) break;
+        const Place p = place_of(u, blocks, cols);
+        load_chunk(a + (uint64_t)p.row * ld + p.col, p.count, v[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < kUnits; ++i) {
+        const uint32_t u = u0 + i * (kBlock / 16);
+        if (u >= units) break;
+        const Place p = place_of(u, blocks, cols);
+        const uint64_t code = (uint64_t)u * kBlockCols + (threadIdx.x & 15) * kChunkCols, exp = (uint64_t)p.row * exp_stride + p.col / kBlockCols;
+        if (a_codes) store_block(v[i], a_codes + code, a_exps + exp);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[i][j] = act<kAct>(v[i][j]);   // (f(0) = 0: columns that do not exist stay zeros)
+        if (z) store_chunk(z + (uint64_t)p.row * ld_z + p.col, p.count, v[i]);
+        if (z_codes) store_block(v[i], z_codes + code, z_exps + exp);
+    }
+}
+
+// da = dz f'(a), a from its 8 bits; da plain and in 8 bits, what is null is left out
+template <typename T, int kAct>
+__global__ __launch_bounds__(kBlock) void k_activate_grad(const T *dz, uint64_t ld, uint32_t cols, Divide blocks, uint32_t units, const uint8_t *a_codes,
+                                                          const uint8_t *a_exps, T *da, uint64_t ld_da, uint8_t *da_codes, uint8_t *da_exps, uint32_t exp_stride) {
+    float v[kUnits][8];
+    u2 c[kUnits];
+    uint32_t e[kUnits];
+    const uint32_t u0 = first_unit();
+#pragma unroll
+    for (int i = 0; i < kUnits; ++i) {
+        const uint32_t u = u0 + i * (kBlock / 16);
+        if (u >= units) break;
+        const Place p = place_of(u, blocks, cols);
+        load_chunk(dz + (uint64_t)p.row * ld + p.col, p.count, v[i]);
+        c[i] = *(const u2 *)(a_codes + (uint64_t)u * kBlockCols + (threadIdx.x & 15) * kChunkCols);
+        e[i] = a_exps[(uint64_t)p.row * exp_stride + p.col / kBlockCols];
+    }
+#pragma unroll
+    for (int i = 0; i < kUnits; ++i) {
+        const uint32_t u = u0 + i * (kBlock / 16);
+        if (u >= units) break;
+        const Place p = place_of(u, blocks, cols);
+        float a[8];
+        values_of(c[i], exp_scale(e[i]), a);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[i][j] *= act_slope<kAct>(a[j]);
+        if (da) store_chunk(da + (uint64_t)p.row * ld_da + p.col, p.count, v[i]);
+        if (da_codes)
+            store_block(v[i], da_codes + (uint64_t)u * kBlockCols + (threadIdx.x & 15) * kChunkCols, da_exps + (uint64_t)p.row * exp_stride + p.col / kBlockCols);
+    }
+}
+
+uint32_t unit_grid(uint32_t units) { return (units + kUnits * (kBlock / 16) - 1) / (kUnits * (kBlock / 16)); }
+
+template <typename F>
+void with_type(lgc_type type, F &&f) {
+    if (type == LGC_FP32) f((float *)nullptr);
+    else f((Bf16 *)nullptr);
+}
+template <typename T, typename F>
+void with_act(lgc_act act, F &&f) {
+    if (act == LGC_RELU) f(std::integral_constant<int, LGC_RELU>());
+    else if (act == LGC_GELU) f(std::integral_constant<int, LGC_GELU>());
+    else f(std::integral_constant<int, LGC_SILU>());
+}
+
+}  // namespace
+
+void launch_quantize(const void *x, lgc_type type, uint32_t rows, uint32_t cols, uint64_t ld, uint8_t *codes, uint8_t *exps, hipStream_t st) {
+    const uint32_t blocks = (uint32_t)block_count(cols), units = rows * blocks;
+    with_type(type, [&](auto *t) {
+        typedef std::remove_pointer_t<decltype(t)> T;
+        k_quantize<T><<<unit_grid(units), kBlock, 0, st>>>((const T *)x, ld, cols, divide_by(blocks), units, codes, exps, (uint32_t)exps_stride(cols));
+    });
+}
+
+void launch_dequantize(const uint8_t *codes, const uint8_t *exps, bool tiles, uint32_t rows, uint32_t cols, void *x, lgc_type type, uint64_t ld, hipStream_t st) {
+    const uint32_t blocks = (uint32_t)block_count(cols), units = rows * blocks;
+    with_type(type, [&](auto *t) {
+        typedef std::remove_pointer_t<decltype(t)> T;
+        k_dequantize<T><<<unit_grid(units), kBlock, 0, st>>>(codes, exps, (uint32_t)exps_stride(cols), tiles ? 1 : 0, cols, divide_by(blocks), units, (T *)x, ld);
+    });
+}
+
+void launch_quantize_tiles(const void *w, lgc_type type, uint32_t rows, uint32_t cols, uint64_t ld, uint8_t *codes, uint8_t *exps, uint8_t *codes_t, uint8_t *exps_t,
+                           hipStream_t st) {
+    const dim3 grid((uint32_t)block_count(cols), (uint32_t)block_count(rows));
+    with_type(type, [&](auto *t) {
+        typedef std::remove_pointer_t<decltype(t)> T;
+        k_quantize_tiles<T><<<grid, kBlock, 0, st>>>((const T *)w, ld, rows, cols, codes, exps, (uint32_t)exps_stride(cols), codes_stride(cols), codes_t, exps_t,
+                                                     (uint32_t)exps_stride(rows), codes_stride(rows));
+    });
+}
+
+void launch_activate(lgc_act act, const void *a, lgc_type type, uint32_t rows, uint32_t cols, uint64_t ld, void *z, uint64_t ld_z, uint8_t *a_codes, uint8_t *a_exps,
+                     uint8_t *z_codes, uint8_t *z_exps, hipStream_t st) {
+    const uint32_t blocks = (uint32_t)block_count(cols), units = rows * blocks;
+    with_type(type, [&](auto *t) {
+        typedef std::remove_pointer_t<decltype(t)> T;
+        with_act<T>(act, [&](auto kind) {
+            k_activate<T, kind><<<unit_grid(units), kBlock, 0, st>>>((const T *)a, ld, cols, divide_by(blocks), units, (T *)z, ld_z, a_codes, a_exps, z_codes, z_exps,
+                                                                     (uint32_t)exps_stride(cols));
+        });
+    });
+}
+
+void launch_activate_grad(lgc_act act, const void *dz, lgc_type type, uint32_t rows, uint32_t cols, uint64_t ld, const uint8_t *a_codes, const uint8_t *a_exps,
+                          void *da, uint64_t ld_da, uint8_t *da_codes, uint8_t *da_exps, hipStream_t st) {
+    const uint32_t blocks = (uint32_t)block_count(cols), units = rows * blocks;
+    with_type(type, [&](auto *t) {
+        typedef std::remove_pointer_t<decltype(t)> T;
+        with_act<T>(act, [&](auto kind) {
+            k_activate_grad<T, kind><<<unit_grid(units), kBlock, 0, st>>>((const T *)dz, ld, cols, divide_by(blocks), units, a_codes, a_exps, (T *)da, ld_da, da_codes,
+                                                                          da_exps, (uint32_t)exps_stride(cols));
+        });
+    });
+}
+
+}  // namespace lgc

@@ -292,4 +292,31 @@ void launch_gather_at(float *v, float *u, uint64_t stride, uint32_t n, int batch
                       float *out, Stats *stats, hipStream_t st);
 void launch_average(const float *x, uint32_t len, int batch, float scale, float *out, hipStream_t st);
 
+// ---- the training step's operators ----
+constexpr int kBlockCols = 128;   // columns that share an exponent of a matrix in 8 bits
+// Codes and exponents of rows have strides of their own: whole blocks, and exponents in fours (a product reads four of a row at once).
+__host__ __device__ inline uint64_t block_count(uint64_t cols) { return (cols + kBlockCols - 1) / kBlockCols; }
+__host__ __device__ inline uint64_t codes_stride(uint64_t cols) { return block_count(cols) * kBlockCols; }
+__host__ __device__ inline uint64_t exps_stride(uint64_t cols) { return (block_count(cols) + 3) / 4 * 4; }
+constexpr size_t kTrainingFloats = (size_t)16 << 20;   // scratch of lgc_reserve_training: partial sums, never more of them than fit
+// blocks.hip; tiles: an exponent is shared by 128 rows.  Pointers of what is not wanted are null
+void launch_quantize(const void *x, lgc_type type, uint32_t rows, uint32_t cols, uint64_t ld, uint8_t *codes, uint8_t *exps, hipStream_t st);
+void launch_dequantize(const uint8_t *codes, const uint8_t *exps, bool tiles, uint32_t rows, uint32_t cols, void *x, lgc_type type, uint64_t ld, hipStream_t st);
+void launch_quantize_tiles(const void *w, lgc_type type, uint32_t rows, uint32_t cols, uint64_t ld, uint8_t *codes, uint8_t *exps, uint8_t *codes_t, uint8_t *exps_t,
+                           hipStream_t st);
+void launch_activate(lgc_act act, const void *a, lgc_type type, uint32_t rows, uint32_t cols, uint64_t ld, void *z, uint64_t ld_z, uint8_t *a_codes, uint8_t *a_exps,
+                     uint8_t *z_codes, uint8_t *z_exps, hipStream_t st);
+void launch_activate_grad(lgc_act act, const void *dz, lgc_type type, uint32_t rows, uint32_t cols, uint64_t ld, const uint8_t *a_codes, const uint8_t *a_exps,
+                          void *da, uint64_t ld_da, uint8_t *da_codes, uint8_t *da_exps, hipStream_t st);
+// norm.hip
+void launch_norm(const void *x, lgc_type type, uint32_t rows, uint32_t cols, uint64_t ld, const float *gamma, const float *beta, float eps, void *y, uint64_t ld_y,
+                 float *mean, float *rstd, uint8_t *codes, uint8_t *exps, hipStream_t st);
+void launch_norm_grad(const void *dy, uint64_t ld_dy, const void *x, uint64_t ld, lgc_type type, uint32_t rows, uint32_t cols, const float *gamma, const float *mean,
+                      const float *rstd, void *dx, uint64_t ld_dx, float *dgamma, float *dbeta, float *scratch, size_t scratch_floats, int cus, hipStream_t st);
+// product.hip, weight_grad.hip
+void launch_product(const uint8_t *a, const uint8_t *a_exps, const uint8_t *b, const uint8_t *b_exps, uint32_t m, uint32_t n, uint32_t k, const float *bias, void *y,
+                    lgc_type type, uint64_t ld, float *scratch, size_t scratch_floats, int cus, hipStream_t st);
+void launch_weight_grad(const void *dy, lgc_type type, uint32_t rows, uint32_t n, uint64_t ld, const uint8_t *codes, const uint8_t *exps, uint32_t k, float *dw, float *db,
+                        float *scratch, size_t scratch_floats, int cus, hipStream_t st);
+
 }  // namespace lgc

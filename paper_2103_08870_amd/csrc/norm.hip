@@ -1,0 +1,366 @@
+// Layer norm and its gradient.  A row's sums are made in fp32 from values held in registers: mean first, then the squares of the
+// distances from it, so that a mean far from zero costs no digits.
+#include <algorithm>
+
+#include "blocks.h"
+
+namespace lgc {
+namespace {
+
+constexpr int kColumnRows = 16;   // wavefronts that share the sum of a column's partial sums
+
+__device__ __forceinline__ float wave_sum(float x) {
+    auto add = [](float a, uint32_t b) { return a + __uint_as_float(b); };
+    x = add(x, __builtin_amdgcn_update_dpp(0u, __float_as_uint(x), 0x111, 0xf, 0xf, false));
+    x = add(x, __builtin_amdgcn_update_dpp(0u, __float_as_uint(x), 0x112, 0xf, 0xf, false));
+    x = add(x, __builtin_amdgcn_update_dpp(0u, __float_as_uint(x), 0x114, 0xf, 0xf, false));
+    x = add(x, __builtin_amdgcn_update_dpp(0u, __float_as_uint(x), 0x118, 0xf, 0xf, false));
+    x = add(x, __builtin_amdgcn_update_dpp(0u, __float_as_uint(x), 0x142, 0xa, 0xf, false));
+    x = add(x, __builtin_amdgcn_update_dpp(0u, __float_as_uint(x), 0x143, 0xc, 0xf, false));
+    return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), 63));
+}
+
+// Sums of two numbers over the kThreads threads of a row.  tmp: 2 x kThreads / 64 words; a second call needs words of its own, or a barrier between.
+template <int kThreads>
+__device__ __forceinline__ f2 row_sum(float a, float b, f2 *tmp) {
+    f2 s = {wave_sum(a), wave_sum(b)};
+    if constexpr (kThreads == 64) return s;
+    if ((threadIdx.x & 63) == 0) tmp[threadIdx.x / 64] = s;
+    __syncthreads();
+    s = tmp[0];
+#pragma unroll
+    for (int i = 1; i < kThreads / 64; ++i) { s[0] += tmp[i][0]; s[1] += tmp[i][1]; }
+    return s;
+}
+
+__device__ __forceinline__ int count_at(uint32_t col, uint32_t cols) { return col >= cols ? 0 : cols - col >= 8 ? 8 : (int)(cols - col); }
+
+struct NormArgs {
+    const void *x;
+    uint64_t ld;
+    uint32_t rows, cols;
+    const float *gamma, *beta;
+    float eps;
+    void *y;
+    uint64_t ld_y;
+    float *mean, *rstd;
+    uint8_t *codes, *exps;
+    uint64_t code_stride;
+    uint32_t exp_stride;
+};
+
+template <typename T>
+__device__ __forceinline__ void norm_out(const NormArgs &a, uint64_t row, uint32_t col, int count, const float (&x)[8], float mean, float rstd) {
+    float g[8], b[8], y[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) { g[i] = 1.f; b[i] = 0.f; }
+    if (a.gamma) load_chunk(a.gamma + col, count, g);
+    if (a.beta) load_chunk(a.beta + col, count, b);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] = i < count ? fmaf((x[i] - mean) * rstd, g[i], b[i]) : 0.f;
+    if (a.y) store_chunk((T *)a.y + row * a.ld_y + col, count, y);
+    if (a.codes && col < a.code_stride) store_block(y, a.codes + row * a.code_stride + col, a.exps + row * a.exp_stride + col / kBlockCols);
+}
+
+// kThreads threads per row (64: four rows per block), kChunks chunks of eight columns each
+template <typename T, int kThreads, int kChunks>
+__global__ __launch_bounds__(kThreads < kBlock ? kBlock : kThreads) void k_norm(NormArgs a) {
+    __shared__ f2 tmp[2][kThreads / 64];
+    constexpr int kRowsHere = kThreads == 64 ? kWaves : 1;
+    const uint32_t lane = kThreads == 64 ? threadIdx.x & 63 : threadIdx.x;
+    const float per = 1.f / (float)a.cols;
+    for (uint64_t row = (uint64_t)blockIdx.x * kRowsHere + (kThreads == 64 ? threadIdx.x / 64 : 0); row < a.rows; row += (uint64_t)gridDim.x * kRowsHere) {
+        float x[kChunks][8], sum = 0.f, square = 0.f;
+#pragma unroll
+        for (int c = 0; c < kChunks; ++c) {
+            const uint32_t col = (c * kThreads + lane) * 8;
+            load_chunk((const T *)a.x + row * a.ld + col, count_at(col, a.cols), x[c]);
+        }
+#pragma unroll
+        for (int c = 0; c < kChunks; ++c)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum += x[c][i];
+        const float mean = row_sum<kThreads>(sum, 0.f, tmp[0])[0] * per;
+#pragma unroll
+        for (int c = 0; c < kChunks; ++c) {
+            const int count = count_at((c * kThreads + lane) * 8, a.cols);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float d = i < count ? x[c][i] - mean : 0.f;
+                square = fmaf(d, d, square);
+            }
+        }
+        const float rstd = 1.f / sqrtf(row_sum<kThreads>(square, 0.f, tmp[1])[0] * per + a.eps);
+        if (lane == 0) {
+            if (a.mean) a.mean[row] = mean;
+            if (a.rstd) a.rstd[row] = rstd;
+        }
+#pragma unroll
+        for (int c = 0; c < kChunks; ++c) {
+            const uint32_t col = (c * kThreads + lane) * 8;
+            norm_out<T>(a, row, col, count_at(col, a.cols), x[c], mean, rstd);
+        }
+    }
+}
+
+// rows longer than registers hold: read once for each sum and once more
+template <typename T>
+__global__ __launch_bounds__(1024) void k_norm_long(NormArgs a) {
+    __shared__ f2 tmp[2][16];
+    const float per = 1.f / (float)a.cols;
+    for (uint64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        const T *x = (const T *)a.x + row * a.ld;
+        float v[8], sum = 0.f, square = 0.f;
+        for (uint32_t col = threadIdx.x * 8; col < a.cols; col += 8192) {
+            load_chunk(x + col, count_at(col, a.cols), v);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum += v[i];
+        }
+        const float mean = row_sum<1024>(sum, 0.f, tmp[0])[0] * per;
+        for (uint32_t col = threadIdx.x * 8; col < a.cols; col += 8192) {
+            const int count = count_at(col, a.cols);
+            load_chunk(x + col, count, v);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float d = i < count ? v[i] - mean : 0.f;
+                square = fmaf(d, d, square);
+            }
+        }
+        const float rstd = 1.f / sqrtf(row_sum<1024>(square, 0.f, tmp[1])[0] * per + a.eps);
+        if (threadIdx.x == 0) {
+            if (a.mean) a.mean[row] = mean;
+            if (a.rstd) a.rstd[row] = rstd;
+        }
+        for (uint32_t col = threadIdx.x * 8; col < codes_stride(a.cols); col += 8192) {
+            const int count = count_at(col, a.cols);
+            load_chunk(x + col, count, v);
+            norm_out<T>(a, row, col, count, v, mean, rstd);
+        }
+    }
+}
+
+// ---------------------------------------------------------------- gradient
+
+struct NormGradArgs {
+    const void *dy, *x;
+    uint64_t ld_dy, ld;
+    uint32_t rows, cols;
+    const float *gamma, *mean, *rstd;
+    void *dx;
+    uint64_t ld_dx;
+    float *part;   // [blocks][2][cols] sums of the blocks' rows of dy h and of dy, h = (x - mean) rstd
+};
+
+// As k_norm; a block takes every gridDim.x-th row (or four), keeps its columns' sums in registers and writes them at its end.
+template <typename T, int kThreads, int kChunks>
+__global__ __launch_bounds__(kThreads < kBlock ? kBlock : kThreads) void k_norm_grad(NormGradArgs a) {
+    constexpr int kRowsHere = kThreads == 64 ? kWaves : 1;
+    __shared__ f2 tmp[2][kThreads / 64];
+    __shared__ float joined[kThreads == 64 ? kChunks * 64 * 8 : 1];
+    const uint32_t lane = kThreads == 64 ? threadIdx.x & 63 : threadIdx.x, wave = threadIdx.x / 64;
+    const float per = 1.f / (float)a.cols;
+    float g[kChunks][8], sum_h[kChunks][8], sum_1[kChunks][8];
+#pragma unroll
+    for (int c = 0; c < kChunks; ++c) {
+        const uint32_t col = (c * kThreads + lane) * 8;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) { g[c][i] = 1.f; sum_h[c][i] = sum_1[c][i] = 0.f; }
+        if (a.gamma) load_chunk(a.gamma + col, count_at(col, a.cols), g[c]);
+    }
+    int turn = 0;
+    for (uint64_t row = (uint64_t)blockIdx.x * kRowsHere + (kThreads == 64 ? wave : 0); row < a.rows; row += (uint64_t)gridDim.x * kRowsHere, turn ^= 1) {
+        float h[kChunks][8], dy[kChunks][8], s1 = 0.f, s2 = 0.f;
+        const float mean = a.mean[row], rstd = a.rstd[row];
+#pragma unroll
+        for (int c = 0; c < kChunks; ++c) {
+            const uint32_t col = (c * kThreads + lane) * 8;
+            const int count = count_at(col, a.cols);
+            load_chunk((const T *)a.x + row * a.ld + col, count, h[c]);
+            load_chunk((const T *)a.dy + row * a.ld_dy + col, count, dy[c]);
+        }
+#pragma unroll
+        for (int c = 0; c < kChunks; ++c)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {   // (where there is no column, dy is 0)
+                h[c][i] = (h[c][i] - mean) * rstd;
+                sum_h[c][i] = fmaf(dy[c][i], h[c][i], sum_h[c][i]);
+                sum_1[c][i] += dy[c][i];
+                dy[c][i] *= g[c][i];
+                s1 += dy[c][i];
+                s2 = fmaf(dy[c][i], h[c][i], s2);
+            }
+        const f2 s = row_sum<kThreads>(s1, s2, tmp[turn]);
+        const float c1 = s[0] * per, c2 = s[1] * per;
+        if (a.dx)
+#pragma unroll
+            for (int c = 0; c < kChunks; ++c) {
+                const uint32_t col = (c * kThreads + lane) * 8;
+                float d[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) d[i] = rstd * (dy[c][i] - c1 - h[c][i] * c2);
+                store_chunk((T *)a.dx + row * a.ld_dx + col, count_at(col, a.cols), d);
+            }
+    }
+    float *part = a.part + (uint64_t)blockIdx.x * 2 * a.cols;
+    if constexpr (kThreads == 64) {   // the four wavefronts' sums, added in their order
+#pragma unroll
+        for (int which = 0; which < 2; ++which)
+            for (int w = 0; w < kWaves; ++w) {
+                __syncthreads();
+                if ((int)wave == w)
+#pragma unroll
+                    for (int c = 0; c < kChunks; ++c)
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            const int at = (c * 8 + i) * 64 + lane;
+                            const float mine = which ? sum_1[c][i] : sum_h[c][i], all = w == 0 ? mine : joined[at] + mine;
+                            joined[at] = all;
+                            const uint32_t col = (c * 64 + lane) * 8 + i;
+                            if (w == kWaves - 1 && col < a.cols) part[(uint64_t)which * a.cols + col] = all;
+                        }
+            }
+    } else {
+#pragma unroll
+        for (int c = 0; c < kChunks; ++c) {
+            const uint32_t col = (c * kThreads + lane) * 8;
+            store_chunk(part + col, count_at(col, a.cols), sum_h[c]);
+            store_chunk(part + a.cols + col, count_at(col, a.cols), sum_1[c]);
+        }
+    }
+}
+
+// Long rows: dx alone
+template <typename T>
+__global__ __launch_bounds__(1024) void k_norm_grad_long(NormGradArgs a) {
+    __shared__ f2 tmp[2][16];
+    const float per = 1.f / (float)a.cols;
+    int turn = 0;
+    for (uint64_t row = blockIdx.x; row < a.rows; row += gridDim.x, turn ^= 1) {
+        const T *x = (const T *)a.x + row * a.ld, *dy = (const T *)a.dy + row * a.ld_dy;
+        const float mean = a.mean[row], rstd = a.rstd[row];
+        float h[8], d[8], g[8], s1 = 0.f, s2 = 0.f;
+        auto load = [&](uint32_t col, int count) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) g[i] = 1.f;
+            load_chunk(x + col, count, h);
+            load_chunk(dy + col, count, d);
+            if (a.gamma) load_chunk(a.gamma + col, count, g);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) { h[i] = (h[i] - mean) * rstd; d[i] *= g[i]; }
+        };
+        for (uint32_t col = threadIdx.x * 8; col < a.cols; col += 8192) {
+            load(col, count_at(col, a.cols));
+#pragma unroll
+            for (int i = 0; i < 8; ++i) { s1 += d[i]; s2 = fmaf(d[i], h[i], s2); }
+        }
+        const f2 s = row_sum<1024>(s1, s2, tmp[turn]);
+        const float c1 = s[0] * per, c2 = s[1] * per;
+        for (uint32_t col = threadIdx.x * 8; col < a.cols; col += 8192) {
+            const int count = count_at(col, a.cols);
+            load(col, count);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) d[i] = rstd * (d[i] - c1 - h[i] * c2);
+            store_chunk((T *)a.dx + row * a.ld_dx + col, count, d);
+        }
+    }
+}
+
+// Long rows: the columns' sums over a block's rows (every gridDim.y-th), one chunk of columns per thread
+template <typename T>
+__global__ __launch_bounds__(kBlock) void k_norm_grad_columns(NormGradArgs a) {
+    const uint32_t col = (blockIdx.x * kBlock + threadIdx.x) * 8;
+    const int count = count_at(col, a.cols);
+    if (count == 0) return;
+    float sum_h[8] = {}, sum_1[8] = {};
+    for (uint64_t row = blockIdx.y; row < a.rows; row += gridDim.y) {
+        float h[8], d[8];
+        load_chunk((const T *)a.x + row * a.ld + col, count, h);
+        load_chunk((const T *)a.dy + row * a.ld_dy + col, count, d);
+        const float mean = a.mean[row], rstd = a.rstd[row];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) { sum_h[i] = fmaf(d[i], (h[i] - mean) * rstd, sum_h[i]); sum_1[i] += d[i]; }
+    }
+    float *part = a.part + (uint64_t)blockIdx.y * 2 * a.cols;
+    store_chunk(part + col, count, sum_h);
+    store_chunk(part + a.cols + col, count, sum_1);
+}
+
+// Column sums of the blocks' partial sums, in a fixed order; blockIdx.y: which of the two
+__global__ __launch_bounds__(64 * kColumnRows) void k_norm_columns(const float *part, uint32_t blocks, uint32_t cols, float *dgamma, float *dbeta) {
+    __shared__ float tmp[kColumnRows][64];
+    float *out = blockIdx.y ? dbeta : dgamma;
+    if (!out) return;
+    const uint32_t col = blockIdx.x * 64 + (threadIdx.x & 63), wave = threadIdx.x / 64;
+    float s = 0.f;
+    if (col < cols)
+#pragma unroll 8
+        for (uint32_t p = wave; p < blocks; p += kColumnRows) s += part[((uint64_t)p * 2 + blockIdx.y) * cols + col];
+    tmp[wave][threadIdx.x & 63] = s;
+    __syncthreads();
+    if (wave == 0 && col < cols) {
+#pragma unroll
+        for (int i = 1; i < kColumnRows; ++i) s += tmp[i][threadIdx.x];
+        out[col] = s;
+    }
+}
+
+constexpr uint32_t kMostBlocks = 1u << 20;   // of a launch; a block goes on with later rows
+constexpr uint32_t kLongNorm = 32768, kLongGrad = 16384;   // columns from which on registers do not hold a row
+
+template <typename T>
+void norm_of(const NormArgs &a, hipStream_t st) {
+#define NORM(kThreads, kChunks) k_norm<T, kThreads, kChunks><<<std::min(kThreads == 64 ? (a.rows + kWaves - 1) / kWaves : a.rows, kMostBlocks), kThreads < kBlock ? kBlock : kThreads, 0, st>>>(a)
+    const uint32_t c = a.cols;
+    if (c <= 512) NORM(64, 1);
+    else if (c <= 1024) NORM(64, 2);
+    else if (c <= 2048) NORM(256, 1);
+    else if (c <= 4096) NORM(256, 2);
+    else if (c <= 8192) NORM(256, 4);
+    else if (c <= 16384) NORM(1024, 2);
+    else if (c <= kLongNorm) NORM(1024, 4);
+    else k_norm_long<T><<<std::min(a.rows, kMostBlocks), 1024, 0, st>>>(a);
+#undef NORM
+}
+
+template <typename T>
+void norm_grad_of(const NormGradArgs &a, uint32_t blocks, hipStream_t st) {
+#define GRAD(kThreads, kChunks) k_norm_grad<T, kThreads, kChunks><<<blocks, kThreads < kBlock ? kBlock : kThreads, 0, st>>>(a)
+    const uint32_t c = a.cols;
+    if (c <= 512) GRAD(64, 1);
+    else if (c <= 1024) GRAD(64, 2);
+    else if (c <= 2048) GRAD(256, 1);
+    else if (c <= 4096) GRAD(256, 2);
+    else if (c <= 8192) GRAD(1024, 1);
+    else if (c <= kLongGrad) GRAD(1024, 2);
+    else {
+        if (a.dx) k_norm_grad_long<T><<<std::min(a.rows, kMostBlocks), 1024, 0, st>>>(a);
+        k_norm_grad_columns<T><<<dim3((c + kBlock * 8 - 1) / (kBlock * 8), blocks), kBlock, 0, st>>>(a);
+    }
+#undef GRAD
+}
+
+}  // namespace
+
+void launch_norm(const void *x, lgc_type type, uint32_t rows, uint32_t cols, uint64_t ld, const float *gamma, const float *beta, float eps, void *y, uint64_t ld_y,
+                 float *mean, float *rstd, uint8_t *codes, uint8_t *exps, hipStream_t st) {
+    const NormArgs a{x, ld, rows, cols, gamma, beta, eps, y, ld_y, mean, rstd, codes, exps, codes_stride(cols), (uint32_t)exps_stride(cols)};
+    if (type == LGC_FP32) norm_of<float>(a, st);
+    else norm_of<Bf16>(a, st);
+}
+
+void launch_norm_grad(const void *dy, uint64_t ld_dy, const void *x, uint64_t ld, lgc_type type, uint32_t rows, uint32_t cols, const float *gamma, const float *mean,
+                      const float *rstd, void *dx, uint64_t ld_dx, float *dgamma, float *dbeta, float *scratch, size_t scratch_floats, int cus, hipStream_t st) {
+    const uint32_t rows_at_once = cols <= 1024 ? kWaves : 1;
+    uint32_t blocks = cols > kLongGrad ? 64 : (uint32_t)cus * (cols <= 4096 ? 4 : cols <= 8192 ? 2 : 1);
+    const uint32_t most = (uint32_t)(scratch_floats / (2 * (size_t)cols));
+    if (blocks > most) blocks = most;
+    if (blocks > (rows + rows_at_once - 1) / rows_at_once) blocks = (rows + rows_at_once - 1) / rows_at_once;
+    const NormGradArgs a{dy, x, ld_dy, ld, rows, cols, gamma, mean, rstd, dx, ld_dx, scratch};
+    if (rows) {
+        if (type == LGC_FP32) norm_grad_of<float>(a, blocks, st);
+        else norm_grad_of<Bf16>(a, blocks, st);
+    }
+    if (dgamma || dbeta) k_norm_columns<<<dim3((cols + 63) / 64, 2), 64 * kColumnRows, 0, st>>>(scratch, blocks, cols, dgamma, dbeta);
+}
+
+}  // namespace lgc
