@@ -1,4 +1,6 @@
 // Products of matrices in 8 bits: y = A B^T + bias, A [m][k] with an exponent per row and 128 columns, B [n][k] with one per 128 x 128.
+#include <algorithm>
+
 #include "blocks.h"
 
 namespace lgc {
@@ -7,11 +9,16 @@ namespace {
 typedef int i8 __attribute__((ext_vector_type(8)));
 typedef int i4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf8 __attribute__((ext_vector_type(8)));
+typedef float f16 __attribute__((ext_vector_type(16)));
+typedef __attribute__((address_space(3))) void *Lds;
+typedef const __attribute__((address_space(1))) void *Global;
 
 struct ProductArgs {
     const uint8_t *a, *a_exps, *b, *b_exps;
     uint32_t m, n, blocks;   // blocks of 128 that a row has
     uint32_t exp_stride;
+    uint32_t tiles_m, tiles_n;
+    uint32_t share;          // blocks of 128 per part; blockIdx.y: which part
     const float *bias;
     void *y;
     uint64_t ld;
@@ -24,83 +31,230 @@ __device__ __forceinline__ bf8 bf16_of(int lo, int hi, float scale) {
     return bf8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
-// acc += the 16 x 16 x 128 product of a lane's 32 codes of B's rows and 32 of A's, times 2^(eb - 127) 2^(ea - 127).
-// To bf16, the products of the codes themselves; the matrix cores add eight neighbouring products with some 14 bits below the largest one's, and
-// these sums in fp32: 1.5e-5 of the result for normal inputs, which rounding to bf16 hides.  To fp32, products of the values as bf16, which are exact.
-template <typename T>
-__device__ __forceinline__ f4 multiply(const i8 b, const i8 a, f4 acc, uint32_t eb, uint32_t ea) {
-    if constexpr (sizeof(T) == 2) return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b, a, acc, 0, 0, 0, eb, 0, ea);
-    else {
-        const float sb = exp_scale(eb & 255), sa = exp_scale(ea & 255);
+// Which tile a block works on.  Blocks go to the eight XCDs in turn: each XCD gets neighbours, in bands of kBand tiles of m, whose rows its L2 holds.
+__device__ __forceinline__ void tile_of(uint32_t id, uint32_t tiles_m, uint32_t tiles_n, uint32_t &tm, uint32_t &tn) {
+    constexpr uint32_t kBand = 4;
+    const uint32_t all = tiles_m * tiles_n, xcd = id & 7, q = all >> 3, r = all & 7;
+    id = xcd * q + min(xcd, r) + (id >> 3);
+    const uint32_t band = id / (kBand * tiles_n), in = id - band * kBand * tiles_n, high = min(kBand, tiles_m - band * kBand);
+    tn = in / high;
+    tm = band * kBand + in - tn * high;
+}
+
+// To bf16, products of the codes themselves, with the scales applied by the matrix cores, which add eight neighbouring products with some 14 bits below
+// the largest one's, and these sums in fp32: 1.5e-5 of the result for normal inputs, which rounding to bf16 hides.  To fp32 (kExact), products of the
+// values as bf16, which are exact, at half the rate.
+//
+// A tile of 2 kWave x 2 kWave per block, a quarter per wavefront.  Columns come in steps of 64: loads go straight to LDS, into a ring of four steps, four
+// steps ahead of the products; a step's fragments are read while the products of the step before run.  A row's four pieces of 16 bytes are exchanged in LDS
+// by its number, so that 8 and 16 neighbouring rows' pieces meet all banks.
+template <typename T, int kWave, bool kExact>
+__global__ __launch_bounds__(kBlock, 1) void k_product(ProductArgs p) {
+    constexpr int kTile = 2 * kWave, kSide = kWave / 32, kStep = 64, kRing = 4, kHalf = kTile * kStep, kLoads = 2 * kHalf / (kBlock * 16);
+    // One array: told apart from another one, loads into it would be waited for before every read of it.
+    __shared__ __align__(16) uint8_t lds[kRing * 2 * kHalf + 2 * kTile * 4];
+    uint8_t *const exps = lds + kRing * 2 * kHalf;
+    uint32_t tm, tn;
+    tile_of(blockIdx.x, p.tiles_m, p.tiles_n, tm, tn);
+    const uint32_t m0 = tm * kTile, n0 = tn * kTile, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const uint32_t wm = (wave & 1) * kWave, wn = (wave >> 1) * kWave, r = lane & 31, g = lane >> 5;
+    const uint32_t kb0 = blockIdx.y * p.share, kb1 = min(kb0 + p.share, p.blocks);
+    const uint64_t stride = (uint64_t)p.blocks * kBlockCols;
+    auto swap = [](uint32_t row) { return (row >> 1 & 3) ^ (row >> 3 & 1); };
+
+    // loads: 16 rows of 64 bytes per wavefront and load, first all of A's, then B's
+    const uint8_t *a = p.a + (uint64_t)m0 * stride + (uint64_t)kb0 * kBlockCols, *b = p.b + (uint64_t)n0 * stride + (uint64_t)kb0 * kBlockCols;
+    uint32_t from[kLoads];
 #pragma unroll
-        for (int i = 0; i < 8; i += 2) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bf16_of(b[i], b[i + 1], sb), bf16_of(a[i], a[i + 1], sa), acc, 0, 0, 0);
-        return acc;
+    for (int i = 0; i < kLoads; ++i) {
+        const uint32_t row = ((i % (kLoads / 2)) * kWaves + wave) * 16 + lane / 4, last = (i < kLoads / 2 ? p.m - m0 : p.n - n0) - 1;
+        from[i] = min(row, last) * (uint32_t)stride + ((lane & 3) ^ swap(row)) * 16;
+    }
+    auto load = [&](uint32_t step, uint32_t slot) {
+        const uint8_t *at[2] = {a + (uint64_t)step * kStep, b + (uint64_t)step * kStep};
+        asm("" : "+s"(at[0]), "+s"(at[1]));   // (scalar base, one vector register of offset)
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i)
+            __builtin_amdgcn_global_load_lds((Global)(at[i / (kLoads / 2)] + from[i]),
+                                             (Lds)(lds + slot * (2 * kHalf) + i / (kLoads / 2) * kHalf + ((i % (kLoads / 2)) * kWaves + wave) * 1024), 16, 0, 0);
+    };
+    const uint32_t piece[2] = {r * kStep + ((2 * g) ^ swap(r)) * 16, r * kStep + ((2 * g + 1) ^ swap(r)) * 16};   // (32 rows on, the exchange is the same)
+    auto fragment = [&](const uint8_t *at) {
+        const i4 lo = *(const i4 *)(at + piece[0]), hi = *(const i4 *)(at + piece[1]);
+        return i8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+    };
+    i8 fa[2][kSide], fb[2][kSide];
+    auto fragments = [&](int set, uint32_t slot) {
+#pragma unroll
+        for (int i = 0; i < kSide; ++i) {
+            fb[set][i] = fragment(lds + slot * (2 * kHalf) + kHalf + (wn + 32 * i) * kStep);
+            fa[set][i] = fragment(lds + slot * (2 * kHalf) + (wm + 32 * i) * kStep);
+        }
+    };
+    f16 acc[kSide][kSide] = {};
+    // exponents of A's rows: four blocks' at once, to LDS, a group of four ahead; B's, of the wavefront's columns
+    static_assert(kTile == kBlock || kTile == kBlock / 2, "a row per thread");
+    const uint8_t *a_exps = p.a_exps + (uint64_t)min(m0 + threadIdx.x % kTile, p.m - 1) * p.exp_stride;
+    typedef const __attribute__((address_space(4))) uint32_t *Scalar;
+    const Scalar b_exps = (Scalar)(p.b_exps + (uint64_t)(min(n0 + wn, p.n - 1) / kBlockCols) * p.exp_stride);
+    auto exponents = [&](uint32_t four) {   // (of 128 rows, two wavefronts write the same twice)
+        __builtin_amdgcn_global_load_lds((Global)(a_exps + 4 * four), (Lds)(exps + (four & 1) * (kTile * 4) + wave * 64 % kTile * 4), 4, 0, 0);
+    };
+    uint32_t ea[kSide], eb, ea_next[kSide], eb_next;
+    auto next_exponents = [&](uint32_t kb) {
+#pragma unroll
+        for (int i = 0; i < kSide; ++i) ea_next[i] = ((const uint32_t *)(exps + (kb >> 2 & 1) * (kTile * 4)))[wm + 32 * i + r];
+        eb_next = b_exps[kb >> 2];
+    };
+    auto multiply = [&](int set) {
+        if constexpr (!kExact) {
+#pragma unroll
+            for (int i = 0; i < kSide; ++i)
+#pragma unroll
+                for (int j = 0; j < kSide; ++j) acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fb[set][j], fa[set][i], acc[i][j], 0, 0, 0, eb, 0, ea[i]);
+        } else {
+#pragma unroll
+            for (int q = 0; q < 8; q += 2) {
+                bf8 x[kSide];
+#pragma unroll
+                for (int i = 0; i < kSide; ++i) x[i] = bf16_of(fa[set][i][q], fa[set][i][q + 1], exp_scale(ea[i] & 255));
+#pragma unroll
+                for (int j = 0; j < kSide; ++j) {
+                    const bf8 w = bf16_of(fb[set][j][q], fb[set][j][q + 1], exp_scale(eb & 255));
+#pragma unroll
+                    for (int i = 0; i < kSide; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w, x[i], acc[i][j], 0, 0, 0);
+                }
+            }
+        }
+    };
+    // The wavefront's own loads but the latest `kLeft`, then everybody's: a step's loads and the reads of the step that lay in its place.  The fences keep
+    // the LDS reads on their side.
+    auto meet = [&](auto left) {
+        constexpr int kLeft = decltype(left)::value;
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_waitcnt(0x0070 | (kLeft & 15) | (kLeft >> 4) << 14);   // vmcnt(kLeft), lgkmcnt(0)
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+    const uint32_t steps = 2 * (kb1 - kb0), last = steps - 1;
+    exponents(kb0 / 4);
+#pragma unroll
+    for (int i = 0; i < kRing; ++i) load(min((uint32_t)i, last), i);
+    meet(std::integral_constant<int, 3 * kLoads>());
+    fragments(0, 0);
+    next_exponents(kb0);
+    for (uint32_t kb = kb0; kb < kb1; ++kb) {
+        if ((kb & 3) == 0 && kb / 4 < (kb1 - 1) / 4) exponents(kb / 4 + 1);
+#pragma unroll
+        for (int i = 0; i < kSide; ++i) ea[i] = ea_next[i] >> 8 * (kb & 3);
+        eb = eb_next >> 8 * (kb & 3);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const uint32_t s = 2 * (kb - kb0) + h;
+            meet(std::integral_constant<int, 2 * kLoads>());
+            fragments(h ^ 1, (s + 1) & (kRing - 1));
+            if (h == 1) next_exponents(min(kb + 1, kb1 - 1));
+            load(min(s + kRing, last), s & (kRing - 1));
+            multiply(h);
+            if constexpr (!kExact) {   // the next step's reads, then the loads, between the products
+                constexpr int kHalfOf = kSide * kSide / 2;
+#pragma unroll
+                for (int i = 0; i < kHalfOf; ++i) {
+                    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x100, 4 * kSide / kHalfOf, 0);
+                }
+#pragma unroll
+                for (int i = 0; i < kHalfOf; ++i) {
+                    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x020, kLoads / kHalfOf, 0);
+                }
+            }
+        }
+    }
+    meet(std::integral_constant<int, 0>());   // nothing may arrive in LDS any more
+
+    // Lane: row r of 32, columns 8 c + 4 g + 0 .. 3 of 32.  Rows go through LDS, 32 at a time and each wavefront for itself, to be stored in whole lines.
+    constexpr int kPitch = kWave + 4, kPer = 16 / (int)sizeof(T), kPieces = kWave / kPer;
+    float *mine = (float *)lds + wave * 32 * kPitch;
+    static_assert(4 * 32 * kPitch * 4 <= (int)sizeof lds && 64 % kPieces == 0, "room; a lane has the same columns of every row");
+    T *y = (T *)p.y + (gridDim.y > 1 ? (uint64_t)blockIdx.y * p.m * p.ld : 0);
+    const uint32_t col = lane % kPieces * kPer, n = n0 + wn + col;
+    const int count = n >= p.n ? 0 : p.n - n >= kPer ? kPer : (int)(p.n - n);
+    float bias[kPer];
+#pragma unroll
+    for (int d = 0; d < kPer; ++d) bias[d] = p.bias && d < count ? p.bias[n + d] : 0.f;
+#pragma unroll
+    for (int i = 0; i < kSide; ++i) {
+#pragma unroll
+        for (int j = 0; j < kSide; ++j)
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+                *(f4 *)(mine + r * kPitch + 32 * j + 8 * c + 4 * g) = f4{acc[i][j][4 * c], acc[i][j][4 * c + 1], acc[i][j][4 * c + 2], acc[i][j][4 * c + 3]};
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll 4
+        for (int s = 0; s < 32 * kPieces / 64; ++s) {
+            const uint32_t row = s * (64 / kPieces) + lane / kPieces, m = m0 + wm + 32 * i + row;
+            float v[kPer];
+#pragma unroll
+            for (int d = 0; d < kPer; d += 4) {
+                const f4 q = *(const f4 *)(mine + row * kPitch + col + d);
+                v[d] = q[0] + bias[d]; v[d + 1] = q[1] + bias[d + 1]; v[d + 2] = q[2] + bias[d + 2]; v[d + 3] = q[3] + bias[d + 3];
+            }
+            T *at = y + (uint64_t)m * p.ld + n;
+            if (m >= p.m) continue;
+            if (count == kPer) {
+                if constexpr (sizeof(T) == 2) *(u4e *)at = u4{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7])};
+                else *(f4u *)at = f4{v[0], v[1], v[2], v[3]};
+            } else
+#pragma unroll
+                for (int d = 0; d < kPer; ++d)
+                    if (d < count) store_one(at + d, v[d]);
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
 }
 
-// A tile of 128 x 128 per block, 64 x 64 per wavefront
+// y = bias + the sum of `parts` arrays [m][n], in their order
 template <typename T>
-__global__ __launch_bounds__(kBlock) void k_product(ProductArgs p) {
-    __shared__ __align__(16) uint8_t lds[2][128 * 128];
-    const uint32_t m0 = blockIdx.x * 128, n0 = blockIdx.y * 128, lane = threadIdx.x & 63, wave = threadIdx.x / 64;
-    const uint32_t wm = (wave & 1) * 64, wn = (wave >> 1) * 64, r = lane & 15, g = lane >> 4;
-    const uint64_t stride = (uint64_t)p.blocks * kBlockCols;
-    f4 acc[4][4] = {};
-    for (uint32_t kb = 0; kb < p.blocks; ++kb) {
-        u4 x[2][4];
+__global__ __launch_bounds__(kBlock) void k_join(const float *part, uint32_t parts, uint32_t m, uint32_t n, Divide chunks, const float *bias, T *y, uint64_t ld) {
+    const uint64_t id = (uint64_t)blockIdx.x * kBlock + threadIdx.x;
+    if (id >= (uint64_t)m * chunks.by) return;
+    const uint32_t row = quotient((uint32_t)id, chunks), col = ((uint32_t)id - row * chunks.by) * 8;
+    const int count = n - col >= 8 ? 8 : (int)(n - col);
+    float s[8] = {}, v[8];
+    if (bias) load_chunk(bias + col, count, s);
+    for (uint32_t i = 0; i < parts; ++i) {
+        load_chunk(part + ((uint64_t)i * m + row) * n + col, count, v);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint32_t row = threadIdx.x / 8 + 32 * i;
-            x[0][i] = *(const u4 *)(p.a + min(m0 + row, p.m - 1) * stride + kb * 128 + (threadIdx.x & 7) * 16);
-            x[1][i] = *(const u4 *)(p.b + min(n0 + row, p.n - 1) * stride + kb * 128 + (threadIdx.x & 7) * 16);
-        }
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint32_t row = threadIdx.x / 8 + 32 * i, at = row * 128 + (((threadIdx.x & 7) ^ (row & 7)) * 16);
-            *(u4 *)(lds[0] + at) = x[0][i];
-            *(u4 *)(lds[1] + at) = x[1][i];
-        }
-        __syncthreads();
-        auto fragment = [&](const uint8_t *tile, uint32_t row) {
-            const i4 lo = *(const i4 *)(tile + row * 128 + (((2 * g) ^ (row & 7)) * 16)), hi = *(const i4 *)(tile + row * 128 + (((2 * g + 1) ^ (row & 7)) * 16));
-            return i8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-        };
-        const uint32_t eb = p.b_exps[(uint64_t)(n0 / 128) * p.exp_stride + kb];
-        i8 b[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) b[j] = fragment(lds[1], wn + 16 * j + r);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const i8 a = fragment(lds[0], wm + 16 * i + r);
-            const uint32_t ea = p.a_exps[(uint64_t)min(m0 + wm + 16 * i + r, p.m - 1) * p.exp_stride + kb];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) acc[i][j] = multiply<T>(b[j], a, acc[i][j], eb, ea);
-        }
+        for (int j = 0; j < 8; ++j) s[j] += v[j];
     }
-    // lane: row r of the 16, columns 4 g .. of the 16
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const uint32_t row = m0 + wm + 16 * i + r;
-        if (row >= p.m) continue;
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                const uint32_t col = n0 + wn + 16 * j + 4 * g + c;
-                if (col < p.n) store_one((T *)p.y + row * p.ld + col, acc[i][j][c] + (p.bias ? p.bias[col] : 0.f));
-            }
-    }
+    store_chunk(y + (uint64_t)row * ld + col, count, s);
 }
 
 }  // namespace
 
 void launch_product(const uint8_t *a, const uint8_t *a_exps, const uint8_t *b, const uint8_t *b_exps, uint32_t m, uint32_t n, uint32_t k, const float *bias, void *y,
                     lgc_type type, uint64_t ld, float *scratch, size_t scratch_floats, int cus, hipStream_t st) {
-    const ProductArgs p{a, a_exps, b, b_exps, m, n, (uint32_t)block_count(k), (uint32_t)exps_stride(k), bias, y, ld};
-    const dim3 grid((m + 127) / 128, (n + 127) / 128);
-    if (type == LGC_FP32) k_product<float><<<grid, kBlock, 0, st>>>(p);
-    else k_product<Bf16><<<grid, kBlock, 0, st>>>(p);
+    auto tiles = [&](uint32_t side) { return (uint64_t)((m + side - 1) / side) * ((n + side - 1) / side); };
+    const uint32_t blocks = (uint32_t)block_count(k);
+    const bool large = type == LGC_BF16 && tiles(256) >= (uint64_t)cus;
+    const uint32_t side = large ? 256 : 128;
+    uint64_t parts = std::max<uint64_t>(1, 2 * (uint64_t)cus / tiles(side));
+    parts = std::max<uint64_t>(1, std::min({parts, (uint64_t)blocks / 4, scratch_floats / ((uint64_t)m * n)}));
+    const uint32_t share = (uint32_t)((blocks + parts - 1) / parts + 3) / 4 * 4;   // whole groups of exponents
+    parts = (blocks + share - 1) / share;
+    ProductArgs p{a, a_exps, b, b_exps, m, n, blocks, (uint32_t)exps_stride(k), (m + side - 1) / side, (n + side - 1) / side, share, bias, y, ld};
+    if (parts > 1) { p.bias = nullptr; p.y = scratch; p.ld = n; }
+    const dim3 grid((uint32_t)tiles(side), (uint32_t)parts);
+    if (large) k_product<Bf16, 128, false><<<grid, kBlock, 0, st>>>(p);
+    else if (type == LGC_FP32) k_product<float, 64, true><<<grid, kBlock, 0, st>>>(p);
+    else if (parts > 1) k_product<float, 64, false><<<grid, kBlock, 0, st>>>(p);
+    else k_product<Bf16, 64, false><<<grid, kBlock, 0, st>>>(p);
+    if (parts == 1) return;
+    const uint32_t chunks = (n + 7) / 8;
+    const uint32_t join = (uint32_t)(((uint64_t)m * chunks + kBlock - 1) / kBlock);
+    if (type == LGC_FP32) k_join<float><<<join, kBlock, 0, st>>>(scratch, (uint32_t)parts, m, n, divide_by(chunks), bias, (float *)y, ld);
+    else k_join<Bf16><<<join, kBlock, 0, st>>>(scratch, (uint32_t)parts, m, n, divide_by(chunks), bias, (Bf16 *)y, ld);
 }
 
 }  // namespace lgc
