@@ -31,6 +31,13 @@ __device__ __forceinline__ bf8 bf16_of(int lo, int hi, float scale) {
     return bf8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
+// The same for all lanes
+__device__ __forceinline__ const uint8_t *scalar(const uint8_t *p) {
+    const uint64_t x = (uint64_t)p;
+    const uint32_t high = __builtin_amdgcn_readfirstlane((uint32_t)(x >> 32)), low = __builtin_amdgcn_readfirstlane((uint32_t)x);   // (it gives an int, which must not be widened)
+    return (const uint8_t *)((uint64_t)high << 32 | low);
+}
+
 // Which tile a block works on.  Blocks go to the eight XCDs in turn: each XCD gets neighbours, in bands of kBand tiles of m, whose rows its L2 holds.
 __device__ __forceinline__ void tile_of(uint32_t id, uint32_t tiles_m, uint32_t tiles_n, uint32_t &tm, uint32_t &tn) {
     constexpr uint32_t kBand = 4;
@@ -51,39 +58,49 @@ __device__ __forceinline__ void tile_of(uint32_t id, uint32_t tiles_m, uint32_t 
 template <typename T, int kSideM, int kSideN, int kWavesM, int kWavesN, bool kExact>
 __global__ __launch_bounds__(64 * kWavesM * kWavesN) void k_product(ProductArgs p) {
     constexpr int kWaveM = 32 * kSideM, kWaveN = 32 * kSideN, kTile = kWaveM * kWavesM, kAll = kWavesM * kWavesN;
-    constexpr int kHalf = kTile * kBlockCols, kPlace = 2 * kHalf, kLoads = kPlace / (kAll * 1024);
+    constexpr int kHalf = kTile * kBlockCols, kPlace = 2 * kHalf, kLoads = kPlace / (kAll * 1024), kExps = 2 * kTile * 4;
+    constexpr int kPer = 16 / (int)sizeof(T), kPitch = 64 + kPer, kRows = kAll * 32 * kPitch * (int)sizeof(T), kBias = kTile * 4;
     static_assert(kTile == kWaveN * kWavesN, "square tiles");
+    static_assert(kAll * 64 % kTile == 0, "a row per thread");
+    static_assert(kRows <= 2 * kPlace, "room");
     // One array: told apart from another one, loads into it would be waited for before every read of it.
-    __shared__ __align__(16) uint8_t lds[2 * kPlace + 2 * kTile * 4];
-    uint8_t *const exps = lds + 2 * kPlace;
-    uint32_t tm, tn;
-    tile_of(blockIdx.x, p.tiles_m, p.tiles_n, tm, tn);
-    const uint32_t m0 = tm * kTile, n0 = tn * kTile, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    __shared__ __align__(16) uint8_t lds[kExps + kBias + 2 * kPlace];
+    uint8_t *const exps = lds, *const biases = lds + kExps, *const places = biases + kBias;
+    const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const uint32_t wm = wave % kWavesM * kWaveM, wn = wave / kWavesM * kWaveN, r = lane & 31, g = lane >> 5;
     const uint32_t kb0 = blockIdx.y * p.share, kb1 = min(kb0 + p.share, p.blocks);
     const uint64_t stride = (uint64_t)p.blocks * kBlockCols;
     auto swap = [](uint32_t row) { return (row & 7) ^ (row >> 3 & 1); };
 
-    // loads: 8 rows per wavefront and load, first all of A's, then B's
-    const uint8_t *a = p.a + (uint64_t)m0 * stride, *b = p.b + (uint64_t)n0 * stride;
-    uint32_t from[kLoads];
-#pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-        const uint32_t row = ((i % (kLoads / 2)) * kAll + wave) * 8 + lane / 8, last = (i < kLoads / 2 ? p.m - m0 : p.n - n0) - 1;
-        from[i] = min(row, last) * (uint32_t)stride + ((lane & 7) ^ swap(row)) * 16;
-    }
-    auto load = [&](uint32_t kb, uint32_t place) {
-        const uint8_t *at[2] = {a + (uint64_t)kb * kBlockCols, b + (uint64_t)kb * kBlockCols};   // scalar: a load's own part is one register
-        asm("" : "+s"(at[0]));
-        asm("" : "+s"(at[1]));
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            uint32_t mine = from[i];
-            asm("" : "+v"(mine));
-            __builtin_amdgcn_global_load_lds((Global)(at[i / (kLoads / 2)] + mine),
-                                             (Lds)(lds + place * kPlace + i / (kLoads / 2) * kHalf + ((i % (kLoads / 2)) * kAll + wave) * 1024), 16, 0, 0);
-        }
+    uint32_t tm, tn;
+    tile_of(blockIdx.x, p.tiles_m, p.tiles_n, tm, tn);
+    const uint32_t m0 = tm * kTile, n0 = tn * kTile;
+    // loads: 8 rows per wavefront and load, first all of A's, then B's; rows that do not exist are the last one that does
+    const uint8_t *const a = p.a + (uint64_t)m0 * stride, *const b = p.b + (uint64_t)n0 * stride;
+    const uint32_t from = (wave * 8 + lane / 8) * (uint32_t)stride, part = ((lane & 7) ^ swap(wave * 8 + lane / 8)) * 16, further = kAll * 8 * (uint32_t)stride;
+    const uint32_t last_a = (min(p.m - m0, (uint32_t)kTile) - 1) * (uint32_t)stride, last_b = (min(p.n - n0, (uint32_t)kTile) - 1) * (uint32_t)stride;
+    static_assert(kAll % 2 == 0, "the exchange is the same for all of a wavefront's loads");
+    const uint8_t *const a_exps = p.a_exps + (uint64_t)min(m0 + threadIdx.x % kTile, p.m - 1) * p.exp_stride;
+    typedef const __attribute__((address_space(4))) uint32_t *Scalar;
+    const Scalar b_exps = (Scalar)(p.b_exps + (uint64_t)(min(n0 + wn, p.n - 1) / kBlockCols) * p.exp_stride);
+    auto load = [&](uint32_t kb, int i) {
+        const uint8_t *const at = scalar((i < kLoads / 2 ? a : b) + (uint64_t)kb * kBlockCols);   // (a load's own part is one register)
+        uint32_t mine = from;
+        asm("" : "+v"(mine) : "s"(kb));   // (worked out here, not kept in registers for every load)
+        mine = min(mine + i % (kLoads / 2) * further, i < kLoads / 2 ? last_a : last_b) + part;
+        __builtin_amdgcn_global_load_lds((Global)(at + mine), (Lds)(places + (kb & 1) * kPlace + i / (kLoads / 2) * kHalf + ((i % (kLoads / 2)) * kAll + wave) * 1024), 16, 0, 0);
     };
+    // exponents of A's rows: four blocks' at once, to LDS, a group of four ahead; B's, of the wavefront's columns
+    auto exponents = [&](uint32_t four) {   // (two wavefronts write the same)
+        __builtin_amdgcn_global_load_lds((Global)(a_exps + 4 * four), (Lds)(exps + (four & 1) * (kTile * 4) + wave * 64 % kTile * 4), 4, 0, 0);
+    };
+    uint32_t ea[kSideM], eb, ea_next[kSideM], eb_next;
+    auto next_exponents = [&](uint32_t kb) {
+#pragma unroll
+        for (int i = 0; i < kSideM; ++i) ea_next[i] = ((const uint32_t *)(exps + (kb >> 2 & 1) * (kTile * 4)))[wm + 32 * i + r];
+        eb_next = b_exps[kb >> 2];
+    };
+
     uint32_t piece[2][2];   // of a half: 32 bytes of the lane's row (32 rows on, the exchange is the same)
 #pragma unroll
     for (int h = 0; h < 2; ++h)
@@ -94,42 +111,27 @@ __global__ __launch_bounds__(64 * kWavesM * kWavesN) void k_product(ProductArgs 
         return i8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
     };
     i8 fa[2][kSideM], fb[2][kSideN];
-    auto fragments = [&](int h, uint32_t place) {
-#pragma unroll
-        for (int j = 0; j < kSideN; ++j) fb[h][j] = fragment(lds + place * kPlace + kHalf + (wn + 32 * j) * kBlockCols, h);
-#pragma unroll
-        for (int i = 0; i < kSideM; ++i) fa[h][i] = fragment(lds + place * kPlace + (wm + 32 * i) * kBlockCols, h);
+    auto read = [&](int h, uint32_t kb, int i) {   // one of the kSideN + kSideM
+        const uint8_t *at = places + (kb & 1) * kPlace;
+        if (i < kSideN) fb[h][i] = fragment(at + kHalf + (wn + 32 * i) * kBlockCols, h);
+        else fa[h][i - kSideN] = fragment(at + (wm + 32 * (i - kSideN)) * kBlockCols, h);
     };
     f16 acc[kSideM][kSideN] = {};
-    // exponents of A's rows: four blocks' at once, to LDS, a group of four ahead; B's, of the wavefront's columns
-    static_assert(kAll * 64 == 2 * kTile, "a row per thread, twice");
-    const uint8_t *a_exps = p.a_exps + (uint64_t)min(m0 + threadIdx.x % kTile, p.m - 1) * p.exp_stride;
-    typedef const __attribute__((address_space(4))) uint32_t *Scalar;
-    const Scalar b_exps = (Scalar)(p.b_exps + (uint64_t)(min(n0 + wn, p.n - 1) / kBlockCols) * p.exp_stride);
-    auto exponents = [&](uint32_t four) {   // (two wavefronts write the same)
-        __builtin_amdgcn_global_load_lds((Global)(a_exps + 4 * four), (Lds)(exps + (four & 1) * (kTile * 4) + wave * 64 % kTile * 4), 4, 0, 0);
-    };
-    uint32_t ea[kSideM], eb, ea_next[kSideM], eb_next;
-    auto next_exponents = [&](uint32_t kb) {
-#pragma unroll
-        for (int i = 0; i < kSideM; ++i) ea_next[i] = ((const uint32_t *)(exps + (kb >> 2 & 1) * (kTile * 4)))[wm + 32 * i + r];
-        eb_next = b_exps[kb >> 2];
-    };
-    auto multiply = [&](int set) {
+    auto multiply = [&](int h) {
         if constexpr (!kExact) {
 #pragma unroll
             for (int i = 0; i < kSideM; ++i)
 #pragma unroll
-                for (int j = 0; j < kSideN; ++j) acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fb[set][j], fa[set][i], acc[i][j], 0, 0, 0, eb, 0, ea[i]);
+                for (int j = 0; j < kSideN; ++j) acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fb[h][j], fa[h][i], acc[i][j], 0, 0, 0, eb, 0, ea[i]);
         } else {
 #pragma unroll
             for (int q = 0; q < 8; q += 2) {
                 bf8 x[kSideM];
 #pragma unroll
-                for (int i = 0; i < kSideM; ++i) x[i] = bf16_of(fa[set][i][q], fa[set][i][q + 1], exp_scale(ea[i] & 255));
+                for (int i = 0; i < kSideM; ++i) x[i] = bf16_of(fa[h][i][q], fa[h][i][q + 1], exp_scale(ea[i] & 255));
 #pragma unroll
                 for (int j = 0; j < kSideN; ++j) {
-                    const bf8 w = bf16_of(fb[set][j][q], fb[set][j][q + 1], exp_scale(eb & 255));
+                    const bf8 w = bf16_of(fb[h][j][q], fb[h][j][q + 1], exp_scale(eb & 255));
 #pragma unroll
                     for (int i = 0; i < kSideM; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w, x[i], acc[i][j], 0, 0, 0);
                 }
@@ -137,91 +139,106 @@ __global__ __launch_bounds__(64 * kWavesM * kWavesN) void k_product(ProductArgs 
         }
     };
     // Every wavefront's loads have arrived and its reads are done.
-    auto meet = [&] {
+    auto meet = [] {
         asm volatile("" ::: "memory");
         __builtin_amdgcn_s_waitcnt(0x0070);   // vmcnt(0), lgkmcnt(0)
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
     };
+    constexpr int kReads = kSideM + kSideN, kProducts = kSideM * kSideN;
+
+    if (p.bias) __builtin_amdgcn_global_load_lds((Global)(p.bias + min(n0 + threadIdx.x % kTile, p.n - 1)), (Lds)(biases + wave * 64 % kTile * 4), 4, 0, 0);
+    else ((float *)biases)[threadIdx.x % kTile] = 0.f;
     exponents(kb0 / 4);
-    load(kb0, kb0 & 1);
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) load(kb0, i);
     meet();
-    load(min(kb0 + 1, kb1 - 1), ~kb0 & 1);
-    fragments(0, kb0 & 1);
+#pragma unroll
+    for (int i = 0; i < kReads; ++i) read(0, kb0, i);
     next_exponents(kb0);
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) load(kb0 + 1 < kb1 ? kb0 + 1 : kb0, i);   // (a block alone: the same again, in its place)
     for (uint32_t kb = kb0; kb < kb1; ++kb) {
         if ((kb & 3) == 0 && kb / 4 < (kb1 - 1) / 4) exponents(kb / 4 + 1);
 #pragma unroll
         for (int i = 0; i < kSideM; ++i) ea[i] = ea_next[i] >> 8 * (kb & 3);
         eb = eb_next >> 8 * (kb & 3);
-        fragments(1, kb & 1);
+#pragma unroll
+        for (int i = 0; i < kReads; ++i) read(1, kb, i);
         multiply(0);
-        if constexpr (!kExact) {   // the reads of the next half go between the products
+        if constexpr (!kExact)   // where the compiler is to place the reads: between the products
 #pragma unroll
-            for (int i = 0; i < kSideM * kSideN / 2; ++i) {
+            for (int i = 0; i < kProducts; ++i) {
                 __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-                __builtin_amdgcn_sched_group_barrier(0x100, 2 * (kSideM + kSideN) / (kSideM * kSideN / 2), 0);
+                if (i < kReads) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
             }
-        }
         meet();
-        fragments(0, ~kb & 1);
+        // of the next block (past the last one: what lies there is not used) and, in the place of this one, of two on (the last ones: once more, so
+        // that the loop has no branch)
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            if (i < kReads) read(0, kb + 1, i);
+            load(kb + 2 < kb1 ? kb + 2 : kb, i);
+        }
         next_exponents(min(kb + 1, kb1 - 1));
-        load(min(kb + 2, kb1 - 1), kb & 1);
         multiply(1);
-        if constexpr (!kExact) {   // and so do the loads
+        if constexpr (!kExact)
 #pragma unroll
-            for (int i = 0; i < kSideM * kSideN / 2; ++i) {
+            for (int i = 0; i < kProducts; ++i) {
                 __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-                __builtin_amdgcn_sched_group_barrier(0x100, 2 * (kSideM + kSideN) / (kSideM * kSideN / 2), 0);
+                if (i < kReads) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+                __builtin_amdgcn_sched_group_barrier(0x020, kLoads / kProducts, 0);
             }
-#pragma unroll
-            for (int i = 0; i < kSideM * kSideN / 2; ++i) {
-                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-                __builtin_amdgcn_sched_group_barrier(0x020, kLoads / (kSideM * kSideN / 2), 0);
-            }
-        }
     }
-    meet();   // nothing may arrive in LDS any more
+    meet();   // nothing may arrive any more where the rows go
 
-    // Lane: row r of 32, columns 8 c + 4 g + 0 .. 3 of 32.  Rows go through LDS, 32 at a time and each wavefront for itself, to be stored in whole lines.
-    constexpr int kPitch = kWaveN + 4, kPer = 16 / (int)sizeof(T), kPieces = kWaveN / kPer;
-    float *mine = (float *)lds + wave * 32 * kPitch;
-    static_assert(kAll * 32 * kPitch * 4 <= (int)sizeof lds && 64 % kPieces == 0, "room; a lane has the same columns of every row");
-    T *y = (T *)p.y + (gridDim.y > 1 ? (uint64_t)blockIdx.y * p.m * p.ld : 0);
-    const uint32_t col = lane % kPieces * kPer, n = n0 + wn + col;
-    const int count = n >= p.n ? 0 : p.n - n >= kPer ? kPer : (int)(p.n - n);
-    float bias[kPer];
+    // Lane: row r of 32, columns 8 c + 4 g + 0 .. 3 of 32.  32 rows of 64 columns at a time go through LDS, each wavefront's for itself, to be stored in
+    // whole lines.
+    const uint32_t row = lane / (64 / kPer), col = lane % (64 / kPer) * kPer;
+    T *const out = (T *)places + wave * 32 * kPitch, *const mine = out + r * kPitch + 4 * g, *const line = out + row * kPitch + col;
+    T *const y = (T *)p.y + (gridDim.y > 1 ? (uint64_t)blockIdx.y * p.m * p.ld : 0) + (uint64_t)(m0 + wm + row) * p.ld + n0 + wn + col;
+    f4 bias[kSideN][4];
 #pragma unroll
-    for (int d = 0; d < kPer; ++d) bias[d] = p.bias && d < count ? p.bias[n + d] : 0.f;
+    for (int j = 0; j < kSideN; ++j)
 #pragma unroll
-    for (int i = 0; i < kSideM; ++i) {
+        for (int c = 0; c < 4; ++c) bias[j][c] = *(const f4 *)((const float *)biases + wn + 32 * j + 8 * c + 4 * g);
+    const bool whole = m0 + wm + kWaveM <= p.m && n0 + wn + kWaveN <= p.n;
 #pragma unroll
-        for (int j = 0; j < kSideN; ++j)
+    for (int i = 0; i < kSideM; ++i)
 #pragma unroll
-            for (int c = 0; c < 4; ++c)
-                *(f4 *)(mine + r * kPitch + 32 * j + 8 * c + 4 * g) = f4{acc[i][j][4 * c], acc[i][j][4 * c + 1], acc[i][j][4 * c + 2], acc[i][j][4 * c + 3]};
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-#pragma unroll 4
-        for (int s = 0; s < 32 * kPieces / 64; ++s) {
-            const uint32_t row = s * (64 / kPieces) + lane / kPieces, m = m0 + wm + 32 * i + row;
-            float v[kPer];
+        for (int half = 0; half < kSideN / 2; ++half) {
 #pragma unroll
-            for (int d = 0; d < kPer; d += 4) {
-                const f4 q = *(const f4 *)(mine + row * kPitch + col + d);
-                v[d] = q[0] + bias[d]; v[d + 1] = q[1] + bias[d + 1]; v[d + 2] = q[2] + bias[d + 2]; v[d + 3] = q[3] + bias[d + 3];
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    const f16 &v = acc[i][2 * half + j];
+                    const f4 q = bias[2 * half + j][c] + f4{v[4 * c], v[4 * c + 1], v[4 * c + 2], v[4 * c + 3]};
+                    T *at = mine + 32 * j + 8 * c;
+                    if constexpr (sizeof(T) == 2) *(u2 *)at = u2{bf16_pair(q[0], q[1]), bf16_pair(q[2], q[3])};
+                    else *(f4 *)at = q;
+                }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            if (whole) {
+#pragma unroll
+                for (int s = 0; s < 32 / kPer; ++s) {
+                    const u4 v = *(const u4 *)(line + s * kPer * kPitch);
+                    T *at = y + (uint64_t)(32 * i + s * kPer) * p.ld + 64 * half;
+                    // of many large tiles, which all L2s together do not hold: past them, where they would push out A and B (8192 x 16384 x 4096: 485 us to 440)
+                    if constexpr (kTile == 256) __builtin_nontemporal_store(v, (u4e *)at);
+                    else *(u4e *)at = v;
+                }
+            } else {
+                const uint32_t n = n0 + wn + 64 * half + col;
+#pragma clang loop unroll(disable)
+                for (int s = 0; s < 32 / kPer; ++s) {
+                    if (m0 + wm + 32 * i + s * kPer + row >= p.m) break;
+#pragma clang loop unroll(disable)
+                    for (int d = 0; d < kPer; ++d)
+                        if (n + d < p.n) y[(uint64_t)(32 * i + s * kPer) * p.ld + 64 * half + d] = line[s * kPer * kPitch + d];
+                }
             }
-            T *at = y + (uint64_t)m * p.ld + n;
-            if (m >= p.m) continue;
-            if (count == kPer) {
-                if constexpr (sizeof(T) == 2) *(u4e *)at = u4{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7])};
-                else *(f4u *)at = f4{v[0], v[1], v[2], v[3]};
-            } else
-#pragma unroll
-                for (int d = 0; d < kPer; ++d)
-                    if (d < count) store_one(at + d, v[d]);
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    }
 }
 
 // y = bias + the sum of `parts` arrays [m][n], in their order
