@@ -241,6 +241,83 @@ __global__ __launch_bounds__(64 * kWavesM * kWavesN) void k_product(ProductArgs 
         }
 }
 
+// Few rows of A (16 kM at most): the time is that of reading B once, so B goes from memory to registers, whole lines of 128 bytes, with no LDS and nothing
+// to wait for together.  A block has 16 kN rows of B; its wavefronts take groups of four blocks of 128 columns in turn, a group's loads all at once, and their
+// sums meet in LDS.
+template <typename T, int kM, int kN, int kFew>
+__global__ __launch_bounds__(64 * kFew) void k_product_few(ProductArgs p) {
+    __shared__ __align__(16) f4 part[kFew][kM * kN][64];
+    const uint32_t n0 = blockIdx.x * 16 * kN, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), r = lane & 15, g = lane >> 4;
+    const uint64_t stride = (uint64_t)p.blocks * kBlockCols;
+    const uint8_t *a[kM], *b[kN], *a_exps[kM];
+#pragma unroll
+    for (int i = 0; i < kM; ++i) {
+        const uint32_t row = min(16 * i + r, p.m - 1);
+        a[i] = p.a + row * stride + g * 32;
+        a_exps[i] = p.a_exps + (uint64_t)row * p.exp_stride;
+    }
+#pragma unroll
+    for (int j = 0; j < kN; ++j) b[j] = p.b + min(n0 + 16 * j + r, p.n - 1) * stride + g * 32;
+    typedef const __attribute__((address_space(4))) uint32_t *Scalar;
+    const Scalar b_exps = (Scalar)(p.b_exps + (uint64_t)(n0 / kBlockCols) * p.exp_stride);
+    f4 acc[kM][kN] = {};
+    for (uint32_t four = wave; four * 4 < p.blocks; four += kFew) {
+        const uint32_t eb = b_exps[four];
+        uint32_t ea[kM];
+        i8 fa[4][kM], fb[4][kN];
+        auto load = [](const uint8_t *at) {
+            const i4 lo = *(const i4 *)at, hi = *(const i4 *)(at + 16);
+            return i8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+        };
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const uint64_t at = (uint64_t)min(four * 4 + q, p.blocks - 1) * kBlockCols;
+#pragma unroll
+            for (int j = 0; j < kN; ++j) fb[q][j] = load(b[j] + at);
+#pragma unroll
+            for (int i = 0; i < kM; ++i) fa[q][i] = load(a[i] + at);
+        }
+#pragma unroll
+        for (int i = 0; i < kM; ++i) ea[i] = *(const uint32_t *)(a_exps[i] + 4 * four);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            if (four * 4 + q >= p.blocks) break;
+#pragma unroll
+            for (int i = 0; i < kM; ++i)
+#pragma unroll
+                for (int j = 0; j < kN; ++j) {
+                    if constexpr (sizeof(T) == 2) acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fb[q][j], fa[q][i], acc[i][j], 0, 0, 0, eb >> 8 * q, 0, ea[i] >> 8 * q);
+                    else
+#pragma unroll
+                        for (int c = 0; c < 8; c += 2)
+                            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bf16_of(fb[q][j][c], fb[q][j][c + 1], exp_scale(eb >> 8 * q & 255)),
+                                                                                bf16_of(fa[q][i][c], fa[q][i][c + 1], exp_scale(ea[i] >> 8 * q & 255)), acc[i][j], 0, 0, 0);
+                }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < kM; ++i)
+#pragma unroll
+        for (int j = 0; j < kN; ++j) part[wave][i * kN + j][lane] = acc[i][j];
+    __syncthreads();
+    for (uint32_t id = threadIdx.x; id < kM * kN * 64; id += 64 * kFew) {   // lane: row r, columns 4 g + 0 .. 3 of 16
+        const uint32_t tile = id / 64, m = tile / kN * 16 + r, n = n0 + tile % kN * 16 + 4 * g;
+        f4 s = part[0][tile][lane];
+#pragma unroll
+        for (int w = 1; w < kFew; ++w) s += part[w][tile][lane];
+        if (m >= p.m || n >= p.n) continue;
+        T *at = (T *)p.y + (uint64_t)m * p.ld + n;
+        if (n + 4 <= p.n) {
+            if (p.bias) s += *(const f4u *)(p.bias + n);
+            if constexpr (sizeof(T) == 2) *(u2e *)at = u2{bf16_pair(s[0], s[1]), bf16_pair(s[2], s[3])};
+            else *(f4u *)at = s;
+        } else
+#pragma unroll
+            for (int d = 0; d < 4; ++d)
+                if (n + d < p.n) store_one(at + d, s[d] + (p.bias ? p.bias[n + d] : 0.f));
+    }
+}
+
 // y = bias + the sum of `parts` arrays [m][n], in their order
 template <typename T>
 __global__ __launch_bounds__(kBlock) void k_join(const float *part, uint32_t parts, uint32_t m, uint32_t n, Divide chunks, const float *bias, T *y, uint64_t ld) {
@@ -264,13 +341,32 @@ void launch_product(const uint8_t *a, const uint8_t *a_exps, const uint8_t *b, c
                     lgc_type type, uint64_t ld, float *scratch, size_t scratch_floats, int cus, hipStream_t st) {
     auto tiles = [&](uint32_t side) { return (uint64_t)((m + side - 1) / side) * ((n + side - 1) / side); };
     const uint32_t blocks = (uint32_t)block_count(k);
+    ProductArgs p{a, a_exps, b, b_exps, m, n, blocks, (uint32_t)exps_stride(k), 0, 0, 0, bias, y, ld};
+    if (m <= 64) {
+        auto few = [&](auto rows, auto cols, auto waves) {
+            constexpr int kM = decltype(rows)::value, kN = decltype(cols)::value, kFew = decltype(waves)::value;
+            const uint32_t grid = (n + 16 * kN - 1) / (16 * kN);
+            if (type == LGC_FP32) k_product_few<float, kM, kN, kFew><<<grid, 64 * kFew, 0, st>>>(p);
+            else k_product_few<Bf16, kM, kN, kFew><<<grid, 64 * kFew, 0, st>>>(p);
+        };
+        typedef std::integral_constant<int, 1> One;
+        typedef std::integral_constant<int, 2> Two;
+        typedef std::integral_constant<int, 4> Four;
+        typedef std::integral_constant<int, 8> Eight;
+        if (m <= 16) few(One(), One(), Eight());
+        else if (m <= 32) few(Two(), One(), Eight());
+        else few(Four(), One(), Eight());
+        return;
+    }
     const bool large = type == LGC_BF16 && tiles(256) >= (uint64_t)cus;
     const uint32_t side = large ? 256 : 128;
     uint64_t parts = std::max<uint64_t>(1, 2 * (uint64_t)cus / tiles(side));
     parts = std::max<uint64_t>(1, std::min({parts, (uint64_t)blocks / 4, scratch_floats / ((uint64_t)m * n)}));
     const uint32_t share = (uint32_t)((blocks + parts - 1) / parts + 3) / 4 * 4;   // whole groups of exponents
     parts = (blocks + share - 1) / share;
-    ProductArgs p{a, a_exps, b, b_exps, m, n, blocks, (uint32_t)exps_stride(k), (m + side - 1) / side, (n + side - 1) / side, share, bias, y, ld};
+    p.tiles_m = (m + side - 1) / side;
+    p.tiles_n = (n + side - 1) / side;
+    p.share = share;
     if (parts > 1) { p.bias = nullptr; p.y = scratch; p.ld = n; }
     const dim3 grid((uint32_t)tiles(side), (uint32_t)parts);
     if (large) k_product<Bf16, 4, 2, 2, 4, false><<<grid, 512, 0, st>>>(p);
