@@ -241,10 +241,12 @@ __global__ __launch_bounds__(64 * kWavesM * kWavesN) void k_product(ProductArgs 
         }
 }
 
+constexpr int kFew = 8;   // wavefronts that share 16 or 32 rows of B
+
 // Few rows of A (16 kM at most): the time is that of reading B once, so B goes from memory to registers, whole lines of 128 bytes, with no LDS and nothing
 // to wait for together.  A block has 16 kN rows of B; its wavefronts take groups of four blocks of 128 columns in turn, a group's loads all at once, and their
 // sums meet in LDS.
-template <typename T, int kM, int kN, int kFew>
+template <typename T, int kM, int kN, bool kExact>
 __global__ __launch_bounds__(64 * kFew) void k_product_few(ProductArgs p) {
     __shared__ __align__(16) f4 part[kFew][kM * kN][64];
     const uint32_t n0 = blockIdx.x * 16 * kN, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), r = lane & 15, g = lane >> 4;
@@ -261,7 +263,8 @@ __global__ __launch_bounds__(64 * kFew) void k_product_few(ProductArgs p) {
     typedef const __attribute__((address_space(4))) uint32_t *Scalar;
     const Scalar b_exps = (Scalar)(p.b_exps + (uint64_t)(n0 / kBlockCols) * p.exp_stride);
     f4 acc[kM][kN] = {};
-    for (uint32_t four = wave; four * 4 < p.blocks; four += kFew) {
+    const uint32_t end = min((blockIdx.y + 1) * p.share, p.blocks);   // (a part's share: whole groups of four)
+    for (uint32_t four = blockIdx.y * p.share / 4 + wave; four * 4 < end; four += kFew) {
         const uint32_t eb = b_exps[four];
         uint32_t ea[kM];
         i8 fa[4][kM], fb[4][kN];
@@ -286,7 +289,7 @@ __global__ __launch_bounds__(64 * kFew) void k_product_few(ProductArgs p) {
             for (int i = 0; i < kM; ++i)
 #pragma unroll
                 for (int j = 0; j < kN; ++j) {
-                    if constexpr (sizeof(T) == 2) acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fb[q][j], fa[q][i], acc[i][j], 0, 0, 0, eb >> 8 * q, 0, ea[i] >> 8 * q);
+                    if constexpr (!kExact) acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fb[q][j], fa[q][i], acc[i][j], 0, 0, 0, eb >> 8 * q, 0, ea[i] >> 8 * q);
                     else
 #pragma unroll
                         for (int c = 0; c < 8; c += 2)
@@ -306,7 +309,7 @@ __global__ __launch_bounds__(64 * kFew) void k_product_few(ProductArgs p) {
 #pragma unroll
         for (int w = 1; w < kFew; ++w) s += part[w][tile][lane];
         if (m >= p.m || n >= p.n) continue;
-        T *at = (T *)p.y + (uint64_t)m * p.ld + n;
+        T *at = (T *)p.y + ((gridDim.y > 1 ? (uint64_t)blockIdx.y * p.m : 0) + m) * p.ld + n;
         if (n + 4 <= p.n) {
             if (p.bias) s += *(const f4u *)(p.bias + n);
             if constexpr (sizeof(T) == 2) *(u2e *)at = u2{bf16_pair(s[0], s[1]), bf16_pair(s[2], s[3])};
@@ -342,42 +345,52 @@ void launch_product(const uint8_t *a, const uint8_t *a_exps, const uint8_t *b, c
     auto tiles = [&](uint32_t side) { return (uint64_t)((m + side - 1) / side) * ((n + side - 1) / side); };
     const uint32_t blocks = (uint32_t)block_count(k);
     ProductArgs p{a, a_exps, b, b_exps, m, n, blocks, (uint32_t)exps_stride(k), 0, 0, 0, bias, y, ld};
+    uint64_t parts = 1;
+    auto split = [&](uint64_t want) {   // the sum over k in `want` parts, in whole groups of four blocks, where there is room for their sums
+        parts = std::max<uint64_t>(1, std::min(want, scratch_floats / ((uint64_t)m * n)));
+        p.share = (uint32_t)((blocks + parts - 1) / parts + 3) / 4 * 4;
+        parts = (blocks + p.share - 1) / p.share;
+        if (parts > 1) { p.bias = nullptr; p.y = scratch; p.ld = n; }
+    };
+    auto join = [&] {
+        if (parts == 1) return;
+        const uint32_t chunks = (n + 7) / 8, grid = (uint32_t)(((uint64_t)m * chunks + kBlock - 1) / kBlock);
+        if (type == LGC_FP32) k_join<float><<<grid, kBlock, 0, st>>>(scratch, (uint32_t)parts, m, n, divide_by(chunks), bias, (float *)y, ld);
+        else k_join<Bf16><<<grid, kBlock, 0, st>>>(scratch, (uint32_t)parts, m, n, divide_by(chunks), bias, (Bf16 *)y, ld);
+    };
     if (m <= 64) {
-        auto few = [&](auto rows, auto cols, auto waves) {
-            constexpr int kM = decltype(rows)::value, kN = decltype(cols)::value, kFew = decltype(waves)::value;
-            const uint32_t grid = (n + 16 * kN - 1) / (16 * kN);
-            if (type == LGC_FP32) k_product_few<float, kM, kN, kFew><<<grid, 64 * kFew, 0, st>>>(p);
-            else k_product_few<Bf16, kM, kN, kFew><<<grid, 64 * kFew, 0, st>>>(p);
+        auto few = [&](auto rows, auto cols) {
+            constexpr int kM = decltype(rows)::value, kN = decltype(cols)::value;
+            const uint32_t own = (n + 16 * kN - 1) / (16 * kN);
+            split(own < (uint32_t)cus ? std::min<uint64_t>(2 * cus / own, blocks / (4 * kFew)) : 1);
+            const dim3 grid(own, (uint32_t)parts);
+            if (type == LGC_FP32) k_product_few<float, kM, kN, true><<<grid, 64 * kFew, 0, st>>>(p);
+            else if (parts > 1) k_product_few<float, kM, kN, false><<<grid, 64 * kFew, 0, st>>>(p);
+            else k_product_few<Bf16, kM, kN, false><<<grid, 64 * kFew, 0, st>>>(p);
+            join();
         };
         typedef std::integral_constant<int, 1> One;
         typedef std::integral_constant<int, 2> Two;
         typedef std::integral_constant<int, 4> Four;
-        typedef std::integral_constant<int, 8> Eight;
-        if (m <= 16) few(One(), One(), Eight());
-        else if (m <= 32) few(Two(), One(), Eight());
-        else few(Four(), One(), Eight());
+        // 32 rows of B per block, whose reads of A are half as many, where that leaves a block per compute unit (us, 16 / 32 rows: 16 x 8192 x 4096 10.1 / 8.2,
+        // 64 x 8192 x 4096 22.0 / 15.1, 16 x 4096 x 4096 6.1 / 7.8, 64 x 4096 x 4096 12.5 / 14.0)
+        const bool wide = n / 32 >= (uint32_t)cus;
+        if (m <= 16) wide ? few(One(), Two()) : few(One(), One());
+        else if (m <= 32) wide ? few(Two(), Two()) : few(Two(), One());
+        else wide ? few(Four(), Two()) : few(Four(), One());
         return;
     }
     const bool large = type == LGC_BF16 && tiles(256) >= (uint64_t)cus;
     const uint32_t side = large ? 256 : 128;
-    uint64_t parts = std::max<uint64_t>(1, 2 * (uint64_t)cus / tiles(side));
-    parts = std::max<uint64_t>(1, std::min({parts, (uint64_t)blocks / 4, scratch_floats / ((uint64_t)m * n)}));
-    const uint32_t share = (uint32_t)((blocks + parts - 1) / parts + 3) / 4 * 4;   // whole groups of exponents
-    parts = (blocks + share - 1) / share;
+    split(std::min<uint64_t>(2 * (uint64_t)cus / tiles(side), blocks / 4));
     p.tiles_m = (m + side - 1) / side;
     p.tiles_n = (n + side - 1) / side;
-    p.share = share;
-    if (parts > 1) { p.bias = nullptr; p.y = scratch; p.ld = n; }
     const dim3 grid((uint32_t)tiles(side), (uint32_t)parts);
     if (large) k_product<Bf16, 4, 2, 2, 4, false><<<grid, 512, 0, st>>>(p);
     else if (type == LGC_FP32) k_product<float, 2, 2, 2, 2, true><<<grid, 256, 0, st>>>(p);
     else if (parts > 1) k_product<float, 2, 2, 2, 2, false><<<grid, 256, 0, st>>>(p);
     else k_product<Bf16, 2, 2, 2, 2, false><<<grid, 256, 0, st>>>(p);
-    if (parts == 1) return;
-    const uint32_t chunks = (n + 7) / 8;
-    const uint32_t join = (uint32_t)(((uint64_t)m * chunks + kBlock - 1) / kBlock);
-    if (type == LGC_FP32) k_join<float><<<join, kBlock, 0, st>>>(scratch, (uint32_t)parts, m, n, divide_by(chunks), bias, (float *)y, ld);
-    else k_join<Bf16><<<join, kBlock, 0, st>>>(scratch, (uint32_t)parts, m, n, divide_by(chunks), bias, (Bf16 *)y, ld);
+    join();
 }
 
 }  // namespace lgc
