@@ -1,6 +1,7 @@
 // Gradient of a linear layer's weights and bias from the layer's input as it was kept in 8 bits:
 // dw[n][k] = sum_t dy[t][n] x[t][k],  db[n] = sum_t dy[t][n].
 #include <algorithm>
+#include <utility>
 
 #include "blocks.h"
 
@@ -20,7 +21,8 @@ struct WeightGradArgs {
     uint64_t code_stride;
     uint32_t tiles_n, tiles_k;
     uint32_t share;   // rows per part; blockIdx.y: which part
-    float *dw, *db;   // [parts][n][k], [parts][n]
+    float *dw, *db;   // of the first part
+    uint64_t part;    // floats from part to part
 };
 
 // The leading 8 bits of x as bf16, taken off x (cut, not rounded: three of them are an fp32 number's 24 bits, and none overflows).
@@ -47,100 +49,127 @@ __device__ __forceinline__ void tile_of(uint32_t id, uint32_t tiles_n, uint32_t 
 }
 
 // The exponents of x differ along the sum, so its values meet the matrix cores as bf16, in which they are exact; dy in fp32 as three bf16 parts, which hold it exactly.
-// A tile of 2 kWave x 2 kWave per block, a quarter per wavefront.  64 rows of dy and x at a time go through registers to LDS, while the matrix cores work on
-// the 64 before, and are turned as they are read from there: 16 lanes give the addresses of four rows of 16 columns and get a column of four rows each.
+// A tile of 2 kWave x 2 kWave per block, a quarter per wavefront, 64 rows of dy and x at a time.  Rows go through registers, loaded a step before, to one of two
+// places in LDS, and are turned as they are read from there: 16 lanes give the addresses of four rows of 16 columns and get a column of four rows each.  A step's
+// products come in four groups of 16 rows; between those of a group the next group's columns are read and the next step's rows are stored and the loads of the step
+// after it queued, in the order written here (there is one wavefront per SIMD, or two: nothing else would run while one of them does these alone).
 // LDS rows lie a multiple of 256 bytes apart; pieces of 32 bytes are exchanged within a row by (row & 3), so that these four rows meet all banks.
+constexpr int kSteps = 64;
+
+// f(0), f(1), .. f(N - 1), each with its number as a constant
+template <typename F, int... I>
+__device__ __forceinline__ void each_of(std::integer_sequence<int, I...>, F &&f) { (f(std::integral_constant<int, I>()), ...); }
+template <int N, typename F>
+__device__ __forceinline__ void each(F &&f) { each_of(std::make_integer_sequence<int, N>(), f); }
+
 template <typename T, int kWave>
-__global__ __launch_bounds__(kBlock, 1) void k_weight_grad(WeightGradArgs p) {
-    constexpr int kParts = sizeof(T) == 2 ? 1 : 3, kSteps = 64, kTile = 2 * kWave, kPitch = kTile * 2, kSide = kWave / 32;
+__global__ __launch_bounds__(kBlock, kWave == 64 && sizeof(T) == 2 ? 2 : 1) void k_weight_grad(WeightGradArgs p) {
+    constexpr int kParts = sizeof(T) == 2 ? 1 : 3, kTile = 2 * kWave, kPitch = kTile * 2, kPlace = (kParts + 1) * kSteps * kPitch, kSide = kWave / 32;
     constexpr int kChunks = kTile / 8, kRowsY = kBlock / kChunks, kPassY = kSteps / kRowsY;       // dy: eight columns per thread and pass
     constexpr int kPieces = kTile / 16, kRowsX = kBlock / kPieces, kPassX = kSteps / kRowsX;      // x: sixteen codes
-    __shared__ __align__(16) uint8_t lds[2][(kParts + 1) * kSteps * kPitch];
+    __shared__ __align__(16) uint8_t lds[2 * kPlace];
     uint32_t tn, tk;
     tile_of(blockIdx.x, p.tiles_n, p.tiles_k, tn, tk);
-    const uint32_t n0 = tn * kTile, k0 = tk * kTile, lane = threadIdx.x & 63, wave = threadIdx.x / 64;
+    const uint32_t n0 = tn * kTile, k0 = tk * kTile;
+    const bool sums = p.db && tk == 0;
+    const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const uint32_t wn = (wave & 1) * kWave, wk = (wave >> 1) * kWave;
     const uint32_t t0 = blockIdx.y * p.share, t1 = min(t0 + p.share, p.rows);
 
+    // No branch stands before the loads, which ask for memory that exists, whatever the place: of dy, eight elements from the row's on, or the last eight that there
+    // are (total: elements from dy's first to its last).  Past the row's end they are none of its columns and become columns that are not stored; rows that do not
+    // exist are zeroed, and what comes at the end of the last eight put in its place, when they have arrived.
     const uint32_t y_row = threadIdx.x / kChunks, y_chunk = threadIdx.x % kChunks, y_col = n0 + y_chunk * 8;
-    const int y_count = y_col >= p.n ? 0 : p.n - y_col >= 8 ? 8 : (int)(p.n - y_col);
-    const uint32_t x_row = threadIdx.x / kPieces, x_piece = threadIdx.x % kPieces, x_col = k0 + x_piece * 16;
-    const bool x_here = x_col < p.code_stride, sums = p.db && tk == 0;
+    const uint64_t total = (uint64_t)(p.rows - 1) * p.ld + p.n;
+    const uint32_t x_row = threadIdx.x / kPieces, x_piece = threadIdx.x % kPieces, x_from = min(k0 + x_piece * 16, (uint32_t)p.code_stride - 16);
     u4 y_next[kPassY][kParts == 1 ? 1 : 2], x_next[kPassX];
     uint32_t e_next[kPassX];
     float db[8] = {};
 
-    auto load = [&](uint32_t t) {
-#pragma unroll
-        for (int i = 0; i < kPassY; ++i) {
-            const uint32_t row = t + y_row + i * kRowsY;
-            const T *at = (const T *)p.dy + (uint64_t)row * p.ld + y_col;
-            if (row < t1 && y_count == 8) {
-                y_next[i][0] = *(const u4e *)at;
-                if constexpr (kParts > 1) y_next[i][1] = *(const u4e *)(at + 4);
-            } else {
-                float v[8];
-                load_chunk(at, row < t1 ? y_count : 0, v);
-                if constexpr (kParts == 1) y_next[i][0] = u4{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7])};
-                else
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) y_next[i][j / 4][j % 4] = __float_as_uint(v[j]);
-            }
+    auto y_place = [&](int i, uint32_t t) { return (uint64_t)min(t + y_row + i * kRowsY, p.rows - 1) * p.ld + y_col; };
+    auto load_y_at = [&](int i, const T *at) {
+        y_next[i][0] = *(const u4e *)at;
+        if constexpr (kParts > 1) y_next[i][1] = *(const u4e *)(at + 4);
+    };
+    // Inside, where kTile rows more exist (however narrow dy is, what is asked for does): a place that goes on by a step's rows, and the passes' distances from it
+    const T *y_at_next = (const T *)p.dy + (uint64_t)(t0 + 2 * kSteps + y_row) * p.ld + y_col;
+    const uint8_t *x_at_next = p.codes + (uint64_t)(t0 + 2 * kSteps + x_row) * p.code_stride + x_from;
+    const uint8_t *e_at_next = p.exps + (uint64_t)(t0 + 2 * kSteps + x_row) * p.exp_stride + x_from / kBlockCols;
+    auto store_y = [&](auto inside, int i, uint32_t place, uint32_t t) {
+        const uint32_t row = y_row + i * kRowsY, at = place * kPlace + row * kPitch + (y_chunk * 16 ^ (row & 3) * 64);
+        const bool last = !decltype(inside)::value && (t + kSteps + 8 > p.rows || t + kSteps > t1);   // (the same for all)
+        uint32_t beyond = 0;
+        if (last) {
+            const uint64_t end = y_place(i, t) + 8;
+            beyond = t + row >= t1 || end >= total + 8 ? 8u : end > total ? (uint32_t)(end - total) : 0u;
         }
+        if constexpr (kParts == 1) {
+            u4 w = y_next[i][0];
+            if (last)
+                for (uint32_t j = 0; j < beyond; ++j) w = u4{w[0] >> 16 | w[1] << 16, w[1] >> 16 | w[2] << 16, w[2] >> 16 | w[3] << 16, w[3] >> 16};
+            if (sums)
 #pragma unroll
-        for (int i = 0; i < kPassX; ++i) {
-            const uint32_t row = t + x_row + i * kRowsX;
-            x_next[i] = u4{0, 0, 0, 0};
-            e_next[i] = kLeastExp;
-            if (row < t1 && x_here) {
-                x_next[i] = *(const u4 *)(p.codes + (uint64_t)row * p.code_stride + x_col);
-                e_next[i] = p.exps[(uint64_t)row * p.exp_stride + x_col / kBlockCols];
+                for (int j = 0; j < 4; ++j) { db[2 * j] += __uint_as_float(w[j] << 16); db[2 * j + 1] += __uint_as_float(w[j] & 0xffff0000u); }
+            *(u4 *)(lds + at) = w;
+        } else {
+            float v[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = __uint_as_float(y_next[i][j / 4][j % 4]);
+            if (last)
+                for (uint32_t j = 0; j < beyond; ++j) {
+#pragma unroll
+                    for (int c = 0; c < 7; ++c) v[c] = v[c + 1];
+                    v[7] = 0.f;
+                }
+            if (sums)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) db[j] += v[j];
+#pragma unroll
+            for (int q = 0; q < kParts; ++q) {
+                u4 w;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    w[j] = next_part(v[2 * j]);
+                    w[j] |= next_part(v[2 * j + 1]) << 16;
+                }
+                *(u4 *)(lds + q * kSteps * kPitch + at) = w;
             }
         }
     };
-    auto store = [&](int buffer) {
-        uint8_t *y = lds[buffer], *x = y + kParts * kSteps * kPitch;
+    auto store_x = [&](auto inside, int i, uint32_t place, uint32_t t) {
+        const uint32_t row = x_row + i * kRowsX, at = place * kPlace + kParts * kSteps * kPitch + row * kPitch + (x_piece * 32 ^ (row & 3) * 64);
+        const float scale = exp_scale(e_next[i]);
+        u4 w[2], from = x_next[i];
+        if (!decltype(inside)::value && t + row >= t1) from = u4{0, 0, 0, 0};
 #pragma unroll
-        for (int i = 0; i < kPassY; ++i) {
-            const uint32_t row = y_row + i * kRowsY, at = row * kPitch + (y_chunk * 16 ^ (row & 3) * 64);
-            if constexpr (kParts == 1) {
-                const u4 w = y_next[i][0];
-                *(u4 *)(y + at) = w;
-                if (sums)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) { db[2 * j] += __uint_as_float(w[j] << 16); db[2 * j + 1] += __uint_as_float(w[j] & 0xffff0000u); }
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t c = from[j];
+            w[j / 2][j % 2 * 2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c, scale, false));
+            w[j / 2][j % 2 * 2 + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c, scale, true));
+        }
+        *(u4 *)(lds + at) = w[0];
+        *(u4 *)(lds + at + 16) = w[1];
+    };
+    constexpr int kStaged = kPassY + kPassX;
+    auto load = [&](auto inside, int i, uint32_t t) {
+        if (i < kPassY) {
+            if constexpr (decltype(inside)::value) load_y_at(i, y_at_next + (uint64_t)(i * kRowsY) * p.ld);
+            else load_y_at(i, (const T *)p.dy + min(y_place(i, t), total - 8));
+        } else {
+            const int j = i - kPassY;
+            if constexpr (decltype(inside)::value) {
+                x_next[j] = *(const u4 *)(x_at_next + (uint64_t)(j * kRowsX) * p.code_stride);
+                e_next[j] = e_at_next[(uint64_t)(j * kRowsX) * p.exp_stride];
             } else {
-                float v[8];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] = __uint_as_float(y_next[i][j / 4][j % 4]);
-                if (sums)
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) db[j] += v[j];
-#pragma unroll
-                for (int q = 0; q < kParts; ++q) {
-                    u4 w;
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        w[j] = next_part(v[2 * j]);
-                        w[j] |= next_part(v[2 * j + 1]) << 16;
-                    }
-                    *(u4 *)(y + q * kSteps * kPitch + at) = w;
-                }
+                const uint64_t row = min(t + x_row + j * kRowsX, p.rows - 1);
+                x_next[j] = *(const u4 *)(p.codes + row * p.code_stride + x_from);
+                e_next[j] = p.exps[row * p.exp_stride + x_from / kBlockCols];
             }
         }
-#pragma unroll
-        for (int i = 0; i < kPassX; ++i) {
-            const uint32_t row = x_row + i * kRowsX, at = row * kPitch + (x_piece * 32 ^ (row & 3) * 64);
-            const float scale = exp_scale(e_next[i]);
-            u4 w[2];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                w[j / 2][j % 2 * 2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x_next[i][j], scale, false));
-                w[j / 2][j % 2 * 2 + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x_next[i][j], scale, true));
-            }
-            *(u4 *)(x + at) = w[0];
-            *(u4 *)(x + at + 16) = w[1];
-        }
+    };
+    auto store = [&](auto inside, int i, uint32_t place, uint32_t t) {
+        if (i < kPassY) store_y(inside, i, place, t);
+        else store_x(inside, i - kPassY, place, t);
     };
 
     // 32 x 32 x 16: lane: column lane % 32, rows 8 (lane / 32) + 0 .. 7 of the 16
@@ -152,60 +181,100 @@ __global__ __launch_bounds__(kBlock, 1) void k_weight_grad(WeightGradArgs p) {
         y_at[i] = t_lane * kPitch + (((wn + col) * 2) ^ ((r >> 2) * 64)) + (r & 3) * 8;
         x_at[i] = kParts * kSteps * kPitch + t_lane * kPitch + (((wk + col) * 2) ^ ((r >> 2) * 64)) + (r & 3) * 8;
     }
-    auto column = [&](const uint8_t *at) {
+    auto column = [&](uint32_t at) {
         typedef __attribute__((address_space(3))) s4 *Lds;
-        const s4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)at), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(at + 4 * kPitch));
+        const s4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(lds + at)), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(lds + at + 4 * kPitch));
         return __builtin_bit_cast(bf8, s8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]});
     };
+    constexpr int kReads = kSide * (1 + kParts), kProducts = kSide * kSide * kParts;
+    bf8 x[2][kSide], y[2][kParts][kSide];
+    auto read = [&](int set, uint32_t place, int group, int i) {
+        const uint32_t from = place * kPlace + group * 16 * kPitch;
+        if (i < kSide) x[set][i] = column(from + x_at[i]);
+        else y[set][i / kSide - 1][i % kSide] = column(from + (i / kSide - 1) * kSteps * kPitch + y_at[i % kSide]);
+    };
     f16 acc[kSide][kSide] = {};
-    auto multiply = [&](int buffer) {
-#pragma unroll
-        for (int s = 0; s < kSteps / 16; ++s) {
-            bf8 x[kSide];
-#pragma unroll
-            for (int j = 0; j < kSide; ++j) x[j] = column(lds[buffer] + x_at[j] + s * 16 * kPitch);
-#pragma unroll
-            for (int q = kParts - 1; q >= 0; --q)
-#pragma unroll
-                for (int i = 0; i < kSide; ++i) {
-                    const bf8 y = column(lds[buffer] + y_at[i] + (q * kSteps + s * 16) * kPitch);
-#pragma unroll
-                    for (int j = 0; j < kSide; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[j], y, acc[i][j], 0, 0, 0);
-                }
-        }
+    auto product = [&](int set, int i) {   // the smallest parts first
+        const int part = kParts - 1 - i / (kSide * kSide), n = i / kSide % kSide, k = i % kSide;
+        acc[n][k] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[set][k], y[set][part][n], acc[n][k], 0, 0, 0);
     };
 
-    load(t0);
-    store(0);
+    each<kStaged>([&](auto i) { load(std::false_type(), i, t0); });
+    each<kStaged>([&](auto i) {
+        store(std::false_type(), i, 0, t0);
+        load(std::false_type(), i, t0 + kSteps);
+    });
     __syncthreads();
-    int buffer = 0;
-    for (uint32_t t = t0; t < t1; t += kSteps, buffer ^= 1) {
-        const bool more = t + kSteps < t1;
-        if (more) load(t + kSteps);
-        multiply(buffer);
-        if (more) store(buffer ^ 1);
+    each<kReads>([&](auto i) { read(0, 0, 0, i); });
+    uint32_t t = t0, place = 0;
+    typedef std::true_type Inside;
+    typedef std::false_type Outside;
+#pragma clang loop unroll(disable)
+    for (; t + 2 * kSteps <= t1 && (uint64_t)t + 3 * kSteps + kTile <= p.rows; t += kSteps, place ^= 1) {
+        each<4>([&](auto group) {
+            if constexpr (group == 3) {   // the next step's rows are stored, and this one's read
+                asm volatile("" ::: "memory");
+                __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt(0)
+                __builtin_amdgcn_s_barrier();
+                asm volatile("" ::: "memory");
+            }
+            each<kProducts>([&](auto i) {
+                product(group & 1, i);
+                constexpr int kFrom = i * kReads / kProducts, kTo = (i + 1) * kReads / kProducts;
+                each<kTo - kFrom>([&](auto j) { read(~group & 1, group == 3 ? place ^ 1 : place, (group + 1) & 3, kFrom + j); });
+                if constexpr (group < 3) {
+                    constexpr int kBegin = (group * kProducts + i) * kStaged / (3 * kProducts), kEnd = (group * kProducts + i + 1) * kStaged / (3 * kProducts);
+                    each<kEnd - kBegin>([&](auto j) {
+                        store(Inside(), kBegin + j, place ^ 1, t + kSteps);
+                        load(Inside(), kBegin + j, t + 2 * kSteps);
+                    });
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            });
+        });
+        y_at_next += (uint64_t)kSteps * p.ld;
+        x_at_next += (uint64_t)kSteps * p.code_stride;
+        e_at_next += (uint64_t)kSteps * p.exp_stride;
+    }
+    // the last steps, one thing after the other (past the end: rows that exist, and zeros in their place)
+#pragma clang loop unroll(disable)
+    for (; t < t1; t += kSteps, place ^= 1) {
+        each<kStaged>([&](auto i) {
+            store(Outside(), i, place ^ 1, t + kSteps);
+            load(Outside(), i, t + 2 * kSteps);
+        });
+#pragma clang loop unroll(disable)
+        for (int group = 0; group < 4; ++group) {
+            each<kReads>([&](auto i) { read(0, place, group, i); });
+            each<kProducts>([&](auto i) { product(0, i); });
+        }
         __syncthreads();
     }
+    __syncthreads();
 
-    float *dw = p.dw + (uint64_t)blockIdx.y * p.n * p.k;
+    const uint32_t n_here = n0 + wn + (lane & 31), k_here = k0 + wk + 4 * (lane >> 5);
+    float *const dw = p.dw + blockIdx.y * p.part + (uint64_t)n_here * p.k + k_here;
+    const bool whole = k0 + kTile <= p.k;   // (the same for all)
 #pragma unroll
     for (int i = 0; i < kSide; ++i) {
-        const uint32_t n = n0 + wn + 32 * i + (lane & 31);
-        if (n >= p.n) continue;
+        if (n_here + 32 * i >= p.n) continue;
+        float *const row = dw + (uint64_t)(32 * i) * p.k;
+        if (whole) {
 #pragma unroll
-        for (int j = 0; j < kSide; ++j)
+            for (int j = 0; j < kSide; ++j)
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                const uint32_t k = k0 + wk + 32 * j + 8 * c + 4 * (lane >> 5);
-                float *at = dw + (uint64_t)n * p.k + k;
-                if (k + 4 <= p.k) *(f4u *)at = f4{acc[i][j][4 * c], acc[i][j][4 * c + 1], acc[i][j][4 * c + 2], acc[i][j][4 * c + 3]};
-                else
+                for (int c = 0; c < 4; ++c)
+                    *(f4u *)(row + 32 * j + 8 * c) = f4{acc[i][j][4 * c], acc[i][j][4 * c + 1], acc[i][j][4 * c + 2], acc[i][j][4 * c + 3]};
+        } else {
 #pragma unroll
-                    for (int d = 0; d < 4; ++d) if (k + d < p.k) at[d] = acc[i][j][4 * c + d];
-            }
+            for (int j = 0; j < kSide; ++j)
+#pragma unroll
+                for (int c = 0; c < 16; ++c)
+                    if (k_here + 32 * j + c / 4 * 8 + c % 4 < p.k) row[32 * j + c / 4 * 8 + c % 4] = acc[i][j][c];
+        }
     }
     if (!sums) return;   // the threads' column sums, added in a fixed order
-    float *part = (float *)lds[0];
+    float *part = (float *)lds;
 #pragma unroll
     for (int j = 0; j < 8; ++j) part[y_row * kTile + y_chunk * 8 + j] = db[j];
     __syncthreads();
@@ -213,53 +282,88 @@ __global__ __launch_bounds__(kBlock, 1) void k_weight_grad(WeightGradArgs p) {
         float s = 0.f;
 #pragma unroll
         for (int i = 0; i < kRowsY; ++i) s += part[i * kTile + c];
-        if (n0 + c < p.n) p.db[(uint64_t)blockIdx.y * p.n + n0 + c] = s;
+        if (n0 + c < p.n) p.db[blockIdx.y * p.part + n0 + c] = s;
     }
 }
 
-// Sums of `parts` arrays of `count` floats, in their order
-__global__ __launch_bounds__(kBlock) void k_add_parts(const float *part, uint32_t parts, uint64_t count, float *out) {
-    const uint64_t at = ((uint64_t)blockIdx.x * kBlock + threadIdx.x) * 4;
-    if (at >= count) return;
-    const int here = count - at >= 4 ? 4 : (int)(count - at);
-    f4 s = {0, 0, 0, 0};
-    for (uint32_t i = 0; i < parts; ++i) {
-        const float *from = part + i * count + at;
-        if (here == 4) s += *(const f4u *)from;
-        else
-            for (int j = 0; j < here; ++j) s[j] += from[j];
+// A dy of fewer than eight elements (one row, mostly): a thread per weight
+template <typename T>
+__global__ __launch_bounds__(kBlock) void k_weight_grad_small(WeightGradArgs p) {
+    const uint64_t id = (uint64_t)blockIdx.x * kBlock + threadIdx.x;
+    const uint32_t n = (uint32_t)(id / p.k), k = (uint32_t)(id - (uint64_t)n * p.k);
+    if (n >= p.n) return;
+    float w = 0.f, b = 0.f;
+    for (uint32_t t = 0; t < p.rows; ++t) {
+        const float y = to_float(((const T *)p.dy)[t * p.ld + n]);
+        const uint8_t code = p.codes[t * p.code_stride + k];
+        w = fmaf(y, __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(code, exp_scale(p.exps[(uint64_t)t * p.exp_stride + k / kBlockCols]), false)[0], w);
+        b += y;
     }
-    if (here == 4) *(f4u *)(out + at) = s;
+    p.dw[id] = w;
+    if (p.db && k == 0) p.db[n] = b;
+}
+
+// dw and db: sums of `parts` arrays that hold both, in a fixed order: a wavefront's every fourth, then the wavefronts' four
+__global__ __launch_bounds__(kBlock) void k_add_parts(const float *part, uint32_t parts, uint64_t stride, float *dw, uint64_t count_w, float *db, uint64_t count) {
+    __shared__ f4 sums[kWaves][64];
+    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x / 64;
+    const uint64_t at = ((uint64_t)blockIdx.x * 64 + lane) * 4;
+    f4 s = {0, 0, 0, 0};
+    if (at + 4 <= count) {
+#pragma unroll 4
+        for (uint32_t i = wave; i < parts; i += kWaves) s += *(const f4u *)(part + i * stride + at);
+    } else
+        for (uint32_t i = wave; i < parts; i += kWaves)
+            for (int j = 0; j < 4; ++j)
+                if (at + j < count) s[j] += part[i * stride + at + j];
+    sums[wave][lane] = s;
+    __syncthreads();
+    if (wave) return;
+#pragma unroll
+    for (int i = 1; i < kWaves; ++i) s += sums[i][lane];
+    if (at + 4 <= count_w) *(f4u *)(dw + at) = s;
     else
-        for (int j = 0; j < here; ++j) out[at + j] = s[j];
+        for (int j = 0; j < 4; ++j) {
+            if (at + j < count_w) dw[at + j] = s[j];
+            else if (at + j < count) db[at + j - count_w] = s[j];
+        }
 }
 
 }  // namespace
 
 void launch_weight_grad(const void *dy, lgc_type type, uint32_t rows, uint32_t n, uint64_t ld, const uint8_t *codes, const uint8_t *exps, uint32_t k, float *dw, float *db,
                         float *scratch, size_t scratch_floats, int cus, hipStream_t st) {
+    const uint64_t count_w = (uint64_t)n * k, count = count_w + (db ? n : 0);
+    const uint32_t adds = (uint32_t)((count + 255) / 256);
+    WeightGradArgs p{dy, ld, codes, exps, rows, n, k, (uint32_t)exps_stride(k), codes_stride(k), 0, 0, rows, dw, db, count};
+    if (rows == 0) {
+        k_add_parts<<<adds, kBlock, 0, st>>>(nullptr, 0, 0, dw, count_w, db, count);
+        return;
+    }
+    if ((uint64_t)(rows - 1) * ld + n < 8) {
+        const uint32_t grid = (uint32_t)((count_w + kBlock - 1) / kBlock);
+        if (type == LGC_FP32) k_weight_grad_small<float><<<grid, kBlock, 0, st>>>(p);
+        else k_weight_grad_small<Bf16><<<grid, kBlock, 0, st>>>(p);
+        return;
+    }
     auto tiles = [&](uint32_t side) { return (uint64_t)((n + side - 1) / side) * ((k + side - 1) / side); };
     const bool large = type == LGC_BF16 && tiles(256) >= (uint64_t)cus;
     const uint32_t side = large ? 256 : 128;
-    const uint64_t size = (uint64_t)n * k + (db ? n : 0);
-    uint64_t parts = std::max<uint64_t>(1, 2 * (uint64_t)cus / tiles(side));
-    parts = std::min({parts, (uint64_t)(rows + 255) / 256, scratch_floats / size, (uint64_t)65535});
+    uint64_t parts = std::min({1 * (uint64_t)cus / tiles(side), (uint64_t)(rows + 255) / 256, scratch_floats / count, (uint64_t)65535});
     parts = std::max<uint64_t>(parts, 1);
-    uint32_t share = (uint32_t)((rows + parts - 1) / parts + 63) / 64 * 64;
-    if (share == 0) share = 64;
-    parts = std::max<uint64_t>(1, (rows + share - 1) / share);
-    float *to = parts > 1 ? scratch : dw, *to_db = !db ? nullptr : parts > 1 ? scratch + parts * (uint64_t)n * k : db;
-    const WeightGradArgs p{dy, ld, codes, exps, rows, n, k, (uint32_t)exps_stride(k), codes_stride(k), (n + side - 1) / side, (k + side - 1) / side, share, to, to_db};
+    p.share = (uint32_t)((rows + parts - 1) / parts + 63) / 64 * 64;
+    parts = (rows + p.share - 1) / p.share;
+    p.tiles_n = (n + side - 1) / side;
+    p.tiles_k = (k + side - 1) / side;
+    if (parts > 1) {
+        p.dw = scratch;
+        if (db) p.db = scratch + count_w;
+    }
     const dim3 grid((uint32_t)tiles(side), (uint32_t)parts);
     if (type == LGC_FP32) k_weight_grad<float, 64><<<grid, kBlock, 0, st>>>(p);
     else if (large) k_weight_grad<Bf16, 128><<<grid, kBlock, 0, st>>>(p);
     else k_weight_grad<Bf16, 64><<<grid, kBlock, 0, st>>>(p);
-    if (parts == 1) return;
-    auto add = [&](const float *from, uint64_t count, float *out) {
-        k_add_parts<<<(uint32_t)((count + 4 * kBlock - 1) / (4 * kBlock)), kBlock, 0, st>>>(from, (uint32_t)parts, count, out);
-    };
-    add(to, (uint64_t)n * k, dw);
-    if (db) add(to_db, n, db);
+    if (parts > 1) k_add_parts<<<adds, kBlock, 0, st>>>(scratch, (uint32_t)parts, count, dw, count_w, db, count);
 }
 
 }  // namespace lgc
