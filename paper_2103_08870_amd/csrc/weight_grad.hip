@@ -62,26 +62,32 @@ __device__ __forceinline__ void each_of(std::integer_sequence<int, I...>, F &&f)
 template <int N, typename F>
 __device__ __forceinline__ void each(F &&f) { each_of(std::make_integer_sequence<int, N>(), f); }
 
-template <typename T, int kWave>
-__global__ __launch_bounds__(kBlock, kWave == 64 && sizeof(T) == 2 ? 2 : 1) void k_weight_grad(WeightGradArgs p) {
+// kTeams teams of four wavefronts do this for a part of the block's rows each, and their sums meet in LDS: with small tiles, whose wavefronts wait for LDS half of
+// the time, two per SIMD are faster than one (8192 x 2048 x 2048: 99 us to 83).
+template <typename T, int kWave, int kTeams>
+__global__ __launch_bounds__(kBlock * kTeams) void k_weight_grad(WeightGradArgs p) {
     constexpr int kParts = sizeof(T) == 2 ? 1 : 3, kTile = 2 * kWave, kPitch = kTile * 2, kPlace = (kParts + 1) * kSteps * kPitch, kSide = kWave / 32;
     constexpr int kChunks = kTile / 8, kRowsY = kBlock / kChunks, kPassY = kSteps / kRowsY;       // dy: eight columns per thread and pass
     constexpr int kPieces = kTile / 16, kRowsX = kBlock / kPieces, kPassX = kSteps / kRowsX;      // x: sixteen codes
-    __shared__ __align__(16) uint8_t lds[2 * kPlace];
+    __shared__ __align__(16) uint8_t every[kTeams * 2 * kPlace];
+    const uint32_t tid = threadIdx.x % kBlock, team = __builtin_amdgcn_readfirstlane(threadIdx.x / kBlock);
+    uint8_t *const lds = every + team * (2 * kPlace);
     uint32_t tn, tk;
     tile_of(blockIdx.x, p.tiles_n, p.tiles_k, tn, tk);
     const uint32_t n0 = tn * kTile, k0 = tk * kTile;
     const bool sums = p.db && tk == 0;
-    const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(tid / 64);
     const uint32_t wn = (wave & 1) * kWave, wk = (wave >> 1) * kWave;
-    const uint32_t t0 = blockIdx.y * p.share, t1 = min(t0 + p.share, p.rows);
+    // the team's rows: whole steps of the part's, as many for each; the last team's may end, or lie, past the part's end
+    const uint32_t begin = blockIdx.y * p.share, end = min(begin + p.share, p.rows), steps = (end - begin + kTeams * kSteps - 1) / (kTeams * kSteps);
+    const uint32_t t0 = begin + team * steps * kSteps, t1 = min(t0 + steps * kSteps, end), lag = (kTeams - 1 - team) * steps * kSteps;   // lag: to the last team's
 
     // No branch stands before the loads, which ask for memory that exists, whatever the place: of dy, eight elements from the row's on, or the last eight that there
     // are (total: elements from dy's first to its last).  Past the row's end they are none of its columns and become columns that are not stored; rows that do not
     // exist are zeroed, and what comes at the end of the last eight put in its place, when they have arrived.
-    const uint32_t y_row = threadIdx.x / kChunks, y_chunk = threadIdx.x % kChunks, y_col = n0 + y_chunk * 8;
+    const uint32_t y_row = tid / kChunks, y_chunk = tid % kChunks, y_col = n0 + y_chunk * 8;
     const uint64_t total = (uint64_t)(p.rows - 1) * p.ld + p.n;
-    const uint32_t x_row = threadIdx.x / kPieces, x_piece = threadIdx.x % kPieces, x_from = min(k0 + x_piece * 16, (uint32_t)p.code_stride - 16);
+    const uint32_t x_row = tid / kPieces, x_piece = tid % kPieces, x_from = min(k0 + x_piece * 16, (uint32_t)p.code_stride - 16);
     u4 y_next[kPassY][kParts == 1 ? 1 : 2], x_next[kPassX];
     uint32_t e_next[kPassX];
     float db[8] = {};
@@ -91,7 +97,7 @@ __global__ __launch_bounds__(kBlock, kWave == 64 && sizeof(T) == 2 ? 2 : 1) void
         y_next[i][0] = *(const u4e *)at;
         if constexpr (kParts > 1) y_next[i][1] = *(const u4e *)(at + 4);
     };
-    // Inside, where kTile rows more exist (however narrow dy is, what is asked for does): a place that goes on by a step's rows, and the passes' distances from it
+    // Inside, where all rows asked for exist: a place that goes on by a step's rows, and the passes' distances from it
     const T *y_at_next = (const T *)p.dy + (uint64_t)(t0 + 2 * kSteps + y_row) * p.ld + y_col;
     const uint8_t *x_at_next = p.codes + (uint64_t)(t0 + 2 * kSteps + x_row) * p.code_stride + x_from;
     const uint8_t *e_at_next = p.exps + (uint64_t)(t0 + 2 * kSteps + x_row) * p.exp_stride + x_from / kBlockCols;
@@ -206,11 +212,12 @@ __global__ __launch_bounds__(kBlock, kWave == 64 && sizeof(T) == 2 ? 2 : 1) void
     });
     __syncthreads();
     each<kReads>([&](auto i) { read(0, 0, 0, i); });
-    uint32_t t = t0, place = 0;
+    uint32_t t = t0, place = 0, left = steps;   // (what the loops go by is the same for all teams, as the barriers need)
     typedef std::true_type Inside;
     typedef std::false_type Outside;
+    const uint32_t margin = p.ld >= kTile ? 1 : kTile;   // rows after which a whole row of the tile exists, however narrow dy is
 #pragma clang loop unroll(disable)
-    for (; t + 2 * kSteps <= t1 && (uint64_t)t + 3 * kSteps + kTile <= p.rows; t += kSteps, place ^= 1) {
+    for (; left >= 2 && (uint64_t)t + lag + 2 * kSteps <= end && (uint64_t)t + lag + 3 * kSteps + margin <= p.rows; t += kSteps, place ^= 1, --left) {
         each<4>([&](auto group) {
             if constexpr (group == 3) {   // the next step's rows are stored, and this one's read
                 asm volatile("" ::: "memory");
@@ -238,11 +245,12 @@ __global__ __launch_bounds__(kBlock, kWave == 64 && sizeof(T) == 2 ? 2 : 1) void
     }
     // the last steps, one thing after the other (past the end: rows that exist, and zeros in their place)
 #pragma clang loop unroll(disable)
-    for (; t < t1; t += kSteps, place ^= 1) {
-        each<kStaged>([&](auto i) {
-            store(Outside(), i, place ^ 1, t + kSteps);
-            load(Outside(), i, t + 2 * kSteps);
-        });
+    for (; left; t += kSteps, place ^= 1, --left) {
+        if (kWave > 64 || left > 1)   // (for the large tile, whose registers are full, without a branch)
+            each<kStaged>([&](auto i) {
+                store(Outside(), i, place ^ 1, t + kSteps);
+                load(Outside(), i, t + 2 * kSteps);
+            });
 #pragma clang loop unroll(disable)
         for (int group = 0; group < 4; ++group) {
             each<kReads>([&](auto i) { read(0, place, group, i); });
@@ -252,36 +260,77 @@ __global__ __launch_bounds__(kBlock, kWave == 64 && sizeof(T) == 2 ? 2 : 1) void
     }
     __syncthreads();
 
+    if constexpr (kTeams > 1) {
+        static_assert(kTeams == 2 && kWaves * kSide * kSide * 4096 <= 2 * kPlace, "room in a team's own");
+        f4 *const sums_here = (f4 *)(every + 2 * kPlace) + wave * (kSide * kSide * 256) + lane;
+        if (team == 1) {
+#pragma unroll
+            for (int i = 0; i < kSide * kSide * 4; ++i) {
+                const f16 &v = acc[i / 4 / kSide][i / 4 % kSide];
+                sums_here[i * 64] = f4{v[i % 4 * 4], v[i % 4 * 4 + 1], v[i % 4 * 4 + 2], v[i % 4 * 4 + 3]};
+            }
+        }
+        __syncthreads();
+        if (team == 0) {
+#pragma unroll
+            for (int i = 0; i < kSide * kSide * 4; ++i) {
+                const f4 v = sums_here[i * 64];
+#pragma unroll
+                for (int c = 0; c < 4; ++c) acc[i / 4 / kSide][i / 4 % kSide][i % 4 * 4 + c] += v[c];
+            }
+        }
+        __syncthreads();
+    }
+    if (team == 0) {
     const uint32_t n_here = n0 + wn + (lane & 31), k_here = k0 + wk + 4 * (lane >> 5);
     float *const dw = p.dw + blockIdx.y * p.part + (uint64_t)n_here * p.k + k_here;
-    const bool whole = k0 + kTile <= p.k;   // (the same for all)
+    if (k0 + kTile <= p.k) {   // (the same for all)
 #pragma unroll
-    for (int i = 0; i < kSide; ++i) {
-        if (n_here + 32 * i >= p.n) continue;
-        float *const row = dw + (uint64_t)(32 * i) * p.k;
-        if (whole) {
+        for (int i = 0; i < kSide; ++i) {
+            if (n_here + 32 * i >= p.n) break;
+            float *const row = dw + (uint64_t)(32 * i) * p.k;
 #pragma unroll
             for (int j = 0; j < kSide; ++j)
 #pragma unroll
                 for (int c = 0; c < 4; ++c)
                     *(f4u *)(row + 32 * j + 8 * c) = f4{acc[i][j][4 * c], acc[i][j][4 * c + 1], acc[i][j][4 * c + 2], acc[i][j][4 * c + 3]};
-        } else {
+        }
+    } else {   // rows of 32 through LDS, each wavefront's for itself: columns that do not exist are left out lane by lane
+        constexpr int kRow = kWave + 4;
+        static_assert(kWaves * 32 * kRow * 4 <= 2 * kPlace, "room");
+        float *const mine = (float *)lds + wave * 32 * kRow;
+#pragma unroll
+        for (int i = 0; i < kSide; ++i) {
 #pragma unroll
             for (int j = 0; j < kSide; ++j)
 #pragma unroll
-                for (int c = 0; c < 16; ++c)
-                    if (k_here + 32 * j + c / 4 * 8 + c % 4 < p.k) row[32 * j + c / 4 * 8 + c % 4] = acc[i][j][c];
+                for (int c = 0; c < 4; ++c)
+                    *(f4 *)(mine + (lane & 31) * kRow + 32 * j + 8 * c + 4 * (lane >> 5)) =
+                        f4{acc[i][j][4 * c], acc[i][j][4 * c + 1], acc[i][j][4 * c + 2], acc[i][j][4 * c + 3]};
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            const uint32_t first = n0 + wn + 32 * i;
+            for (uint32_t col = lane; col < kWave && k0 + wk + col < p.k; col += 64) {
+                float *const at = p.dw + blockIdx.y * p.part + (uint64_t)first * p.k + k0 + wk + col;
+#pragma unroll 8
+                for (uint32_t row = 0; row < 32; ++row) {
+                    const float v = mine[row * kRow + col];
+                    if (first + row < p.n) at[(uint64_t)row * p.k] = v;
+                }
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         }
     }
+    }
     if (!sums) return;   // the threads' column sums, added in a fixed order
-    float *part = (float *)lds;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) part[y_row * kTile + y_chunk * 8 + j] = db[j];
     __syncthreads();
-    for (uint32_t c = threadIdx.x; c < kTile; c += kBlock) {
+    float *part = (float *)every;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) part[(team * kRowsY + y_row) * kTile + y_chunk * 8 + j] = db[j];
+    __syncthreads();
+    for (uint32_t c = threadIdx.x; c < kTile; c += kBlock * kTeams) {
         float s = 0.f;
 #pragma unroll
-        for (int i = 0; i < kRowsY; ++i) s += part[i * kTile + c];
+        for (int i = 0; i < kTeams * kRowsY; ++i) s += part[i * kTile + c];
         if (n0 + c < p.n) p.db[blockIdx.y * p.part + n0 + c] = s;
     }
 }
@@ -349,7 +398,10 @@ void launch_weight_grad(const void *dy, lgc_type type, uint32_t rows, uint32_t n
     auto tiles = [&](uint32_t side) { return (uint64_t)((n + side - 1) / side) * ((k + side - 1) / side); };
     const bool large = type == LGC_BF16 && tiles(256) >= (uint64_t)cus;
     const uint32_t side = large ? 256 : 128;
-    uint64_t parts = std::min({1 * (uint64_t)cus / tiles(side), (uint64_t)(rows + 255) / 256, scratch_floats / count, (uint64_t)65535});
+    // Few tiles: the rows in parts, a block per compute unit at most and 512 rows at least: the parts' sums go to memory and back, eight bytes per weight and part
+    // (us with up to one / two blocks per compute unit: 3001 x 768 x 1280 23.0 / 32, 2048 x 2048 x 2048 30 / 45, 8192 x 1024 x 1024 35 / 44; with 256 rows at least:
+    // 512 x 768 x 1280 12.1 / 16.0)
+    uint64_t parts = std::min({(uint64_t)cus / tiles(side), (uint64_t)(rows + 511) / 512, scratch_floats / count, (uint64_t)65535});
     parts = std::max<uint64_t>(parts, 1);
     p.share = (uint32_t)((rows + parts - 1) / parts + 63) / 64 * 64;
     parts = (rows + p.share - 1) / p.share;
@@ -360,9 +412,9 @@ void launch_weight_grad(const void *dy, lgc_type type, uint32_t rows, uint32_t n
         if (db) p.db = scratch + count_w;
     }
     const dim3 grid((uint32_t)tiles(side), (uint32_t)parts);
-    if (type == LGC_FP32) k_weight_grad<float, 64><<<grid, kBlock, 0, st>>>(p);
-    else if (large) k_weight_grad<Bf16, 128><<<grid, kBlock, 0, st>>>(p);
-    else k_weight_grad<Bf16, 64><<<grid, kBlock, 0, st>>>(p);
+    if (type == LGC_FP32) k_weight_grad<float, 64, 1><<<grid, kBlock, 0, st>>>(p);
+    else if (large) k_weight_grad<Bf16, 128, 1><<<grid, kBlock, 0, st>>>(p);
+    else k_weight_grad<Bf16, 64, 2><<<grid, 2 * kBlock, 0, st>>>(p);
     if (parts > 1) k_add_parts<<<adds, kBlock, 0, st>>>(scratch, (uint32_t)parts, count, dw, count_w, db, count);
 }
 
