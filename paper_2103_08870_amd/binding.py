@@ -453,31 +453,46 @@ _ACTS = {"relu": LGC_RELU, "gelu": LGC_GELU, "silu": LGC_SILU}
 _NONE = None, None
 
 
+def _refuse(what: str):
+    raise ValueError(f"liblgc binding: {what}")
+
+
 def _matrix(t: Optional[torch.Tensor], shape, dtype, what: str):
     """(pointer, elements from row to row) of a plain matrix, None: (None, 0)."""
     if t is None:
         return None, 0
-    _require(t.dim() == 2 and t.shape == shape and t.dtype == dtype, f"{what} must be {tuple(shape)} of {dtype}")
-    _require(t.stride(1) == 1 or shape[1] <= 1 or shape[0] == 0, f"{what} must have contiguous rows")
-    return _ptr(t), t.stride(0) if shape[0] > 1 else max(1, shape[1])
+    if t.dim() != 2 or t.shape != shape or t.dtype is not dtype:
+        _refuse(f"{what} must be {tuple(shape)} of {dtype}")
+    ld, step = t.stride()
+    rows, cols = shape
+    if step != 1 and cols > 1 and rows:
+        _refuse(f"{what} must have contiguous rows")
+    if not t.is_cuda:
+        raise ValueError("liblgc takes device tensors only")
+    return t.data_ptr(), ld if rows > 1 else max(1, cols)
 
 
 def _vector(t: Optional[torch.Tensor], n: int, what: str) -> Optional[int]:
-    _require(t is None or t.is_contiguous() and t.numel() == n, f"{what} must be contiguous with {n} elements")
+    if t is None:
+        return None
+    if t.numel() != n or not t.is_contiguous():
+        _refuse(f"{what} must be contiguous with {n} elements")
     return _ptr(t, torch.float32)
 
 
-def _blocks(b: Optional[Blocks], shape, what: str, tiles: bool = False):
+def _blocks(b: Optional[Blocks], rows: int, cols: int, what: str, tiles: bool = False):
     if b is None:
         return _NONE
-    _require((b.rows, b.cols) == tuple(shape) and b.tiles == tiles, f"{what} must be Blocks of {tuple(shape)} with an exponent per "
-                                                                    + ("128 x 128" if tiles else "row and 128 columns"))
+    if b.rows != rows or b.cols != cols or b.tiles != tiles:
+        _refuse(f"{what} must be Blocks of {(rows, cols)} with an exponent per " + ("128 x 128" if tiles else "row and 128 columns"))
     return b.at
 
 
 def _type(t: torch.Tensor, what: str) -> int:
-    _require(t.dim() == 2 and t.dtype in _TYPES, f"{what} must be a matrix of float32 or bfloat16")
-    return _TYPES[t.dtype]
+    kind = _TYPES.get(t.dtype)
+    if kind is None or t.dim() != 2:
+        _refuse(f"{what} must be a matrix of float32 or bfloat16")
+    return kind
 
 
 def lgc_codes_stride(cols: int) -> int:
@@ -497,7 +512,7 @@ def lgc_quantize(ctx: Context, x: torch.Tensor, out: Blocks) -> None:
     """out <- x [rows][cols], an exponent per row and 128 columns."""
     kind = _type(x, "x")
     at, ld = _matrix(x, x.shape, x.dtype, "x")
-    codes, exps = _blocks(out, x.shape, "out")
+    codes, exps = _blocks(out, *x.shape, "out")
     _check(lib().lgc_quantize(ctx.h, at, kind, x.shape[0], x.shape[1], ld, codes, exps, _stream()), ctx.h)
 
 
@@ -505,8 +520,8 @@ def lgc_quantize_weights(ctx: Context, w: torch.Tensor, out: Blocks, transposed:
     """out <- w [rows][cols], transposed <- its transpose, an exponent per 128 x 128; the same numbers in both."""
     kind = _type(w, "w")
     at, ld = _matrix(w, w.shape, w.dtype, "w")
-    codes, exps = _blocks(out, w.shape, "out", True)
-    codes_t, exps_t = _blocks(transposed, w.shape[::-1], "transposed", True)
+    codes, exps = _blocks(out, *w.shape, "out", True)
+    codes_t, exps_t = _blocks(transposed, w.shape[1], w.shape[0], "transposed", True)
     _check(lib().lgc_quantize_weights(ctx.h, at, kind, w.shape[0], w.shape[1], ld, codes, exps, codes_t, exps_t, _stream()), ctx.h)
 
 
@@ -525,7 +540,7 @@ def lgc_layer_norm(ctx: Context, x: torch.Tensor, gamma: Optional[torch.Tensor],
     rows, cols = x.shape
     at, ld = _matrix(x, x.shape, x.dtype, "x")
     out, ld_y = _matrix(y, x.shape, x.dtype, "y")
-    codes, exps = _blocks(blocks, x.shape, "blocks")
+    codes, exps = _blocks(blocks, rows, cols, "blocks")
     _check(lib().lgc_layer_norm(ctx.h, at, kind, rows, cols, ld, _vector(gamma, cols, "gamma"), _vector(beta, cols, "beta"), eps, out, ld_y,
                                 _vector(mean, rows, "mean"), _vector(rstd, rows, "rstd"), codes, exps, _stream()), ctx.h)
 
@@ -544,8 +559,10 @@ def lgc_layer_norm_grad(ctx: Context, dy: torch.Tensor, x: torch.Tensor, gamma: 
 
 
 def _act(act) -> int:
-    _require(act in _ACTS, f"act is one of {', '.join(_ACTS)}")
-    return _ACTS[act]
+    kind = _ACTS.get(act)
+    if kind is None:
+        _refuse(f"act is one of {', '.join(_ACTS)}")
+    return kind
 
 
 def lgc_activate(ctx: Context, act: str, a: torch.Tensor, z: Optional[torch.Tensor] = None, a_blocks: Optional[Blocks] = None,
@@ -554,8 +571,8 @@ def lgc_activate(ctx: Context, act: str, a: torch.Tensor, z: Optional[torch.Tens
     kind = _type(a, "a")
     at, ld = _matrix(a, a.shape, a.dtype, "a")
     out, ld_z = _matrix(z, a.shape, a.dtype, "z")
-    _check(lib().lgc_activate(ctx.h, _act(act), at, kind, a.shape[0], a.shape[1], ld, out, ld_z, *_blocks(a_blocks, a.shape, "a_blocks"),
-                              *_blocks(z_blocks, a.shape, "z_blocks"), _stream()), ctx.h)
+    _check(lib().lgc_activate(ctx.h, _act(act), at, kind, a.shape[0], a.shape[1], ld, out, ld_z, *_blocks(a_blocks, *a.shape, "a_blocks"),
+                              *_blocks(z_blocks, *a.shape, "z_blocks"), _stream()), ctx.h)
 
 
 def lgc_activate_grad(ctx: Context, act: str, dz: torch.Tensor, a_blocks: Blocks, da: Optional[torch.Tensor] = None,
@@ -564,16 +581,16 @@ def lgc_activate_grad(ctx: Context, act: str, dz: torch.Tensor, a_blocks: Blocks
     kind = _type(dz, "dz")
     at, ld = _matrix(dz, dz.shape, dz.dtype, "dz")
     out, ld_da = _matrix(da, dz.shape, dz.dtype, "da")
-    _check(lib().lgc_activate_grad(ctx.h, _act(act), at, kind, dz.shape[0], dz.shape[1], ld, *_blocks(a_blocks, dz.shape, "a_blocks"), out, ld_da,
-                                   *_blocks(da_blocks, dz.shape, "da_blocks"), _stream()), ctx.h)
+    _check(lib().lgc_activate_grad(ctx.h, _act(act), at, kind, dz.shape[0], dz.shape[1], ld, *_blocks(a_blocks, *dz.shape, "a_blocks"), out, ld_da,
+                                   *_blocks(da_blocks, *dz.shape, "da_blocks"), _stream()), ctx.h)
 
 
 def lgc_product(ctx: Context, a: Blocks, b: Blocks, bias: Optional[torch.Tensor], y: torch.Tensor) -> None:
     """y [m][n] <- a [m][k] b [n][k]^T + bias [n]; b with an exponent per 128 x 128."""
     kind = _type(y, "y")
     at, ld = _matrix(y, (a.rows, b.rows), y.dtype, "y")
-    a_codes, a_exps = _blocks(a, (a.rows, a.cols), "a")
-    b_codes, b_exps = _blocks(b, (b.rows, a.cols), "b", True)
+    a_codes, a_exps = _blocks(a, a.rows, a.cols, "a")
+    b_codes, b_exps = _blocks(b, b.rows, a.cols, "b", True)
     _check(lib().lgc_product(ctx.h, a_codes, a_exps, a.rows, b_codes, b_exps, b.rows, a.cols, _vector(bias, b.rows, "bias"), at, kind, ld, _stream()), ctx.h)
 
 
@@ -582,5 +599,5 @@ def lgc_weight_grad(ctx: Context, dy: torch.Tensor, x: Blocks, dw: torch.Tensor,
     kind = _type(dy, "dy")
     rows, n = dy.shape
     at, ld = _matrix(dy, dy.shape, dy.dtype, "dy")
-    codes, exps = _blocks(x, (rows, x.cols), "x")
+    codes, exps = _blocks(x, rows, x.cols, "x")
     _check(lib().lgc_weight_grad(ctx.h, at, kind, rows, n, ld, codes, exps, x.cols, _vector(dw, n * x.cols, "dw"), _vector(db, n, "db"), _stream()), ctx.h)

@@ -1554,7 +1554,7 @@ extern "C" lgc_status lgc_layer_norm(lgc_ctx *ctx, const void *x, lgc_type type,
     c.maybe("gamma", gamma).maybe("beta", beta).maybe("mean", mean).maybe("rstd", rstd);
     if (rows) c.plain("x", x, type, cols, ld).maybe("y", y, type, cols, ld_y).maybe_blocks("y", codes, exps);
     return launch(c, [&] {
-        if (rows) launch_norm(x, type, (uint32_t)rows, (uint32_t)cols, ld, gamma, beta, eps, y, ld_y, mean, rstd, codes, exps, (hipStream_t)stream);
+        if (rows) launch_norm(x, type, (uint32_t)rows, (uint32_t)cols, ld, gamma, beta, eps, y, ld_y, mean, rstd, codes, exps, ctx->cus, (hipStream_t)stream);
     });
 }
 

@@ -25,27 +25,58 @@ __device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
 __device__ __forceinline__ void store_one(float *p, float x) { *p = x; }
 __device__ __forceinline__ void store_one(Bf16 *p, float x) { p->bits = (uint16_t)bf16_pair(x, x); }
 
-// Eight elements of a row at p, of which the first `count` exist (others: 0).
-__device__ __forceinline__ void load_chunk(const float *p, int count, float (&x)[8]) {
-    if (count >= 8) {
-        const f4 a = *(const f4u *)p, b = *(const f4u *)(p + 4);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) { x[i] = a[i]; x[4 + i] = b[i]; }
+// How many of the eight columns from `col` on a row of `cols` has.
+__device__ __forceinline__ int count_at(uint32_t col, uint32_t cols) { return col >= cols ? 0 : cols - col >= 8 ? 8 : (int)(cols - col); }
+
+// The eight elements of a row from column `col` on, as they lie in memory: a load that is under way until they are unpacked.  Where the row has fewer, the last eight
+// that it has are asked for instead, so that no lane needs loads of its own (which the others' would be waited for before); a row of fewer than eight has them all.
+template <typename T>
+struct Chunk {
+    u4 part[sizeof(T) / 2];
+};
+__device__ __forceinline__ Chunk<float> fetch_chunk(const float *row, uint32_t col, uint32_t cols) {
+    Chunk<float> c;
+    if (cols >= 8) {
+        const float *at = row + min(col, cols - 8);
+        c.part[0] = *(const u4u *)at;
+        c.part[1] = *(const u4u *)(at + 4);
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = i < count ? p[i] : 0.f;
+        for (int i = 0; i < 8; ++i) c.part[i / 4][i % 4] = col + i < cols ? __float_as_uint(row[col + i]) : 0u;
     }
+    return c;
 }
-__device__ __forceinline__ void load_chunk(const Bf16 *p, int count, float (&x)[8]) {
-    if (count >= 8) {
-        const u4 a = *(const u4e *)p;
+__device__ __forceinline__ Chunk<Bf16> fetch_chunk(const Bf16 *row, uint32_t col, uint32_t cols) {
+    Chunk<Bf16> c;
+    if (cols >= 8) c.part[0] = *(const u4e *)(row + min(col, cols - 8));
+    else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) { x[2 * i] = __uint_as_float(a[i] << 16); x[2 * i + 1] = __uint_as_float(a[i] & 0xffff0000u); }
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t lo = col + 2 * i, hi = lo + 1;
+            c.part[0][i] = (lo < cols ? row[lo].bits : 0u) | (hi < cols ? (uint32_t)row[hi].bits << 16 : 0u);
+        }
+    }
+    return c;
+}
+// Elements that do not exist become zeros.
+template <typename T>
+__device__ __forceinline__ void unpack(const Chunk<T> &c, uint32_t col, uint32_t cols, float (&x)[8]) {
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(c.part[i / 4][i % 4]);
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = i < count ? to_float(p[i]) : 0.f;
+        for (int i = 0; i < 4; ++i) { x[2 * i] = __uint_as_float(c.part[0][i] << 16); x[2 * i + 1] = __uint_as_float(c.part[0][i] & 0xffff0000u); }
     }
+    if (cols >= 8 && col + 8 > cols)
+        for (int k = count_at(col, cols); k < 8; ++k) {
+#pragma unroll
+            for (int i = 0; i < 7; ++i) x[i] = x[i + 1];
+            x[7] = 0.f;
+        }
 }
+template <typename T>
+__device__ __forceinline__ void load_chunk(const T *row, uint32_t col, uint32_t cols, float (&x)[8]) { unpack(fetch_chunk(row, col, cols), col, cols, x); }
 __device__ __forceinline__ void store_chunk(float *p, int count, const float (&x)[8]) {
     if (count >= 8) {
         *(f4u *)p = f4{x[0], x[1], x[2], x[3]};
@@ -75,7 +106,7 @@ __device__ __forceinline__ uint32_t max_of_16(uint32_t x) {
 }
 
 constexpr uint32_t kInfKey = 0x7f800000u;
-constexpr uint32_t kLeastExp = 10, kMostExp = 247;
+constexpr uint32_t kLeastExp = 10;
 
 // The exponent byte of a block whose largest finite magnitude has this key: the least E, from kLeastExp on, with magnitude <= 448 * 2^(E - 127)
 // (448 = 1.75 * 2^8 is the largest code).  A scale that is a power of two makes the division exact, so that each element is rounded once, and it
@@ -84,30 +115,33 @@ __device__ __forceinline__ uint32_t block_exp(uint32_t key) {
     const int e = (int)(key >> 23) - 8 + ((key & 0x7fffffu) > 0x600000u ? 1 : 0);
     return e < (int)kLeastExp ? kLeastExp : (uint32_t)e;
 }
-__device__ __forceinline__ float exp_scale(uint32_t e) { return __uint_as_float(e << 23); }              // 2^(e - 127)
-__device__ __forceinline__ float exp_inverse(uint32_t e) { return __uint_as_float((254u - e) << 23); }   // 2^(127 - e)
+__device__ __forceinline__ float exp_scale(uint32_t e) { return __uint_as_float(e << 23); }   // 2^(e - 127)
 
-// magnitude's key as the block's scale sees it: infinities and NaNs are left out
-__device__ __forceinline__ uint32_t finite_key(float x) {
-    const uint32_t k = key_of(x);
-    return k < kInfKey ? k : 0u;
-}
-__device__ __forceinline__ uint32_t finite_key(const float (&x)[8]) {
-    uint32_t m = 0;
+// Key of the largest finite magnitude of the eight elements that each of 16 neighbouring lanes holds, in all of them.  The maximum passes over NaNs by itself;
+// only where it meets an infinity are elements looked at one by one.
+__device__ __forceinline__ uint32_t most_of_16(const float (&x)[8]) {
+    float m = 0.f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const uint32_t k = finite_key(x[i]);
-        m = k > m ? k : m;
+    for (int i = 0; i < 8; ++i) m = fmaxf(m, fabsf(x[i]));
+    uint32_t most = max_of_16(__float_as_uint(m));
+    if (most == kInfKey) {
+        uint32_t key = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t k = key_of(x[i]);
+            key = k < kInfKey && k > key ? k : key;
+        }
+        most = max_of_16(key);
     }
-    return m;
+    return most;
 }
-// Codes of eight elements, rounded to the nearest (ties to even); the conversion turns infinities into NaN codes.
-__device__ __forceinline__ u2 codes_of(const float (&x)[8], float inverse) {
+// Codes of eight elements divided by the block's scale, rounded to the nearest (ties to even); the conversion turns infinities into NaN codes.
+__device__ __forceinline__ u2 codes_of(const float (&x)[8], float scale) {
     u2 r;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-        int w = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * i] * inverse, x[4 * i + 1] * inverse, 0, false);
-        r[i] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x[4 * i + 2] * inverse, x[4 * i + 3] * inverse, w, true);
+        const s2 lo = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(s2{0, 0}, x[4 * i], x[4 * i + 1], scale, false);
+        r[i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(lo, x[4 * i + 2], x[4 * i + 3], scale, true));
     }
     return r;
 }
@@ -122,8 +156,8 @@ __device__ __forceinline__ void values_of(const u2 codes, float scale, float (&x
 // 16 lanes store the block that they hold, eight elements each: codes at `codes` (the lane's own eight), exponent at `exp` (the block's).
 // Elements that do not exist are zeros.  All 16 lanes must be active.
 __device__ __forceinline__ void store_block(const float (&x)[8], uint8_t *codes, uint8_t *exp) {
-    const uint32_t e = block_exp(max_of_16(finite_key(x)));
-    *(u2 *)codes = codes_of(x, exp_inverse(e));
+    const uint32_t e = block_exp(most_of_16(x));
+    *(u2 *)codes = codes_of(x, exp_scale(e));
     if ((threadIdx.x & 15) == 0) *exp = (uint8_t)e;
 }
 

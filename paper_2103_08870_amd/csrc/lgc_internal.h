@@ -310,7 +310,7 @@ void launch_activate_grad(lgc_act act, const void *dz, lgc_type type, uint32_t r
                           void *da, uint64_t ld_da, uint8_t *da_codes, uint8_t *da_exps, hipStream_t st);
 // norm.hip
 void launch_norm(const void *x, lgc_type type, uint32_t rows, uint32_t cols, uint64_t ld, const float *gamma, const float *beta, float eps, void *y, uint64_t ld_y,
-                 float *mean, float *rstd, uint8_t *codes, uint8_t *exps, hipStream_t st);
+                 float *mean, float *rstd, uint8_t *codes, uint8_t *exps, int cus, hipStream_t st);
 void launch_norm_grad(const void *dy, uint64_t ld_dy, const void *x, uint64_t ld, lgc_type type, uint32_t rows, uint32_t cols, const float *gamma, const float *mean,
                       const float *rstd, void *dx, uint64_t ld_dx, float *dgamma, float *dbeta, float *scratch, size_t scratch_floats, int cus, hipStream_t st);
 // product.hip, weight_grad.hip

@@ -7,8 +7,6 @@
 namespace lgc {
 namespace {
 
-constexpr int kColumnRows = 16;   // wavefronts that share the sum of a column's partial sums
-
 __device__ __forceinline__ float wave_sum(float x) {
     auto add = [](float a, uint32_t b) { return a + __uint_as_float(b); };
     x = add(x, __builtin_amdgcn_update_dpp(0u, __float_as_uint(x), 0x111, 0xf, 0xf, false));
@@ -33,8 +31,6 @@ __device__ __forceinline__ f2 row_sum(float a, float b, f2 *tmp) {
     return s;
 }
 
-__device__ __forceinline__ int count_at(uint32_t col, uint32_t cols) { return col >= cols ? 0 : cols - col >= 8 ? 8 : (int)(cols - col); }
-
 struct NormArgs {
     const void *x;
     uint64_t ld;
@@ -49,46 +45,72 @@ struct NormArgs {
     uint32_t exp_stride;
 };
 
+// y of eight columns, plain and in 8 bits
 template <typename T>
-__device__ __forceinline__ void norm_out(const NormArgs &a, uint64_t row, uint32_t col, int count, const float (&x)[8], float mean, float rstd) {
-    float g[8], b[8], y[8];
+__device__ __forceinline__ void norm_out(const NormArgs &a, uint64_t row, uint32_t col, int count, const float (&x)[8], float mean, float rstd, const float (&g)[8],
+                                         const float (&b)[8]) {
+    float y[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) { g[i] = 1.f; b[i] = 0.f; }
-    if (a.gamma) load_chunk(a.gamma + col, count, g);
-    if (a.beta) load_chunk(a.beta + col, count, b);
+    for (int i = 0; i < 8; ++i) y[i] = fmaf((x[i] - mean) * rstd, g[i], b[i]);
+    if (count < 8)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) y[i] = i < count ? fmaf((x[i] - mean) * rstd, g[i], b[i]) : 0.f;
+        for (int i = 0; i < 8; ++i) y[i] = i < count ? y[i] : 0.f;
     if (a.y) store_chunk((T *)a.y + row * a.ld_y + col, count, y);
     if (a.codes && col < a.code_stride) store_block(y, a.codes + row * a.code_stride + col, a.exps + row * a.exp_stride + col / kBlockCols);
 }
+__device__ __forceinline__ void load_affine(const NormArgs &a, uint32_t col, float (&g)[8], float (&b)[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) { g[i] = 1.f; b[i] = 0.f; }
+    if (a.gamma) load_chunk(a.gamma, col, a.cols, g);
+    if (a.beta) load_chunk(a.beta, col, a.cols, b);
+}
 
-// kThreads threads per row (64: four rows per block), kChunks chunks of eight columns each
+// kThreads threads per row (64: four rows per block), kChunks chunks of eight columns each.  A block takes every gridDim.x-th row (or four): gamma and beta are
+// read once, and the next row is on its way while this one's sums are made.
 template <typename T, int kThreads, int kChunks>
-__global__ __launch_bounds__(kThreads < kBlock ? kBlock : kThreads) void k_norm(NormArgs a) {
+__global__ __launch_bounds__(kThreads == 64 ? kBlock : kThreads) void k_norm(NormArgs a) {
     __shared__ f2 tmp[2][kThreads / 64];
     constexpr int kRowsHere = kThreads == 64 ? kWaves : 1;
     const uint32_t lane = kThreads == 64 ? threadIdx.x & 63 : threadIdx.x;
+    const uint64_t on = (uint64_t)gridDim.x * kRowsHere;
     const float per = 1.f / (float)a.cols;
-    for (uint64_t row = (uint64_t)blockIdx.x * kRowsHere + (kThreads == 64 ? threadIdx.x / 64 : 0); row < a.rows; row += (uint64_t)gridDim.x * kRowsHere) {
-        float x[kChunks][8], sum = 0.f, square = 0.f;
+    uint64_t row = (uint64_t)blockIdx.x * kRowsHere + (kThreads == 64 ? threadIdx.x / 64 : 0);
+    Chunk<T> next[kChunks];
+    float g[kChunks][8], b[kChunks][8];
+    auto load = [&](uint64_t r) {
 #pragma unroll
         for (int c = 0; c < kChunks; ++c) {
             const uint32_t col = (c * kThreads + lane) * 8;
-            load_chunk((const T *)a.x + row * a.ld + col, count_at(col, a.cols), x[c]);
+            next[c] = fetch_chunk((const T *)a.x + r * a.ld, col, a.cols);
         }
+    };
+    if (row < a.rows) load(row);
 #pragma unroll
-        for (int c = 0; c < kChunks; ++c)
+    for (int c = 0; c < kChunks; ++c) {
+        const uint32_t col = (c * kThreads + lane) * 8;
+        load_affine(a, col, g[c], b[c]);
+    }
+    for (; row < a.rows; row += on) {
+        float x[kChunks][8], sum = 0.f, square = 0.f;
+#pragma unroll
+        for (int c = 0; c < kChunks; ++c) {
+            unpack(next[c], (c * kThreads + lane) * 8, a.cols, x[c]);
 #pragma unroll
             for (int i = 0; i < 8; ++i) sum += x[c][i];
+        }
+        if (row + on < a.rows) load(row + on);
         const float mean = row_sum<kThreads>(sum, 0.f, tmp[0])[0] * per;
 #pragma unroll
         for (int c = 0; c < kChunks; ++c) {
             const int count = count_at((c * kThreads + lane) * 8, a.cols);
+            float d[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float d = i < count ? x[c][i] - mean : 0.f;
-                square = fmaf(d, d, square);
-            }
+            for (int i = 0; i < 8; ++i) d[i] = x[c][i] - mean;
+            if (count < 8)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) d[i] = i < count ? d[i] : 0.f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) square = fmaf(d[i], d[i], square);
         }
         const float rstd = 1.f / sqrtf(row_sum<kThreads>(square, 0.f, tmp[1])[0] * per + a.eps);
         if (lane == 0) {
@@ -98,7 +120,7 @@ __global__ __launch_bounds__(kThreads < kBlock ? kBlock : kThreads) void k_norm(
 #pragma unroll
         for (int c = 0; c < kChunks; ++c) {
             const uint32_t col = (c * kThreads + lane) * 8;
-            norm_out<T>(a, row, col, count_at(col, a.cols), x[c], mean, rstd);
+            norm_out<T>(a, row, col, count_at(col, a.cols), x[c], mean, rstd, g[c], b[c]);
         }
     }
 }
@@ -112,14 +134,14 @@ __global__ __launch_bounds__(1024) void k_norm_long(NormArgs a) {
         const T *x = (const T *)a.x + row * a.ld;
         float v[8], sum = 0.f, square = 0.f;
         for (uint32_t col = threadIdx.x * 8; col < a.cols; col += 8192) {
-            load_chunk(x + col, count_at(col, a.cols), v);
+            load_chunk(x, col, a.cols, v);
 #pragma unroll
             for (int i = 0; i < 8; ++i) sum += v[i];
         }
         const float mean = row_sum<1024>(sum, 0.f, tmp[0])[0] * per;
         for (uint32_t col = threadIdx.x * 8; col < a.cols; col += 8192) {
             const int count = count_at(col, a.cols);
-            load_chunk(x + col, count, v);
+            load_chunk(x, col, a.cols, v);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const float d = i < count ? v[i] - mean : 0.f;
@@ -133,8 +155,10 @@ __global__ __launch_bounds__(1024) void k_norm_long(NormArgs a) {
         }
         for (uint32_t col = threadIdx.x * 8; col < codes_stride(a.cols); col += 8192) {
             const int count = count_at(col, a.cols);
-            load_chunk(x + col, count, v);
-            norm_out<T>(a, row, col, count, v, mean, rstd);
+            float g[8], b[8];
+            load_chunk(x, col, a.cols, v);
+            load_affine(a, col, g, b);
+            norm_out<T>(a, row, col, count, v, mean, rstd, g, b);
         }
     }
 }
@@ -153,42 +177,66 @@ struct NormGradArgs {
 
 // As k_norm; a block takes every gridDim.x-th row (or four), keeps its columns' sums in registers and writes them at its end.
 template <typename T, int kThreads, int kChunks>
-__global__ __launch_bounds__(kThreads < kBlock ? kBlock : kThreads) void k_norm_grad(NormGradArgs a) {
+__global__ __launch_bounds__(kThreads == 64 ? kBlock : kThreads) void k_norm_grad(NormGradArgs a) {
     constexpr int kRowsHere = kThreads == 64 ? kWaves : 1;
+    constexpr bool kAhead = kThreads * kChunks < 2048;   // the next row is on its way while this one's sums are made, and gamma is kept, where registers hold them
     __shared__ f2 tmp[2][kThreads / 64];
     __shared__ float joined[kThreads == 64 ? kChunks * 64 * 8 : 1];
     const uint32_t lane = kThreads == 64 ? threadIdx.x & 63 : threadIdx.x, wave = threadIdx.x / 64;
     const float per = 1.f / (float)a.cols;
-    float g[kChunks][8], sum_h[kChunks][8], sum_1[kChunks][8];
+    float g[kChunks][8], sum_h[kChunks][8] = {}, sum_1[kChunks][8] = {};
+    auto load_gamma = [&](uint32_t col, float (&to)[8]) {
 #pragma unroll
-    for (int c = 0; c < kChunks; ++c) {
-        const uint32_t col = (c * kThreads + lane) * 8;
+        for (int i = 0; i < 8; ++i) to[i] = 1.f;
+        if (a.gamma) load_chunk(a.gamma, col, a.cols, to);
+    };
+    if constexpr (kAhead)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) { g[c][i] = 1.f; sum_h[c][i] = sum_1[c][i] = 0.f; }
-        if (a.gamma) load_chunk(a.gamma + col, count_at(col, a.cols), g[c]);
-    }
-    int turn = 0;
-    for (uint64_t row = (uint64_t)blockIdx.x * kRowsHere + (kThreads == 64 ? wave : 0); row < a.rows; row += (uint64_t)gridDim.x * kRowsHere, turn ^= 1) {
-        float h[kChunks][8], dy[kChunks][8], s1 = 0.f, s2 = 0.f;
-        const float mean = a.mean[row], rstd = a.rstd[row];
+        for (int c = 0; c < kChunks; ++c) load_gamma((c * kThreads + lane) * 8, g[c]);
+    Chunk<T> x_next[kChunks], dy_next[kChunks];
+    float mean_next = 0.f, rstd_next = 0.f;
+    auto load = [&](uint64_t row) {
+        mean_next = a.mean[row];
+        rstd_next = a.rstd[row];
 #pragma unroll
         for (int c = 0; c < kChunks; ++c) {
             const uint32_t col = (c * kThreads + lane) * 8;
-            const int count = count_at(col, a.cols);
-            load_chunk((const T *)a.x + row * a.ld + col, count, h[c]);
-            load_chunk((const T *)a.dy + row * a.ld_dy + col, count, dy[c]);
+            x_next[c] = fetch_chunk((const T *)a.x + row * a.ld, col, a.cols);
+            dy_next[c] = fetch_chunk((const T *)a.dy + row * a.ld_dy, col, a.cols);
         }
+    };
+    const uint64_t on = (uint64_t)gridDim.x * kRowsHere;
+    uint64_t row = (uint64_t)blockIdx.x * kRowsHere + (kThreads == 64 ? wave : 0);
+    if (kAhead && row < a.rows) load(row);
+    for (int turn = 0; row < a.rows; row += on, turn ^= 1) {
+        float h[kChunks][8], dy[kChunks][8], s1 = 0.f, s2 = 0.f;
+        const float mean = kAhead ? mean_next : a.mean[row], rstd = kAhead ? rstd_next : a.rstd[row];
 #pragma unroll
-        for (int c = 0; c < kChunks; ++c)
+        for (int c = 0; c < kChunks; ++c) {
+            const uint32_t col = (c * kThreads + lane) * 8;
+            if constexpr (kAhead) {
+                unpack(x_next[c], col, a.cols, h[c]);
+                unpack(dy_next[c], col, a.cols, dy[c]);
+            } else {
+                load_chunk((const T *)a.x + row * a.ld, col, a.cols, h[c]);
+                load_chunk((const T *)a.dy + row * a.ld_dy, col, a.cols, dy[c]);
+            }
+        }
+        if (kAhead && row + on < a.rows) load(row + on);
+#pragma unroll
+        for (int c = 0; c < kChunks; ++c) {
+            float here[8];
+            if constexpr (!kAhead) load_gamma((c * kThreads + lane) * 8, here);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {   // (where there is no column, dy is 0)
                 h[c][i] = (h[c][i] - mean) * rstd;
                 sum_h[c][i] = fmaf(dy[c][i], h[c][i], sum_h[c][i]);
                 sum_1[c][i] += dy[c][i];
-                dy[c][i] *= g[c][i];
+                dy[c][i] *= kAhead ? g[c][i] : here[i];
                 s1 += dy[c][i];
                 s2 = fmaf(dy[c][i], h[c][i], s2);
             }
+        }
         const f2 s = row_sum<kThreads>(s1, s2, tmp[turn]);
         const float c1 = s[0] * per, c2 = s[1] * per;
         if (a.dx)
@@ -239,17 +287,17 @@ __global__ __launch_bounds__(1024) void k_norm_grad_long(NormGradArgs a) {
         const T *x = (const T *)a.x + row * a.ld, *dy = (const T *)a.dy + row * a.ld_dy;
         const float mean = a.mean[row], rstd = a.rstd[row];
         float h[8], d[8], g[8], s1 = 0.f, s2 = 0.f;
-        auto load = [&](uint32_t col, int count) {
+        auto load = [&](uint32_t col) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) g[i] = 1.f;
-            load_chunk(x + col, count, h);
-            load_chunk(dy + col, count, d);
-            if (a.gamma) load_chunk(a.gamma + col, count, g);
+            load_chunk(x, col, a.cols, h);
+            load_chunk(dy, col, a.cols, d);
+            if (a.gamma) load_chunk(a.gamma, col, a.cols, g);
 #pragma unroll
             for (int i = 0; i < 8; ++i) { h[i] = (h[i] - mean) * rstd; d[i] *= g[i]; }
         };
         for (uint32_t col = threadIdx.x * 8; col < a.cols; col += 8192) {
-            load(col, count_at(col, a.cols));
+            load(col);
 #pragma unroll
             for (int i = 0; i < 8; ++i) { s1 += d[i]; s2 = fmaf(d[i], h[i], s2); }
         }
@@ -257,7 +305,7 @@ __global__ __launch_bounds__(1024) void k_norm_grad_long(NormGradArgs a) {
         const float c1 = s[0] * per, c2 = s[1] * per;
         for (uint32_t col = threadIdx.x * 8; col < a.cols; col += 8192) {
             const int count = count_at(col, a.cols);
-            load(col, count);
+            load(col);
 #pragma unroll
             for (int i = 0; i < 8; ++i) d[i] = rstd * (d[i] - c1 - h[i] * c2);
             store_chunk((T *)a.dx + row * a.ld_dx + col, count, d);
@@ -274,8 +322,8 @@ __global__ __launch_bounds__(kBlock) void k_norm_grad_columns(NormGradArgs a) {
     float sum_h[8] = {}, sum_1[8] = {};
     for (uint64_t row = blockIdx.y; row < a.rows; row += gridDim.y) {
         float h[8], d[8];
-        load_chunk((const T *)a.x + row * a.ld + col, count, h);
-        load_chunk((const T *)a.dy + row * a.ld_dy + col, count, d);
+        load_chunk((const T *)a.x + row * a.ld, col, a.cols, h);
+        load_chunk((const T *)a.dy + row * a.ld_dy, col, a.cols, d);
         const float mean = a.mean[row], rstd = a.rstd[row];
 #pragma unroll
         for (int i = 0; i < 8; ++i) { sum_h[i] = fmaf(d[i], (h[i] - mean) * rstd, sum_h[i]); sum_1[i] += d[i]; }
@@ -285,51 +333,50 @@ __global__ __launch_bounds__(kBlock) void k_norm_grad_columns(NormGradArgs a) {
     store_chunk(part + a.cols + col, count, sum_1);
 }
 
-// Column sums of the blocks' partial sums, in a fixed order; blockIdx.y: which of the two
-__global__ __launch_bounds__(64 * kColumnRows) void k_norm_columns(const float *part, uint32_t blocks, uint32_t cols, float *dgamma, float *dbeta) {
-    __shared__ float tmp[kColumnRows][64];
+// Column sums of the blocks' partial sums, in a fixed order; blockIdx.y: which of the two.  16 columns per block (64 bytes of a partial sum at a time), so that there
+// are blocks enough; 64 threads share a column.
+constexpr int kColumns = 16;
+__global__ __launch_bounds__(64 * kColumns) void k_norm_columns(const float *part, uint32_t blocks, uint32_t cols, float *dgamma, float *dbeta) {
+    __shared__ float tmp[64][kColumns + 1];
     float *out = blockIdx.y ? dbeta : dgamma;
     if (!out) return;
-    const uint32_t col = blockIdx.x * 64 + (threadIdx.x & 63), wave = threadIdx.x / 64;
+    const uint32_t at = threadIdx.x % kColumns, group = threadIdx.x / kColumns, col = blockIdx.x * kColumns + at;
     float s = 0.f;
     if (col < cols)
-#pragma unroll 8
-        for (uint32_t p = wave; p < blocks; p += kColumnRows) s += part[((uint64_t)p * 2 + blockIdx.y) * cols + col];
-    tmp[wave][threadIdx.x & 63] = s;
+#pragma unroll 4
+        for (uint32_t p = group; p < blocks; p += 64) s += part[((uint64_t)p * 2 + blockIdx.y) * cols + col];
+    tmp[group][at] = s;
     __syncthreads();
-    if (wave == 0 && col < cols) {
-#pragma unroll
-        for (int i = 1; i < kColumnRows; ++i) s += tmp[i][threadIdx.x];
-        out[col] = s;
-    }
+    // a wavefront per column: lane: group
+    s = wave_sum(tmp[threadIdx.x & 63][threadIdx.x / 64]);
+    if ((threadIdx.x & 63) == 0 && blockIdx.x * kColumns + threadIdx.x / 64 < cols) out[blockIdx.x * kColumns + threadIdx.x / 64] = s;
 }
 
 constexpr uint32_t kMostBlocks = 1u << 20;   // of a launch; a block goes on with later rows
-constexpr uint32_t kLongNorm = 32768, kLongGrad = 16384;   // columns from which on registers do not hold a row
+constexpr uint32_t kLongNorm = 16384, kLongGrad = 16384;   // columns from which on registers do not hold a row
 
 template <typename T>
-void norm_of(const NormArgs &a, hipStream_t st) {
-#define NORM(kThreads, kChunks) k_norm<T, kThreads, kChunks><<<std::min(kThreads == 64 ? (a.rows + kWaves - 1) / kWaves : a.rows, kMostBlocks), kThreads < kBlock ? kBlock : kThreads, 0, st>>>(a)
+void norm_of(const NormArgs &a, uint32_t blocks, hipStream_t st) {
+#define NORM(kThreads, kChunks) k_norm<T, kThreads, kChunks><<<std::min(kThreads == 64 ? (a.rows + kWaves - 1) / kWaves : a.rows, blocks), kThreads == 64 ? kBlock : kThreads, 0, st>>>(a)
     const uint32_t c = a.cols;
     if (c <= 512) NORM(64, 1);
     else if (c <= 1024) NORM(64, 2);
     else if (c <= 2048) NORM(256, 1);
     else if (c <= 4096) NORM(256, 2);
-    else if (c <= 8192) NORM(256, 4);
-    else if (c <= 16384) NORM(1024, 2);
-    else if (c <= kLongNorm) NORM(1024, 4);
+    else if (c <= 8192) NORM(512, 2);
+    else if (c <= kLongNorm) NORM(1024, 2);
     else k_norm_long<T><<<std::min(a.rows, kMostBlocks), 1024, 0, st>>>(a);
 #undef NORM
 }
 
 template <typename T>
 void norm_grad_of(const NormGradArgs &a, uint32_t blocks, hipStream_t st) {
-#define GRAD(kThreads, kChunks) k_norm_grad<T, kThreads, kChunks><<<blocks, kThreads < kBlock ? kBlock : kThreads, 0, st>>>(a)
+#define GRAD(kThreads, kChunks) k_norm_grad<T, kThreads, kChunks><<<blocks, kThreads == 64 ? kBlock : kThreads, 0, st>>>(a)
     const uint32_t c = a.cols;
     if (c <= 512) GRAD(64, 1);
-    else if (c <= 1024) GRAD(64, 2);
+    else if (c <= 1024) GRAD(128, 1);
     else if (c <= 2048) GRAD(256, 1);
-    else if (c <= 4096) GRAD(256, 2);
+    else if (c <= 4096) GRAD(512, 1);
     else if (c <= 8192) GRAD(1024, 1);
     else if (c <= kLongGrad) GRAD(1024, 2);
     else {
@@ -342,16 +389,18 @@ void norm_grad_of(const NormGradArgs &a, uint32_t blocks, hipStream_t st) {
 }  // namespace
 
 void launch_norm(const void *x, lgc_type type, uint32_t rows, uint32_t cols, uint64_t ld, const float *gamma, const float *beta, float eps, void *y, uint64_t ld_y,
-                 float *mean, float *rstd, uint8_t *codes, uint8_t *exps, hipStream_t st) {
+                 float *mean, float *rstd, uint8_t *codes, uint8_t *exps, int cus, hipStream_t st) {
+    const uint32_t blocks = (uint32_t)cus * (cols <= 1024 || cols > 4096 ? 4 : 8);   // about as many as are resident
     const NormArgs a{x, ld, rows, cols, gamma, beta, eps, y, ld_y, mean, rstd, codes, exps, codes_stride(cols), (uint32_t)exps_stride(cols)};
-    if (type == LGC_FP32) norm_of<float>(a, st);
-    else norm_of<Bf16>(a, st);
+    if (type == LGC_FP32) norm_of<float>(a, blocks, st);
+    else norm_of<Bf16>(a, blocks, st);
 }
 
 void launch_norm_grad(const void *dy, uint64_t ld_dy, const void *x, uint64_t ld, lgc_type type, uint32_t rows, uint32_t cols, const float *gamma, const float *mean,
                       const float *rstd, void *dx, uint64_t ld_dx, float *dgamma, float *dbeta, float *scratch, size_t scratch_floats, int cus, hipStream_t st) {
-    const uint32_t rows_at_once = cols <= 1024 ? kWaves : 1;
-    uint32_t blocks = cols > kLongGrad ? 64 : (uint32_t)cus * (cols <= 4096 ? 4 : cols <= 8192 ? 2 : 1);
+    const uint32_t rows_at_once = cols <= 512 ? kWaves : 1;
+    uint32_t blocks = cols > kLongGrad ? 64 : (uint32_t)cus * (cols <= 2048 ? 4 : cols <= 8192 ? 2 : 1);
+    blocks = std::min(blocks, std::max((uint32_t)cus, rows / (4 * rows_at_once)));
     const uint32_t most = (uint32_t)(scratch_floats / (2 * (size_t)cols));
     if (blocks > most) blocks = most;
     if (blocks > (rows + rows_at_once - 1) / rows_at_once) blocks = (rows + rows_at_once - 1) / rows_at_once;
@@ -360,7 +409,7 @@ void launch_norm_grad(const void *dy, uint64_t ld_dy, const void *x, uint64_t ld
         if (type == LGC_FP32) norm_grad_of<float>(a, blocks, st);
         else norm_grad_of<Bf16>(a, blocks, st);
     }
-    if (dgamma || dbeta) k_norm_columns<<<dim3((cols + 63) / 64, 2), 64 * kColumnRows, 0, st>>>(scratch, blocks, cols, dgamma, dbeta);
+    if (dgamma || dbeta) k_norm_columns<<<dim3((cols + kColumns - 1) / kColumns, 2), 64 * kColumns, 0, st>>>(scratch, blocks, cols, dgamma, dbeta);
 }
 
 }  // namespace lgc

@@ -327,11 +327,12 @@ __global__ __launch_bounds__(kBlock) void k_join(const float *part, uint32_t par
     const uint64_t id = (uint64_t)blockIdx.x * kBlock + threadIdx.x;
     if (id >= (uint64_t)m * chunks.by) return;
     const uint32_t row = quotient((uint32_t)id, chunks), col = ((uint32_t)id - row * chunks.by) * 8;
-    const int count = n - col >= 8 ? 8 : (int)(n - col);
+    const int count = count_at(col, n);
     float s[8] = {}, v[8];
-    if (bias) load_chunk(bias + col, count, s);
+    if (bias) load_chunk(bias, col, n, s);
+#pragma unroll 4
     for (uint32_t i = 0; i < parts; ++i) {
-        load_chunk(part + ((uint64_t)i * m + row) * n + col, count, v);
+        load_chunk(part + ((uint64_t)i * m + row) * n, col, n, v);
 #pragma unroll
         for (int j = 0; j < 8; ++j) s[j] += v[j];
     }
