@@ -63,7 +63,8 @@ template <int N, typename F>
 __device__ __forceinline__ void each(F &&f) { each_of(std::make_integer_sequence<int, N>(), f); }
 
 // kTeams teams of four wavefronts do this for a part of the block's rows each, and their sums meet in LDS: with small tiles, whose wavefronts wait for LDS half of
-// the time, two per SIMD are faster than one (8192 x 2048 x 2048: 99 us to 83).
+// the time, two per SIMD are faster than one (8192 x 2048 x 2048: 99 us to 83).  Where there are blocks enough, two blocks of one team are that too, and one's products
+// run during the other's stores (3467 x 13081 x 512: 87 us to 76).
 template <typename T, int kWave, int kTeams>
 __global__ __launch_bounds__(kBlock * kTeams) void k_weight_grad(WeightGradArgs p) {
     constexpr int kParts = sizeof(T) == 2 ? 1 : 3, kTile = 2 * kWave, kPitch = kTile * 2, kPlace = (kParts + 1) * kSteps * kPitch, kSide = kWave / 32;
@@ -281,24 +282,12 @@ __global__ __launch_bounds__(kBlock * kTeams) void k_weight_grad(WeightGradArgs 
         }
         __syncthreads();
     }
-    if (team == 0) {
-    const uint32_t n_here = n0 + wn + (lane & 31), k_here = k0 + wk + 4 * (lane >> 5);
-    float *const dw = p.dw + blockIdx.y * p.part + (uint64_t)n_here * p.k + k_here;
-    if (k0 + kTile <= p.k) {   // (the same for all)
-#pragma unroll
-        for (int i = 0; i < kSide; ++i) {
-            if (n_here + 32 * i >= p.n) break;
-            float *const row = dw + (uint64_t)(32 * i) * p.k;
-#pragma unroll
-            for (int j = 0; j < kSide; ++j)
-#pragma unroll
-                for (int c = 0; c < 4; ++c)
-                    *(f4u *)(row + 32 * j + 8 * c) = f4{acc[i][j][4 * c], acc[i][j][4 * c + 1], acc[i][j][4 * c + 2], acc[i][j][4 * c + 3]};
-        }
-    } else {   // rows of 32 through LDS, each wavefront's for itself: columns that do not exist are left out lane by lane
-        constexpr int kRow = kWave + 4;
+    if (team == 0) {   // 32 rows at a time through LDS, each wavefront's for itself, to be stored in whole lines
+        constexpr int kRow = kWave + 4, kLanes = kWave / 4;   // kLanes: that a row takes
         static_assert(kWaves * 32 * kRow * 4 <= 2 * kPlace, "room");
         float *const mine = (float *)lds + wave * 32 * kRow;
+        const uint32_t row0 = lane / kLanes, col = lane % kLanes * 4, k_here = k0 + wk + col;
+        const int count = k_here < p.k ? (int)min(p.k - k_here, 4u) : 0;
 #pragma unroll
         for (int i = 0; i < kSide; ++i) {
 #pragma unroll
@@ -308,18 +297,22 @@ __global__ __launch_bounds__(kBlock * kTeams) void k_weight_grad(WeightGradArgs 
                     *(f4 *)(mine + (lane & 31) * kRow + 32 * j + 8 * c + 4 * (lane >> 5)) =
                         f4{acc[i][j][4 * c], acc[i][j][4 * c + 1], acc[i][j][4 * c + 2], acc[i][j][4 * c + 3]};
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-            const uint32_t first = n0 + wn + 32 * i;
-            for (uint32_t col = lane; col < kWave && k0 + wk + col < p.k; col += 64) {
-                float *const at = p.dw + blockIdx.y * p.part + (uint64_t)first * p.k + k0 + wk + col;
-#pragma unroll 8
-                for (uint32_t row = 0; row < 32; ++row) {
-                    const float v = mine[row * kRow + col];
-                    if (first + row < p.n) at[(uint64_t)row * p.k] = v;
+            const uint32_t first = n0 + wn + 32 * i + row0;
+            const float *const line = mine + row0 * kRow + col;
+            float *const at = p.dw + blockIdx.y * p.part + (uint64_t)first * p.k + k_here;
+            if (count == 4) {
+#pragma unroll
+                for (int s = 0; s < 32; s += 64 / kLanes) {
+                    if (first + s >= p.n) break;
+                    const f4 v = *(const f4 *)(line + s * kRow);
+                    if constexpr (kWave == 64) __builtin_nontemporal_store(v, (f4u *)(at + (uint64_t)s * p.k));
+                    else *(f4u *)(at + (uint64_t)s * p.k) = v;
                 }
-            }
+            } else
+                for (int s = 0; s < 32 && first + s < p.n; s += 64 / kLanes)
+                    for (int c = 0; c < count; ++c) at[(uint64_t)s * p.k + c] = line[s * kRow + c];
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         }
-    }
     }
     if (!sums) return;   // the threads' column sums, added in a fixed order
     __syncthreads();
@@ -396,12 +389,17 @@ void launch_weight_grad(const void *dy, lgc_type type, uint32_t rows, uint32_t n
         return;
     }
     auto tiles = [&](uint32_t side) { return (uint64_t)((n + side - 1) / side) * ((k + side - 1) / side); };
-    const bool large = type == LGC_BF16 && tiles(256) >= (uint64_t)cus;
+    // Large tiles for a block per compute unit at least, and for rows that make the products last longer than a tile's stores, during which a block that has a compute
+    // unit for itself multiplies nothing (us, small / large tiles: 32 x 8192 x 8192 52 / 77, 400 x 8192 x 8192 119 / 134, 800 x 8192 x 8192 171 / 167,
+    // 8192 x 4096 x 16384 1216 / 960)
+    const bool large = type == LGC_BF16 && rows > 512 && tiles(256) >= (uint64_t)cus;
     const uint32_t side = large ? 256 : 128;
     // Few tiles: the rows in parts, a block per compute unit at most and 512 rows at least: the parts' sums go to memory and back, eight bytes per weight and part
-    // (us with up to one / two blocks per compute unit: 3001 x 768 x 1280 23.0 / 32, 2048 x 2048 x 2048 30 / 45, 8192 x 1024 x 1024 35 / 44; with 256 rows at least:
-    // 512 x 768 x 1280 12.1 / 16.0)
-    uint64_t parts = std::min({(uint64_t)cus / tiles(side), (uint64_t)(rows + 511) / 512, scratch_floats / count, (uint64_t)65535});
+    // (us with up to one / two blocks per compute unit: 3001 x 768 x 1280 21.7 / 22.8, 2048 x 2048 x 2048 28 / 40, 8192 x 1024 x 1024 33 / 37; with 256 rows at least:
+    // 512 x 768 x 1280 12.1 / 16.0).  Two blocks where one leaves over a third of the compute units idle and the rows are many (16384 x 1500 x 1500 135 / 113,
+    // 8192 x 1500 x 1500 73 / 65, 4096 x 1500 x 1500 41 / 41).
+    const uint64_t one = (uint64_t)cus / tiles(side), two = 2 * (uint64_t)cus / tiles(side);
+    uint64_t parts = std::min({3 * one * tiles(side) < 2 * (uint64_t)cus && rows >= 2048 * two ? two : one, (uint64_t)(rows + 511) / 512, scratch_floats / count, (uint64_t)65535});
     parts = std::max<uint64_t>(parts, 1);
     p.share = (uint32_t)((rows + parts - 1) / parts + 63) / 64 * 64;
     parts = (rows + p.share - 1) / p.share;
@@ -414,6 +412,7 @@ void launch_weight_grad(const void *dy, lgc_type type, uint32_t rows, uint32_t n
     const dim3 grid((uint32_t)tiles(side), (uint32_t)parts);
     if (type == LGC_FP32) k_weight_grad<float, 64, 1><<<grid, kBlock, 0, st>>>(p);
     else if (large) k_weight_grad<Bf16, 128, 1><<<grid, kBlock, 0, st>>>(p);
+    else if (tiles(side) * parts > (uint64_t)cus) k_weight_grad<Bf16, 64, 1><<<grid, kBlock, 0, st>>>(p);   // (two blocks share a compute unit)
     else k_weight_grad<Bf16, 64, 2><<<grid, 2 * kBlock, 0, st>>>(p);
     if (parts > 1) k_add_parts<<<adds, kBlock, 0, st>>>(scratch, (uint32_t)parts, count, dw, count_w, db, count);
 }

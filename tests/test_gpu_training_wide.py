@@ -1,0 +1,91 @@
+"""Products and weight gradients of widths at which other kernels, or other splits of the sum, serve them than small ones: against their definitions in 64 bits, within
+bounds that follow from the format of what is stored and from the length of the fp32 sums (U: half a unit of an fp32 number's last place)."""
+import pytest
+import torch
+
+import training_reference as ref
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+STORE = {torch.float32: U, torch.bfloat16: 2.0 ** -8}      # rounding of a stored result (bf16: a whole unit)
+TYPES = [torch.float32, torch.bfloat16]
+
+
+@pytest.fixture(scope="module")
+def B():
+    from paper_2103_08870_amd import binding
+    binding.lib()
+    assert torch.cuda.is_available()
+    return binding
+
+
+@pytest.fixture(scope="module")
+def ctx(B):
+    c = B.Context(1, 1, 1)
+    B.lgc_reserve_training(c)
+    yield c
+    c.close()
+
+
+def rand(shape, seed, scale=1.0, dtype=torch.float32):
+    gen = torch.Generator().manual_seed(seed)
+    return (torch.randn(shape, generator=gen) * scale).to(dtype)
+
+
+def as_blocks(B, ctx, x, tiles=False):
+    b = B.Blocks(x.shape[0], x.shape[1], tiles=tiles)
+    (B.lgc_quantize_weights if tiles else B.lgc_quantize)(ctx, x.cuda(), b)
+    return b
+
+
+def guarded(rows, cols, pad, dtype):
+    """Rows cols + pad apart, and the array they lie in, all 7."""
+    whole = torch.full((rows, cols + pad), 7.0, dtype=dtype, device="cuda")
+    return whole[:, :cols], whole
+
+
+# A block per compute unit and more of the largest tiles, with rows and columns that end inside one; few rows of many columns; a long sum of few tiles
+PRODUCTS = [(4100, 4200, 300), (4133, 4229, 130), (6, 8300, 300), (20, 8421, 1000), (50, 8195, 700), (2, 130, 16000), (150, 700, 16000), (600, 600, 9000)]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("m,n,k", PRODUCTS)
+def test_product(B, ctx, m, n, k, dtype):
+    a = as_blocks(B, ctx, rand((m, k), m + n + k) * torch.exp(2 * rand((m, 1), k)))
+    b = as_blocks(B, ctx, rand((n, k), n * k % 1000, 0.1), tiles=True)
+    bias = rand((n,), 3).cuda()
+    x, w = ref.blocks_values(a).cuda(), ref.blocks_values(b).cuda()
+    size, exact = x.abs() @ w.abs().t(), x @ w.t()
+    for add, pad in ((bias, 0), (None, 3)):
+        y, whole = guarded(m, n, pad, dtype)
+        B.lgc_product(ctx, a, b, add, y)
+        want = exact if add is None else exact + add.double()
+        # bf16: of eight neighbouring products each may lose 2^-14 of the largest; fp32: k additions at most
+        bound = (2.0 ** -11 if dtype == torch.bfloat16 else (k + 16) * U) * size + STORE[dtype] * want.abs() + 4 * U * (1.0 if add is None else add.abs().double())
+        assert ((y.double() - want).abs() <= bound).all()
+        assert (whole[:, n:] == 7.0).all()
+
+
+# One, two and many steps of many tiles; the largest tiles, whole and with edges; tiles that leave compute units idle and a long sum, in parts
+WEIGHT_GRADS = [(1, 2100, 2200), (70, 2177, 2201), (130, 8192, 700), (513, 4096, 4096), (650, 4099, 4131), (6200, 1500, 1501), (700, 1500, 1536)]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,n,k", WEIGHT_GRADS)
+def test_weight_grad(B, ctx, rows, n, k, dtype):
+    x = as_blocks(B, ctx, rand((rows, k), rows + k) * torch.exp(2 * rand((rows, 1), n)))
+    source = rand((rows, n), n + k, 1e-2, dtype).cuda()
+    xv, yv = ref.blocks_values(x).cuda(), source.double()
+    want, size = yv.t() @ xv, yv.abs().t() @ xv.abs()
+    for pad in (0, 1):
+        dy, _ = guarded(rows, n, pad, dtype)
+        dy.copy_(source)
+        dw, db = torch.full((n + 1, k), 7.0, device="cuda"), torch.full((n + 1,), 7.0, device="cuda")
+        B.lgc_weight_grad(ctx, dy, x, dw[:n], db[:n])
+        assert ((dw[:n].double() - want).abs() <= (rows + 64) * U * size + 1e-36).all()
+        assert ((db[:n].double() - yv.sum(0)).abs() <= (rows + 64) * U * yv.abs().sum(0) + 1e-36).all()
+        assert (dw[n] == 7.0).all() and db[n] == 7.0
+        alone = torch.empty((n, k), device="cuda")
+        B.lgc_weight_grad(ctx, dy, x, alone)
+        assert torch.equal(alone, dw[:n])
