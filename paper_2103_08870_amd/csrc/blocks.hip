@@ -76,10 +76,11 @@ __global__ __launch_bounds__(kBlock) void k_dequantize(const uint8_t *codes, con
 template <typename T>
 __global__ __launch_bounds__(kBlock) void k_quantize_tiles(const T *w, uint64_t ld, uint32_t rows, uint32_t cols, uint8_t *codes, uint8_t *exps, uint32_t exp_stride,
                                                            uint64_t code_stride, uint8_t *codes_t, uint8_t *exps_t, uint32_t exp_stride_t, uint64_t code_stride_t) {
+    const uint32_t across = (uint32_t)(code_stride / kBlockCols), tile_row = blockIdx.x / across, tile_col = blockIdx.x - tile_row * across;
     constexpr int kPitch = kBlockCols + 8;   // bytes per column of the tile in LDS: rows of codes in eights
     __shared__ __align__(16) uint8_t turned[kBlockCols * kPitch];
     __shared__ uint32_t most[kWaves];
-    const uint32_t r0 = blockIdx.y * kBlockCols, c0 = blockIdx.x * kBlockCols, col = c0 + (threadIdx.x & 15) * kChunkCols;
+    const uint32_t r0 = tile_row * kBlockCols, c0 = tile_col * kBlockCols, col = c0 + (threadIdx.x & 15) * kChunkCols;
     Chunk<T> next[8];
     float v[8][8];
 #pragma unroll
@@ -118,8 +119,8 @@ __global__ __launch_bounds__(kBlock) void k_quantize_tiles(const T *w, uint64_t 
             for (int j = 0; j < 8; ++j) turned[((threadIdx.x & 15) * 8 + j) * kPitch + r] = (uint8_t)(c[j / 4] >> (8 * (j % 4)));
     }
     if (threadIdx.x == 0) {
-        exps[(uint64_t)blockIdx.y * exp_stride + blockIdx.x] = (uint8_t)e;
-        if (codes_t) exps_t[(uint64_t)blockIdx.x * exp_stride_t + blockIdx.y] = (uint8_t)e;
+        exps[(uint64_t)tile_row * exp_stride + tile_col] = (uint8_t)e;
+        if (codes_t) exps_t[(uint64_t)tile_col * exp_stride_t + tile_row] = (uint8_t)e;
     }
     if (!codes_t) return;
     __syncthreads();
@@ -272,7 +273,7 @@ void launch_dequantize(const uint8_t *codes, const uint8_t *exps, bool tiles, ui
 
 void launch_quantize_tiles(const void *w, lgc_type type, uint32_t rows, uint32_t cols, uint64_t ld, uint8_t *codes, uint8_t *exps, uint8_t *codes_t, uint8_t *exps_t,
                            hipStream_t st) {
-    const dim3 grid((uint32_t)block_count(cols), (uint32_t)block_count(rows));
+    const uint32_t grid = (uint32_t)(block_count(cols) * block_count(rows));
     with_type(type, [&](auto *t) {
         typedef std::remove_pointer_t<decltype(t)> T;
         k_quantize_tiles<T><<<grid, kBlock, 0, st>>>((const T *)w, ld, rows, cols, codes, exps, (uint32_t)exps_stride(cols), codes_stride(cols), codes_t, exps_t,

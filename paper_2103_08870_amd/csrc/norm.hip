@@ -355,13 +355,17 @@ __global__ __launch_bounds__(64 * kColumns) void k_norm_columns(const float *par
 constexpr uint32_t kMostBlocks = 1u << 20;   // of a launch; a block goes on with later rows
 constexpr uint32_t kLongNorm = 16384, kLongGrad = 16384;   // columns from which on registers do not hold a row
 
+// Threads per row: as few as keep a row in registers, with 16 columns each (us, and what was tried beside it, 8 bits to: 32768 x 1024 20.6, 128 threads of 8 columns
+// 36.6; 8192 x 4096 22.0, 512 of 8 25.9, 128 of 32 32.5; 4096 x 8192 24.7, 1024 of 8 35.1, 256 of 32 28.7; 2048 x 16384 30.5, 512 of 32 34.0, rows read three times 43.9).
+// Up to 2048 columns there are twice as many for few rows (64 x 2048 3.0 / 3.5; 2000 x 2048 5.9 / 5.8; 16384 x 2048 26.0 / 22.9; 32768 x 1500 56.2 / 47.0).
 template <typename T>
-void norm_of(const NormArgs &a, uint32_t blocks, hipStream_t st) {
+void norm_of(const NormArgs &a, uint32_t blocks, bool many, hipStream_t st) {
 #define NORM(kThreads, kChunks) k_norm<T, kThreads, kChunks><<<std::min(kThreads == 64 ? (a.rows + kWaves - 1) / kWaves : a.rows, blocks), kThreads == 64 ? kBlock : kThreads, 0, st>>>(a)
     const uint32_t c = a.cols;
     if (c <= 512) NORM(64, 1);
     else if (c <= 1024) NORM(64, 2);
-    else if (c <= 2048) NORM(256, 1);
+    else if (c <= 2048 && !many) NORM(256, 1);
+    else if (c <= 2048) NORM(128, 2);
     else if (c <= 4096) NORM(256, 2);
     else if (c <= 8192) NORM(512, 2);
     else if (c <= kLongNorm) NORM(1024, 2);
@@ -369,6 +373,8 @@ void norm_of(const NormArgs &a, uint32_t blocks, hipStream_t st) {
 #undef NORM
 }
 
+// Threads per row: with 8 columns each, which leaves registers for the columns' sums and the next row (us, and half as many threads of 16: 32768 x 1024 42.9 / 45.8,
+// 16384 x 2048 41.9 / 42.8, 8192 x 4096 41.5 / 43.0, 4096 x 8192 50.9 / 52.1, 2048 x 16384 (16 and 32) 60.0 / 76.7, rows read twice 98.4; 64 x 1024 5.3 / 8.2)
 template <typename T>
 void norm_grad_of(const NormGradArgs &a, uint32_t blocks, hipStream_t st) {
 #define GRAD(kThreads, kChunks) k_norm_grad<T, kThreads, kChunks><<<blocks, kThreads == 64 ? kBlock : kThreads, 0, st>>>(a)
@@ -392,8 +398,9 @@ void launch_norm(const void *x, lgc_type type, uint32_t rows, uint32_t cols, uin
                  float *mean, float *rstd, uint8_t *codes, uint8_t *exps, int cus, hipStream_t st) {
     const uint32_t blocks = (uint32_t)cus * (cols <= 1024 || cols > 4096 ? 4 : 8);   // about as many as are resident
     const NormArgs a{x, ld, rows, cols, gamma, beta, eps, y, ld_y, mean, rstd, codes, exps, codes_stride(cols), (uint32_t)exps_stride(cols)};
-    if (type == LGC_FP32) norm_of<float>(a, blocks, st);
-    else norm_of<Bf16>(a, blocks, st);
+    const bool many = rows >= 32 * (uint32_t)cus;
+    if (type == LGC_FP32) norm_of<float>(a, blocks, many, st);
+    else norm_of<Bf16>(a, blocks, many, st);
 }
 
 void launch_norm_grad(const void *dy, uint64_t ld_dy, const void *x, uint64_t ld, lgc_type type, uint32_t rows, uint32_t cols, const float *gamma, const float *mean,

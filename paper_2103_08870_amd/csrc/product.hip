@@ -250,12 +250,10 @@ __global__ __launch_bounds__(64 * kWavesM * kWavesN) void k_product(ProductArgs 
         }
 }
 
-constexpr int kFew = 8;   // wavefronts that share 16 or 32 rows of B
-
 // Few rows of A (16 kM at most): the time is that of reading B once, so B goes from memory to registers, whole lines of 128 bytes, with no LDS and nothing
-// to wait for together.  A block has 16 kN rows of B; its wavefronts take groups of four blocks of 128 columns in turn, a group's loads all at once, and their
+// to wait for together.  A block has 16 kN rows of B; its kFew wavefronts take groups of four blocks of 128 columns in turn, a group's loads all at once, and their
 // sums meet in LDS.
-template <typename T, int kM, int kN, bool kExact>
+template <typename T, int kM, int kN, int kFew, bool kExact>
 __global__ __launch_bounds__(64 * kFew) void k_product_few(ProductArgs p) {
     __shared__ __align__(16) f4 part[kFew][kM * kN][64];
     const uint32_t n0 = blockIdx.x * 16 * kN, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), r = lane & 15, g = lane >> 4;
@@ -368,29 +366,38 @@ void launch_product(const uint8_t *a, const uint8_t *a_exps, const uint8_t *b, c
         if (type == LGC_FP32) k_join<float><<<grid, kBlock, 0, st>>>(scratch, (uint32_t)parts, m, n, divide_by(chunks), bias, (float *)y, ld);
         else k_join<Bf16><<<grid, kBlock, 0, st>>>(scratch, (uint32_t)parts, m, n, divide_by(chunks), bias, (Bf16 *)y, ld);
     };
-    if (m <= 64) {
-        auto few = [&](auto rows, auto cols) {
-            constexpr int kM = decltype(rows)::value, kN = decltype(cols)::value;
+    // 32 rows of B per block, whose reads of A are half as many, where that leaves a block per compute unit (us, 16 / 32 rows: 16 x 16384 x 4096 18.3 / 14.3,
+    // 64 x 8192 x 4096 22.6 / 15.4, 16 x 4096 x 4096 6.1 / 7.8, 64 x 4096 x 4096 12.5 / 14.0)
+    const bool wide = n / 32 >= (uint32_t)cus;
+    // Every block reads all of A, from an L2: tiles are faster for over 32 rows where that is 64 MB and more (us, few rows / tiles: 48 x 8192 x 4096 13.8 / 15.5,
+    // 64 x 1024 x 1024 5.0 / 6.7, 64 x 4096 x 4096 12.7 / 13.4, 64 x 8192 x 4096 15.4 / 15.0, 64 x 2048 x 16384 25.9 / 17.7, 64 x 12000 x 4096 26.1 / 19.4), and not
+    // before (32 x 16384 x 4096 18.8 / 22.4, 32 x 8192 x 8192 22.3 / 22.7)
+    if (m <= 32 || (m <= 64 && (uint64_t)(n / (wide ? 32 : 16)) * m * k < 1u << 26)) {
+        auto few = [&](auto rows, auto cols, auto team) {
+            constexpr int kM = decltype(rows)::value, kN = decltype(cols)::value, kFew = decltype(team)::value;
             const uint32_t own = (n + 16 * kN - 1) / (16 * kN);
             split(own < (uint32_t)cus ? std::min<uint64_t>(2 * cus / own, blocks / (4 * kFew)) : 1);
             const dim3 grid(own, (uint32_t)parts);
-            if (type == LGC_FP32) k_product_few<float, kM, kN, true><<<grid, 64 * kFew, 0, st>>>(p);
-            else if (parts > 1) k_product_few<float, kM, kN, false><<<grid, 64 * kFew, 0, st>>>(p);
-            else k_product_few<Bf16, kM, kN, false><<<grid, 64 * kFew, 0, st>>>(p);
+            if (type == LGC_FP32) k_product_few<float, kM, kN, kFew, true><<<grid, 64 * kFew, 0, st>>>(p);
+            else if (parts > 1) k_product_few<float, kM, kN, kFew, false><<<grid, 64 * kFew, 0, st>>>(p);
+            else k_product_few<Bf16, kM, kN, kFew, false><<<grid, 64 * kFew, 0, st>>>(p);
             join();
         };
         typedef std::integral_constant<int, 1> One;
         typedef std::integral_constant<int, 2> Two;
         typedef std::integral_constant<int, 4> Four;
-        // 32 rows of B per block, whose reads of A are half as many, where that leaves a block per compute unit (us, 16 / 32 rows: 16 x 8192 x 4096 10.1 / 8.2,
-        // 64 x 8192 x 4096 22.0 / 15.1, 16 x 4096 x 4096 6.1 / 7.8, 64 x 4096 x 4096 12.5 / 14.0)
-        const bool wide = n / 32 >= (uint32_t)cus;
-        if (m <= 16) wide ? few(One(), Two()) : few(One(), One());
-        else if (m <= 32) wide ? few(Two(), Two()) : few(Two(), One());
-        else wide ? few(Four(), Two()) : few(Four(), One());
+        typedef std::integral_constant<int, 8> Eight;
+        typedef std::integral_constant<int, 16> Sixteen;
+        // sixteen wavefronts for long rows, so that each has loads under way while others multiply (us, 8 / 16: 1 x 8192 x 8192 19.0 / 12.2, 16 x 16384 x 8192
+        // 36.3 / 29.6, 16 x 16384 x 16384 63 / 60, 16 x 16384 x 4096 14.3 / 14.5)
+        if (m <= 16) wide && k >= 8192 ? few(One(), Two(), Sixteen()) : wide ? few(One(), Two(), Eight()) : few(One(), One(), Eight());
+        else if (m <= 32) wide ? few(Two(), Two(), Eight()) : few(Two(), One(), Eight());
+        else wide ? few(Four(), Two(), Eight()) : few(Four(), One(), Eight());
         return;
     }
-    const bool large = type == LGC_BF16 && tiles(256) >= (uint64_t)cus;
+    // Large tiles where small ones would not all be resident, two per compute unit (us, small / large: 2048 x 4096 x 4096 36 / 50, 2304 x 4096 x 4096 56 / 46,
+    // 4096 x 4864 x 4096 103 / 99, 4096 x 5632 x 4096 97 / 99, 8192 x 16384 x 4096 546 / 443)
+    const bool large = type == LGC_BF16 && tiles(128) > 2 * (uint64_t)cus;
     const uint32_t side = large ? 256 : 128;
     // Few tiles: the sum over k in parts, a block per compute unit, of 8 blocks of columns at least; two per compute unit where each keeps 32: the parts' sums go to
     // memory and back (us with up to one / two: 2048 x 2048 x 2048 15.0 / 24.0, 1000 x 2500 x 1777 13.0 / 21.1, 512 x 4096 x 16384 52.3 / 46.2)

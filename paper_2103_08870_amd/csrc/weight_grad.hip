@@ -349,7 +349,7 @@ __global__ __launch_bounds__(kBlock) void k_weight_grad_small(WeightGradArgs p) 
 __global__ __launch_bounds__(kBlock) void k_add_parts(const float *part, uint32_t parts, uint64_t stride, float *dw, uint64_t count_w, float *db, uint64_t count) {
     __shared__ f4 sums[kWaves][64];
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x / 64;
-    const uint64_t at = ((uint64_t)blockIdx.x * 64 + lane) * 4;
+    const uint64_t at = (((uint64_t)blockIdx.y * gridDim.x + blockIdx.x) * 64 + lane) * 4;
     f4 s = {0, 0, 0, 0};
     if (at + 4 <= count) {
 #pragma unroll 4
@@ -376,10 +376,11 @@ __global__ __launch_bounds__(kBlock) void k_add_parts(const float *part, uint32_
 void launch_weight_grad(const void *dy, lgc_type type, uint32_t rows, uint32_t n, uint64_t ld, const uint8_t *codes, const uint8_t *exps, uint32_t k, float *dw, float *db,
                         float *scratch, size_t scratch_floats, int cus, hipStream_t st) {
     const uint64_t count_w = (uint64_t)n * k, count = count_w + (db ? n : 0);
-    const uint32_t adds = (uint32_t)((count + 255) / 256);
+    const uint32_t adds = (uint32_t)((count + 255) / 256), most = 1u << 20;   // (most: threads of a launch's dimension are counted in 32 bits)
+    const dim3 add_grid(std::min(adds, most), (adds + most - 1) / most);
     WeightGradArgs p{dy, ld, codes, exps, rows, n, k, (uint32_t)exps_stride(k), codes_stride(k), 0, 0, rows, dw, db, count};
     if (rows == 0) {
-        k_add_parts<<<adds, kBlock, 0, st>>>(nullptr, 0, 0, dw, count_w, db, count);
+        k_add_parts<<<add_grid, kBlock, 0, st>>>(nullptr, 0, 0, dw, count_w, db, count);
         return;
     }
     if ((uint64_t)(rows - 1) * ld + n < 8) {
@@ -389,10 +390,12 @@ void launch_weight_grad(const void *dy, lgc_type type, uint32_t rows, uint32_t n
         return;
     }
     auto tiles = [&](uint32_t side) { return (uint64_t)((n + side - 1) / side) * ((k + side - 1) / side); };
-    // Large tiles for a block per compute unit at least, and for rows that make the products last longer than a tile's stores, during which a block that has a compute
-    // unit for itself multiplies nothing (us, small / large tiles: 32 x 8192 x 8192 52 / 77, 400 x 8192 x 8192 119 / 134, 800 x 8192 x 8192 171 / 167,
-    // 8192 x 4096 x 16384 1216 / 960)
-    const bool large = type == LGC_BF16 && rows > 512 && tiles(256) >= (uint64_t)cus;
+    // Large tiles where they leave no more than a third of the compute units idle, taken over all rounds of a tile per unit (us, small / large, 4096 rows:
+    // 2816 x 4096 132 / 135, 3000 x 4096 158 / 144, 4096 x 4864 211 / 237, 4096 x 5632 256 / 243; 8192 x 4096 x 16384 1216 / 960), and for rows that make the products last
+    // longer than a tile's stores, during which a block that has a compute unit for itself multiplies nothing (32 x 8192 x 8192 52 / 77, 400 x 8192 x 8192 119 / 134,
+    // 600 x 4096 x 5632 56 / 69, 1000 x 3000 x 4096 43 / 49, 800 x 8192 x 8192 171 / 167, 2000 x 4096 x 5632 132 / 142)
+    const uint64_t rounds = (tiles(256) + cus - 1) / cus;
+    const bool large = type == LGC_BF16 && rows > 1024 && 3 * tiles(256) >= 2 * rounds * (uint64_t)cus;
     const uint32_t side = large ? 256 : 128;
     // Few tiles: the rows in parts, a block per compute unit at most and 512 rows at least: the parts' sums go to memory and back, eight bytes per weight and part
     // (us with up to one / two blocks per compute unit: 3001 x 768 x 1280 21.7 / 22.8, 2048 x 2048 x 2048 28 / 40, 8192 x 1024 x 1024 33 / 37; with 256 rows at least:
@@ -414,7 +417,7 @@ void launch_weight_grad(const void *dy, lgc_type type, uint32_t rows, uint32_t n
     else if (large) k_weight_grad<Bf16, 128, 1><<<grid, kBlock, 0, st>>>(p);
     else if (tiles(side) * parts > (uint64_t)cus) k_weight_grad<Bf16, 64, 1><<<grid, kBlock, 0, st>>>(p);   // (two blocks share a compute unit)
     else k_weight_grad<Bf16, 64, 2><<<grid, 2 * kBlock, 0, st>>>(p);
-    if (parts > 1) k_add_parts<<<adds, kBlock, 0, st>>>(scratch, (uint32_t)parts, count, dw, count_w, db, count);
+    if (parts > 1) k_add_parts<<<add_grid, kBlock, 0, st>>>(scratch, (uint32_t)parts, count, dw, count_w, db, count);
 }
 
 }  // namespace lgc

@@ -89,3 +89,31 @@ def test_weight_grad(B, ctx, rows, n, k, dtype):
         alone = torch.empty((n, k), device="cuda")
         B.lgc_weight_grad(ctx, dy, x, alone)
         assert torch.equal(alone, dw[:n])
+
+
+# Sixteen wavefronts for few long rows; over 32 rows that tiles serve; large tiles that a third of the compute units has none of
+@pytest.mark.parametrize("m,n,k", [(1, 8200, 8192), (13, 8321, 8300), (60, 2100, 16000), (50, 12100, 2500), (2900, 3000, 200)])
+def test_product_between_kernels(B, ctx, m, n, k):
+    test_product(B, ctx, m, n, k, torch.bfloat16)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,cols", [(8200, 1500), (8193, 2048), (8192, 1025), (9000, 700)])
+def test_layer_norm_of_many_rows(B, ctx, rows, cols, dtype):
+    x = (rand((rows, cols), rows, 2.0) + 1.0).to(dtype).cuda()
+    gamma, beta = rand((cols,), 1).cuda(), rand((cols,), 2).cuda()
+    y, y8, mean, rstd = torch.empty_like(x), B.Blocks(rows, cols), torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+    B.lgc_layer_norm(ctx, x, gamma, beta, 1e-5, y=y, blocks=y8, mean=mean, rstd=rstd)
+    d = x.double()
+    mu = d.mean(1)
+    r = ((d - mu[:, None]).square().mean(1) + 1e-5).rsqrt()
+    want = (d - mu[:, None]) * r[:, None] * gamma.double() + beta.double()
+    # sums of cols numbers about 2 in size, whose mean is off by cols / 4 units at most and their squares' by as much again
+    close = cols * U
+    assert ((mean.double() - mu).abs() <= close * d.abs().mean(1)).all() and ((rstd.double() - r).abs() <= close * r).all()
+    bound = 4 * close * (1 + want.abs() + gamma.abs().double())
+    assert ((y.double() - want).abs() <= bound + STORE[dtype] * want.abs()).all()
+    out = torch.empty((rows, cols), device="cuda")
+    B.lgc_dequantize(ctx, y8, out)
+    most = torch.nn.functional.pad(want.abs(), (0, -cols % 128)).view(rows, -1, 128).amax(2).repeat_interleave(128, 1)[:, :cols]
+    assert ((out.double() - want).abs() <= bound + want.abs() / 16 + most * 2.0 ** -17).all()   # half a unit of 3 bits; below them, half of 2^-9 of 2^-7 of the largest
