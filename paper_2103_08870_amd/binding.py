@@ -157,12 +157,13 @@ def _ptr(t: Optional[torch.Tensor], dtype=None) -> Optional[int]:
 # torch's own short way to the current stream's handle, where this torch has it: building a Stream object to ask for the
 # handle costs 2.8 us per call, as much as a kernel launch.
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
 def _stream() -> int:
     if _raw_stream is None:
         return torch.cuda.current_stream().cuda_stream
-    return _raw_stream(torch.cuda.current_device())
+    return _raw_stream(_device())
 
 
 def _require(cond: bool, what: str) -> None:
@@ -451,20 +452,35 @@ def lgc_profile_read(ctx: Context) -> Tuple[float, int]:
 _TYPES = {torch.float32: LGC_FP32, torch.bfloat16: LGC_BF16}
 _ACTS = {"relu": LGC_RELU, "gelu": LGC_GELU, "silu": LGC_SILU}
 _NONE = None, None
+_FP32 = torch.float32
 
 
 def _refuse(what: str):
     raise ValueError(f"liblgc binding: {what}")
 
 
-def _matrix(t: Optional[torch.Tensor], shape, dtype, what: str):
+# (The calls below are short: what checks their arguments counts, by the tenth of a microsecond an attribute of a tensor, so each is asked for once.)
+
+def _own(t: torch.Tensor, what: str):
+    """(type, rows, columns, pointer, elements from row to row) of the plain matrix that gives a call its sizes."""
+    kind, shape = _TYPES.get(t.dtype), t.shape
+    if kind is None or len(shape) != 2:
+        _refuse(f"{what} must be a matrix of float32 or bfloat16")
+    rows, cols = shape
+    return kind, rows, cols, *_rows(t, rows, cols, what)
+
+
+def _matrix(t: Optional[torch.Tensor], rows: int, cols: int, dtype, what: str):
     """(pointer, elements from row to row) of a plain matrix, None: (None, 0)."""
     if t is None:
         return None, 0
-    if t.dim() != 2 or t.shape != shape or t.dtype is not dtype:
-        _refuse(f"{what} must be {tuple(shape)} of {dtype}")
+    if t.shape != (rows, cols) or t.dtype is not dtype:
+        _refuse(f"{what} must be {(rows, cols)} of {dtype}")
+    return _rows(t, rows, cols, what)
+
+
+def _rows(t: torch.Tensor, rows: int, cols: int, what: str):
     ld, step = t.stride()
-    rows, cols = shape
     if step != 1 and cols > 1 and rows:
         _refuse(f"{what} must have contiguous rows")
     if not t.is_cuda:
@@ -477,7 +493,7 @@ def _vector(t: Optional[torch.Tensor], n: int, what: str) -> Optional[int]:
         return None
     if t.numel() != n or not t.is_contiguous():
         _refuse(f"{what} must be contiguous with {n} elements")
-    return _ptr(t, torch.float32)
+    return _ptr(t, _FP32)
 
 
 def _blocks(b: Optional[Blocks], rows: int, cols: int, what: str, tiles: bool = False):
@@ -486,13 +502,6 @@ def _blocks(b: Optional[Blocks], rows: int, cols: int, what: str, tiles: bool = 
     if b.rows != rows or b.cols != cols or b.tiles != tiles:
         _refuse(f"{what} must be Blocks of {(rows, cols)} with an exponent per " + ("128 x 128" if tiles else "row and 128 columns"))
     return b.at
-
-
-def _type(t: torch.Tensor, what: str) -> int:
-    kind = _TYPES.get(t.dtype)
-    if kind is None or t.dim() != 2:
-        _refuse(f"{what} must be a matrix of float32 or bfloat16")
-    return kind
 
 
 def lgc_codes_stride(cols: int) -> int:
@@ -510,36 +519,32 @@ def lgc_reserve_training(ctx: Context) -> None:
 
 def lgc_quantize(ctx: Context, x: torch.Tensor, out: Blocks) -> None:
     """out <- x [rows][cols], an exponent per row and 128 columns."""
-    kind = _type(x, "x")
-    at, ld = _matrix(x, x.shape, x.dtype, "x")
-    codes, exps = _blocks(out, *x.shape, "out")
-    _check(lib().lgc_quantize(ctx.h, at, kind, x.shape[0], x.shape[1], ld, codes, exps, _stream()), ctx.h)
+    kind, rows, cols, at, ld = _own(x, "x")
+    codes, exps = _blocks(out, rows, cols, "out")
+    _check(lib().lgc_quantize(ctx.h, at, kind, rows, cols, ld, codes, exps, _stream()), ctx.h)
 
 
 def lgc_quantize_weights(ctx: Context, w: torch.Tensor, out: Blocks, transposed: Optional[Blocks] = None) -> None:
     """out <- w [rows][cols], transposed <- its transpose, an exponent per 128 x 128; the same numbers in both."""
-    kind = _type(w, "w")
-    at, ld = _matrix(w, w.shape, w.dtype, "w")
-    codes, exps = _blocks(out, *w.shape, "out", True)
-    codes_t, exps_t = _blocks(transposed, w.shape[1], w.shape[0], "transposed", True)
-    _check(lib().lgc_quantize_weights(ctx.h, at, kind, w.shape[0], w.shape[1], ld, codes, exps, codes_t, exps_t, _stream()), ctx.h)
+    kind, rows, cols, at, ld = _own(w, "w")
+    codes, exps = _blocks(out, rows, cols, "out", True)
+    codes_t, exps_t = _blocks(transposed, cols, rows, "transposed", True)
+    _check(lib().lgc_quantize_weights(ctx.h, at, kind, rows, cols, ld, codes, exps, codes_t, exps_t, _stream()), ctx.h)
 
 
 def lgc_dequantize(ctx: Context, blocks: Blocks, out: torch.Tensor) -> None:
     """out [rows][cols] <- the values of blocks, exactly."""
-    kind = _type(out, "out")
-    at, ld = _matrix(out, (blocks.rows, blocks.cols), out.dtype, "out")
-    _check(lib().lgc_dequantize(ctx.h, *blocks.at, 128 if blocks.tiles else 1, blocks.rows, blocks.cols, at, kind, ld, _stream()), ctx.h)
+    kind, rows, cols, at, ld = _own(out, "out")
+    codes, exps = _blocks(blocks, rows, cols, "blocks", blocks.tiles)
+    _check(lib().lgc_dequantize(ctx.h, codes, exps, 128 if blocks.tiles else 1, rows, cols, at, kind, ld, _stream()), ctx.h)
 
 
 def lgc_layer_norm(ctx: Context, x: torch.Tensor, gamma: Optional[torch.Tensor], beta: Optional[torch.Tensor], eps: float,
                    y: Optional[torch.Tensor] = None, mean: Optional[torch.Tensor] = None, rstd: Optional[torch.Tensor] = None,
                    blocks: Optional[Blocks] = None) -> None:
     """y, blocks (y in 8 bits), mean, rstd <- layer norm of the rows of x; what is None is left out."""
-    kind = _type(x, "x")
-    rows, cols = x.shape
-    at, ld = _matrix(x, x.shape, x.dtype, "x")
-    out, ld_y = _matrix(y, x.shape, x.dtype, "y")
+    kind, rows, cols, at, ld = _own(x, "x")
+    out, ld_y = _matrix(y, rows, cols, x.dtype, "y")
     codes, exps = _blocks(blocks, rows, cols, "blocks")
     _check(lib().lgc_layer_norm(ctx.h, at, kind, rows, cols, ld, _vector(gamma, cols, "gamma"), _vector(beta, cols, "beta"), eps, out, ld_y,
                                 _vector(mean, rows, "mean"), _vector(rstd, rows, "rstd"), codes, exps, _stream()), ctx.h)
@@ -548,11 +553,9 @@ def lgc_layer_norm(ctx: Context, x: torch.Tensor, gamma: Optional[torch.Tensor],
 def lgc_layer_norm_grad(ctx: Context, dy: torch.Tensor, x: torch.Tensor, gamma: Optional[torch.Tensor], mean: torch.Tensor, rstd: torch.Tensor,
                         dx: Optional[torch.Tensor] = None, dgamma: Optional[torch.Tensor] = None, dbeta: Optional[torch.Tensor] = None) -> None:
     """Gradients of lgc_layer_norm from its mean and rstd; what is None is left out."""
-    kind = _type(x, "x")
-    rows, cols = x.shape
-    at, ld = _matrix(x, x.shape, x.dtype, "x")
-    at_dy, ld_dy = _matrix(dy, x.shape, x.dtype, "dy")
-    at_dx, ld_dx = _matrix(dx, x.shape, x.dtype, "dx")
+    kind, rows, cols, at, ld = _own(x, "x")
+    at_dy, ld_dy = _matrix(dy, rows, cols, x.dtype, "dy")
+    at_dx, ld_dx = _matrix(dx, rows, cols, x.dtype, "dx")
     _check(lib().lgc_layer_norm_grad(ctx.h, at_dy, ld_dy, at, ld, kind, rows, cols, _vector(gamma, cols, "gamma"), _vector(mean, rows, "mean"),
                                      _vector(rstd, rows, "rstd"), at_dx, ld_dx, _vector(dgamma, cols, "dgamma"), _vector(dbeta, cols, "dbeta"),
                                      _stream()), ctx.h)
@@ -568,36 +571,31 @@ def _act(act) -> int:
 def lgc_activate(ctx: Context, act: str, a: torch.Tensor, z: Optional[torch.Tensor] = None, a_blocks: Optional[Blocks] = None,
                  z_blocks: Optional[Blocks] = None) -> None:
     """z, z_blocks (z in 8 bits), a_blocks (a in 8 bits, for lgc_activate_grad) <- f(a); act: "relu", "gelu" or "silu"."""
-    kind = _type(a, "a")
-    at, ld = _matrix(a, a.shape, a.dtype, "a")
-    out, ld_z = _matrix(z, a.shape, a.dtype, "z")
-    _check(lib().lgc_activate(ctx.h, _act(act), at, kind, a.shape[0], a.shape[1], ld, out, ld_z, *_blocks(a_blocks, *a.shape, "a_blocks"),
-                              *_blocks(z_blocks, *a.shape, "z_blocks"), _stream()), ctx.h)
+    kind, rows, cols, at, ld = _own(a, "a")
+    out, ld_z = _matrix(z, rows, cols, a.dtype, "z")
+    _check(lib().lgc_activate(ctx.h, _act(act), at, kind, rows, cols, ld, out, ld_z, *_blocks(a_blocks, rows, cols, "a_blocks"),
+                              *_blocks(z_blocks, rows, cols, "z_blocks"), _stream()), ctx.h)
 
 
 def lgc_activate_grad(ctx: Context, act: str, dz: torch.Tensor, a_blocks: Blocks, da: Optional[torch.Tensor] = None,
                       da_blocks: Optional[Blocks] = None) -> None:
     """da, da_blocks (da in 8 bits) <- dz f'(a), a as lgc_activate kept it."""
-    kind = _type(dz, "dz")
-    at, ld = _matrix(dz, dz.shape, dz.dtype, "dz")
-    out, ld_da = _matrix(da, dz.shape, dz.dtype, "da")
-    _check(lib().lgc_activate_grad(ctx.h, _act(act), at, kind, dz.shape[0], dz.shape[1], ld, *_blocks(a_blocks, *dz.shape, "a_blocks"), out, ld_da,
-                                   *_blocks(da_blocks, *dz.shape, "da_blocks"), _stream()), ctx.h)
+    kind, rows, cols, at, ld = _own(dz, "dz")
+    out, ld_da = _matrix(da, rows, cols, dz.dtype, "da")
+    _check(lib().lgc_activate_grad(ctx.h, _act(act), at, kind, rows, cols, ld, *_blocks(a_blocks, rows, cols, "a_blocks"), out, ld_da,
+                                   *_blocks(da_blocks, rows, cols, "da_blocks"), _stream()), ctx.h)
 
 
 def lgc_product(ctx: Context, a: Blocks, b: Blocks, bias: Optional[torch.Tensor], y: torch.Tensor) -> None:
     """y [m][n] <- a [m][k] b [n][k]^T + bias [n]; b with an exponent per 128 x 128."""
-    kind = _type(y, "y")
-    at, ld = _matrix(y, (a.rows, b.rows), y.dtype, "y")
-    a_codes, a_exps = _blocks(a, a.rows, a.cols, "a")
-    b_codes, b_exps = _blocks(b, b.rows, a.cols, "b", True)
-    _check(lib().lgc_product(ctx.h, a_codes, a_exps, a.rows, b_codes, b_exps, b.rows, a.cols, _vector(bias, b.rows, "bias"), at, kind, ld, _stream()), ctx.h)
+    kind, m, n, at, ld = _own(y, "y")
+    a_codes, a_exps = _blocks(a, m, a.cols, "a")
+    b_codes, b_exps = _blocks(b, n, a.cols, "b", True)
+    _check(lib().lgc_product(ctx.h, a_codes, a_exps, m, b_codes, b_exps, n, a.cols, _vector(bias, n, "bias"), at, kind, ld, _stream()), ctx.h)
 
 
 def lgc_weight_grad(ctx: Context, dy: torch.Tensor, x: Blocks, dw: torch.Tensor, db: Optional[torch.Tensor] = None) -> None:
     """dw [n][k] <- dy [rows][n]^T x [rows][k], db [n] <- the columns' sums of dy; dw anywhere in a flat fp32 gradient."""
-    kind = _type(dy, "dy")
-    rows, n = dy.shape
-    at, ld = _matrix(dy, dy.shape, dy.dtype, "dy")
+    kind, rows, n, at, ld = _own(dy, "dy")
     codes, exps = _blocks(x, rows, x.cols, "x")
     _check(lib().lgc_weight_grad(ctx.h, at, kind, rows, n, ld, codes, exps, x.cols, _vector(dw, n * x.cols, "dw"), _vector(db, n, "db"), _stream()), ctx.h)

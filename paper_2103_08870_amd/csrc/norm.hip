@@ -277,6 +277,118 @@ __global__ __launch_bounds__(kThreads == 64 ? kBlock : kThreads) void k_norm_gra
     }
 }
 
+// 16 sums over a wavefront's lanes of the same lane % kOn: each lane gives the lane kOn away one half of the sums that it still has, and takes on the other half; at
+// the end a lane has one of the 16, and lanes 16 kOn apart have the same.
+template <int kOn, int kHalf>
+__device__ __forceinline__ void halve(float (&sums)[16]) {
+    const bool up = threadIdx.x & kOn;
+    if constexpr (kHalf > 0)
+#pragma unroll
+        for (int j = 0; j < kHalf; ++j) {
+            const float give = up ? sums[j] : sums[j + kHalf], keep = up ? sums[j + kHalf] : sums[j];
+            sums[j] = keep + __shfl_xor(give, kOn);
+        }
+    else
+        sums[0] += __shfl_xor(sums[0], kOn);
+    if constexpr (kOn < 32) halve<2 * kOn, kHalf / 2>(sums);
+}
+
+// Few rows, in one launch: neither gradient needs the other's sums, since mean and rstd are given.  The first blocks take strips of columns, 64 bytes of a row wide,
+// over all rows (or over a part's: `parts` times as many blocks, whose sums k_norm_columns adds); the others take rows, kThreads threads each.  x and dy are read twice,
+// mostly from the caches.
+template <typename T, int kThreads, int kChunks>
+__global__ __launch_bounds__(kThreads < 512 ? 512 : kThreads) void k_norm_grad_few(NormGradArgs a, uint32_t strips, uint32_t parts, float *dgamma, float *dbeta) {
+    constexpr int kAll = kThreads < 512 ? 512 : kThreads, kLanes = 8 / sizeof(T), kAtOnce = 2;
+    __shared__ f2 tmp[kAll / 64];
+    __shared__ float sums_of[kAll / 64][kLanes][16];
+    const uint32_t wave = threadIdx.x / 64;
+    if (blockIdx.x < strips * parts) {
+        // blocks go to the eight XCDs in turn: neighbouring strips, which share lines, to the same
+        const uint32_t part = blockIdx.x / strips, id = blockIdx.x - part * strips, xcd = id & 7, strip = xcd * (strips >> 3) + min(xcd, strips & 7) + (id >> 3);
+        const uint32_t col = (strip * kLanes + threadIdx.x % kLanes) * 8, share = (a.rows + parts - 1) / parts, end = min(a.rows, (part + 1) * share);
+        float sums[16] = {};   // of dy h, of dy
+        for (uint32_t from = part * share + threadIdx.x / kLanes; from < end; from += kAtOnce * (kAll / kLanes)) {
+            Chunk<T> x[kAtOnce], dy[kAtOnce];
+            float mean[kAtOnce], rstd[kAtOnce];
+#pragma unroll
+            for (int i = 0; i < kAtOnce; ++i) {
+                const uint32_t row = min(from + i * (kAll / kLanes), a.rows - 1);
+                x[i] = fetch_chunk((const T *)a.x + row * a.ld, col, a.cols);
+                dy[i] = fetch_chunk((const T *)a.dy + row * a.ld_dy, col, a.cols);
+                mean[i] = a.mean[row];
+                rstd[i] = a.rstd[row];
+            }
+#pragma unroll
+            for (int i = 0; i < kAtOnce; ++i) {
+                if (from + i * (kAll / kLanes) >= end) break;
+                float h[8], d[8];
+                unpack(x[i], col, a.cols, h);
+                unpack(dy[i], col, a.cols, d);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    sums[j] = fmaf(d[j], (h[j] - mean[i]) * rstd[i], sums[j]);
+                    sums[8 + j] += d[j];
+                }
+            }
+        }
+        halve<kLanes, 8>(sums);
+        // lane: its bits from kLanes on, the lowest first, say which half, quarter, .. of the 16 it has
+        const uint32_t bits = (threadIdx.x & 63) / kLanes;
+        if (bits < 16) sums_of[wave][threadIdx.x % kLanes][(bits & 1) * 8 + (bits >> 1 & 1) * 4 + (bits >> 2 & 1) * 2 + (bits >> 3)] = sums[0];
+        __syncthreads();
+        if (threadIdx.x >= kLanes * 16) return;
+        const uint32_t lane = threadIdx.x / 16, j = threadIdx.x % 16, here = (strip * kLanes + lane) * 8 + j % 8;
+        float s = sums_of[0][lane][j], *out = j < 8 ? dgamma : dbeta;
+#pragma unroll
+        for (int i = 1; i < kAll / 64; ++i) s += sums_of[i][lane][j];
+        if (parts > 1) out = a.part + ((uint64_t)part * 2 + j / 8) * a.cols;
+        if (out && here < a.cols) out[here] = s;
+        return;
+    }
+    const uint32_t row = (blockIdx.x - strips * parts) * (kAll / kThreads) + threadIdx.x / kThreads, lane = threadIdx.x % kThreads, from = min(row, a.rows - 1);
+    const float mean = a.mean[from], rstd = a.rstd[from];
+    float h[kChunks][8], dy[kChunks][8], s1 = 0.f, s2 = 0.f;
+#pragma unroll
+    for (int c = 0; c < kChunks; ++c) {
+        const uint32_t col = (c * kThreads + lane) * 8;
+        load_chunk((const T *)a.x + from * a.ld, col, a.cols, h[c]);
+        load_chunk((const T *)a.dy + from * a.ld_dy, col, a.cols, dy[c]);
+    }
+#pragma unroll
+    for (int c = 0; c < kChunks; ++c) {
+        float g[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) g[i] = 1.f;
+        if (a.gamma) load_chunk(a.gamma, (c * kThreads + lane) * 8, a.cols, g);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            h[c][i] = (h[c][i] - mean) * rstd;
+            dy[c][i] *= g[i];
+            s1 += dy[c][i];
+            s2 = fmaf(dy[c][i], h[c][i], s2);
+        }
+    }
+    f2 s = {wave_sum(s1), wave_sum(s2)};
+    if constexpr (kThreads > 64) {
+        if ((threadIdx.x & 63) == 0) tmp[wave] = s;
+        __syncthreads();
+        const f2 *const mine = tmp + threadIdx.x / kThreads * (kThreads / 64);
+        s = mine[0];
+#pragma unroll
+        for (int i = 1; i < kThreads / 64; ++i) { s[0] += mine[i][0]; s[1] += mine[i][1]; }
+    }
+    if (row >= a.rows) return;
+    const float per = 1.f / (float)a.cols, c1 = s[0] * per, c2 = s[1] * per;
+#pragma unroll
+    for (int c = 0; c < kChunks; ++c) {
+        const uint32_t col = (c * kThreads + lane) * 8;
+        float d[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) d[i] = rstd * (dy[c][i] - c1 - h[c][i] * c2);
+        store_chunk((T *)a.dx + row * a.ld_dx + col, count_at(col, a.cols), d);
+    }
+}
+
 // Long rows: dx alone
 template <typename T>
 __global__ __launch_bounds__(1024) void k_norm_grad_long(NormGradArgs a) {
@@ -374,7 +486,7 @@ void norm_of(const NormArgs &a, uint32_t blocks, bool many, hipStream_t st) {
 }
 
 // Threads per row: with 8 columns each, which leaves registers for the columns' sums and the next row (us, and half as many threads of 16: 32768 x 1024 42.9 / 45.8,
-// 16384 x 2048 41.9 / 42.8, 8192 x 4096 41.5 / 43.0, 4096 x 8192 50.9 / 52.1, 2048 x 16384 (16 and 32) 60.0 / 76.7, rows read twice 98.4; 64 x 1024 5.3 / 8.2)
+// 16384 x 2048 41.9 / 42.8, 8192 x 4096 41.5 / 43.0, 4096 x 8192 50.9 / 52.1, 2048 x 16384 (16 and 32) 60.0 / 76.7, rows read twice 98.4)
 template <typename T>
 void norm_grad_of(const NormGradArgs &a, uint32_t blocks, hipStream_t st) {
 #define GRAD(kThreads, kChunks) k_norm_grad<T, kThreads, kChunks><<<blocks, kThreads == 64 ? kBlock : kThreads, 0, st>>>(a)
@@ -392,6 +504,20 @@ void norm_grad_of(const NormGradArgs &a, uint32_t blocks, hipStream_t st) {
 #undef GRAD
 }
 
+template <typename T>
+void norm_grad_few(const NormGradArgs &a, uint32_t parts, float *dgamma, float *dbeta, hipStream_t st) {
+    const uint32_t c = a.cols, strips = dgamma || dbeta ? (c + 64 / sizeof(T) - 1) / (64 / sizeof(T)) : 0;
+    auto blocks = [&](uint32_t threads) { return strips * parts + (a.dx ? threads < 512 ? (a.rows + 512 / threads - 1) / (512 / threads) : a.rows : 0); };
+#define FEW(kThreads, kChunks) k_norm_grad_few<T, kThreads, kChunks><<<blocks(kThreads), kThreads < 512 ? 512 : kThreads, 0, st>>>(a, strips, parts, dgamma, dbeta)
+    if (c <= 512) FEW(64, 1);
+    else if (c <= 1024) FEW(128, 1);
+    else if (c <= 2048) FEW(256, 1);
+    else if (c <= 4096) FEW(512, 1);
+    else if (c <= 8192) FEW(1024, 1);
+    else FEW(1024, 2);
+#undef FEW
+}
+
 }  // namespace
 
 void launch_norm(const void *x, lgc_type type, uint32_t rows, uint32_t cols, uint64_t ld, const float *gamma, const float *beta, float eps, void *y, uint64_t ld_y,
@@ -405,6 +531,19 @@ void launch_norm(const void *x, lgc_type type, uint32_t rows, uint32_t cols, uin
 
 void launch_norm_grad(const void *dy, uint64_t ld_dy, const void *x, uint64_t ld, lgc_type type, uint32_t rows, uint32_t cols, const float *gamma, const float *mean,
                       const float *rstd, void *dx, uint64_t ld_dx, float *dgamma, float *dbeta, float *scratch, size_t scratch_floats, int cus, hipStream_t st) {
+    // us, rows by blocks that go on / few rows: 64 x 1111 5.9 / 3.2, 512 x 300 7.3 / 4.4, 1024 x 4096 14.4 / 9.4, 1024 x 16384 36.9 / 28.8, 2047 x 1111 14.8 / 12.6,
+    // 2047 x 4096 20.4 / 15.2, 4096 x 300 10.2 / 8.1, 4096 x 1111 19.3 / 19.4, 4096 x 4096 24.8 / 26.8, 2047 x 16384 60 / 68
+    if (rows && (dx || dgamma || dbeta) && cols <= kLongGrad && (rows <= 1024 || (rows <= 4096 && rows * cols <= 9u << 20))) {
+        // Strips enough for half of the compute units, where they are long enough for a second launch (one / two parts: 1024 x 1111 9.4 / 9.6, 2047 x 1111 14.6 / 12.6;
+        // one / eight: 512 x 300 4.4 / 5.3, 4096 x 300 22.4 / 8.1)
+        const uint32_t strips = (cols + 64 / (type == LGC_FP32 ? 4 : 2) - 1) / (64 / (type == LGC_FP32 ? 4 : 2));
+        const uint32_t parts = rows <= 1024 || !(dgamma || dbeta) ? 1 : std::min(((uint32_t)cus / 2 + strips - 1) / strips, 8u);
+        const NormGradArgs a{dy, x, ld_dy, ld, rows, cols, gamma, mean, rstd, dx, ld_dx, scratch};
+        if (type == LGC_FP32) norm_grad_few<float>(a, parts, dgamma, dbeta, st);
+        else norm_grad_few<Bf16>(a, parts, dgamma, dbeta, st);
+        if (parts > 1) k_norm_columns<<<dim3((cols + kColumns - 1) / kColumns, 2), 64 * kColumns, 0, st>>>(scratch, parts, cols, dgamma, dbeta);
+        return;
+    }
     const uint32_t rows_at_once = cols <= 512 ? kWaves : 1;
     uint32_t blocks = cols > kLongGrad ? 64 : (uint32_t)cus * (cols <= 2048 ? 4 : cols <= 8192 ? 2 : 1);
     blocks = std::min(blocks, std::max((uint32_t)cus, rows / (4 * rows_at_once)));

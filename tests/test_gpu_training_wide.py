@@ -117,3 +117,35 @@ def test_layer_norm_of_many_rows(B, ctx, rows, cols, dtype):
     B.lgc_dequantize(ctx, y8, out)
     most = torch.nn.functional.pad(want.abs(), (0, -cols % 128)).view(rows, -1, 128).amax(2).repeat_interleave(128, 1)[:, :cols]
     assert ((out.double() - want).abs() <= bound + want.abs() / 16 + most * 2.0 ** -17).all()   # half a unit of 3 bits; below them, half of 2^-9 of 2^-7 of the largest
+
+
+# Rows in one launch, with the columns' sums in parts, and by blocks that go on from row to row: either side of where one gives way to another
+NORM_GRADS = [(1024, 300), (1025, 300), (2047, 1111), (4096, 515), (4097, 515), (4099, 1000), (4101, 2000), (4097, 4000), (1025, 16000), (600, 16383), (1100, 8192), (4098, 40)]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,cols", NORM_GRADS)
+def test_layer_norm_grad_of_many_rows(B, ctx, rows, cols, dtype):
+    x, dy, gamma = (rand((rows, cols), rows, 2.0) + 1.0).to(dtype), rand((rows, cols), cols, 1e-2, dtype), rand((cols,), 1).cuda()
+    x, dy = x.cuda(), dy.cuda()
+    d = x.double()
+    mean, rstd = d.mean(1).float(), ((d - d.mean(1, keepdim=True)).square().mean(1) + 1e-5).rsqrt().float()
+    want, wg, wb = ref.layer_norm_grad(dy, x, gamma, mean, rstd)
+    dx, dg, db = torch.full_like(x, 9.0), torch.full((cols,), 9.0, device="cuda"), torch.full((cols,), 9.0, device="cuda")
+    B.lgc_layer_norm_grad(ctx, dy, x, gamma, mean, rstd, dx, dg, db)
+    r = rstd.double()[:, None]
+    hx = ((d - mean.double()[:, None]) * r).abs() + 2 * U * d.abs() * r
+    q = dy.double().abs() * gamma.double().abs()
+    # a row's sums: 16 additions in a thread and 10 among threads; the rest is a rounding or two of each factor
+    bound = r * (8 * U * q + 64 * U * (q.mean(1, keepdim=True) + hx * (q * hx).mean(1, keepdim=True))) + (STORE[dtype] + 4 * U) * want.abs() + 1e-30
+    assert ((dx.double() - want).abs() <= bound).all()
+    assert ((dg.double() - wg).abs() <= (rows + 40) * U * (dy.double().abs() * hx).sum(0) + 4 * U * (dy.double().abs() * d.abs() * r).sum(0)).all()
+    assert ((db.double() - wb).abs() <= (rows + 40) * U * dy.double().abs().sum(0)).all()
+    again = [torch.empty_like(t) for t in (dx, dg, db)]
+    B.lgc_layer_norm_grad(ctx, dy, x, gamma, mean, rstd, *again)
+    assert all(torch.equal(a, b) for a, b in zip(again, (dx, dg, db)))
+    alone = torch.empty_like(dg)
+    B.lgc_layer_norm_grad(ctx, dy, x, gamma, mean, rstd, dgamma=alone)
+    assert torch.equal(alone, dg)
+    B.lgc_layer_norm_grad(ctx, dy, x, gamma, mean, rstd, again[0].zero_())
+    assert torch.equal(again[0], dx)
