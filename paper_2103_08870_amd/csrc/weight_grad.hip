@@ -48,12 +48,6 @@ __device__ __forceinline__ void tile_of(uint32_t id, uint32_t tiles_n, uint32_t 
     tn = band * kBand + in - tk * high;
 }
 
-// The exponents of x differ along the sum, so its values meet the matrix cores as bf16, in which they are exact; dy in fp32 as three bf16 parts, which hold it exactly.
-// A tile of 2 kWave x 2 kWave per block, a quarter per wavefront, 64 rows of dy and x at a time.  Rows go through registers, loaded a step before, to one of two
-// places in LDS, and are turned as they are read from there: 16 lanes give the addresses of four rows of 16 columns and get a column of four rows each.  A step's
-// products come in four groups of 16 rows; between those of a group the next group's columns are read and the next step's rows are stored and the loads of the step
-// after it queued, in the order written here (there is one wavefront per SIMD, or two: nothing else would run while one of them does these alone).
-// LDS rows lie a multiple of 256 bytes apart; pieces of 32 bytes are exchanged within a row by (row & 3), so that these four rows meet all banks.
 constexpr int kSteps = 64;
 
 // f(0), f(1), .. f(N - 1), each with its number as a constant
@@ -62,23 +56,36 @@ __device__ __forceinline__ void each_of(std::integer_sequence<int, I...>, F &&f)
 template <int N, typename F>
 __device__ __forceinline__ void each(F &&f) { each_of(std::make_integer_sequence<int, N>(), f); }
 
-// kTeams teams of four wavefronts do this for a part of the block's rows each, and their sums meet in LDS: with small tiles, whose wavefronts wait for LDS half of
-// the time, two per SIMD are faster than one (8192 x 2048 x 2048: 99 us to 83).  Where there are blocks enough, two blocks of one team are that too, and one's products
-// run during the other's stores (3467 x 13081 x 512: 87 us to 76).
-template <typename T, int kWave, int kTeams>
-__global__ __launch_bounds__(kBlock * kTeams) void k_weight_grad(WeightGradArgs p) {
-    constexpr int kParts = sizeof(T) == 2 ? 1 : 3, kTile = 2 * kWave, kPitch = kTile * 2, kPlace = (kParts + 1) * kSteps * kPitch, kSide = kWave / 32;
-    constexpr int kChunks = kTile / 8, kRowsY = kBlock / kChunks, kPassY = kSteps / kRowsY;       // dy: eight columns per thread and pass
-    constexpr int kPieces = kTile / 16, kRowsX = kBlock / kPieces, kPassX = kSteps / kRowsX;      // x: sixteen codes
+// The exponents of x differ along the sum, so its values meet the matrix cores as bf16, in which they are exact; dy in fp32 as three bf16 parts, which hold it exactly.
+// A tile of 2 kWaveN columns of dy by as many of x per block, kWaveN by kWaveK per wavefront, 64 rows of dy and x at a time.  Rows go through registers, loaded a step before, to one of two
+// places in LDS, and are turned as they are read from there: 16 lanes give the addresses of four rows of 16 columns and get a column of four rows each.  A step's
+// products come in four groups of 16 rows; between those of a group the next group's columns are read and the next step's rows are stored and the loads of the step
+// after it queued, in the order written here.  A SIMD has two wavefronts, so that one's products run during the other's reads and stores (8192 x 4096 x 16384 with one of
+// 128 x 128: 940 us, with two of 128 x 64 890, though these read half as much again; 4096 cubed 142 and 125).
+// LDS rows lie a multiple of 256 bytes apart; pieces of 32 bytes are exchanged within a row by (row & 3), so that these four rows meet all banks.
+//
+// Bound by the matrix instructions and LDS where rows are many (8192 x 4096 x 16384, dy in bf16: 865 - 890 us, 1.25 PFLOP/s), by the stores of dw where they are few
+// (32 x 8192 x 8192: 46 us, 5.9 TB/s of dw), and between by the time that a tile's first rows take to come and its sums to leave (3001 x 777 x 1300: 22.3 us).
+//
+// kTeams teams of kTeam wavefronts do this for a part of the block's rows each, and their sums meet in LDS: with small tiles, two teams of four are those two wavefronts
+// per SIMD (8192 x 2048 x 2048: 99 us to 82).  Where there are blocks enough, two blocks of one team are that too, and one's products run during the other's stores
+// (3467 x 13081 x 512: 87 us to 74).
+template <typename T, int kWaveN, int kWaveK, int kTeam, int kTeams>
+__global__ __launch_bounds__(64 * kTeam * kTeams) void k_weight_grad(WeightGradArgs p) {
+    constexpr int kParts = sizeof(T) == 2 ? 1 : 3, kTile = 2 * kWaveN, kPitch = kTile * 2, kPlace = (kParts + 1) * kSteps * kPitch, kSideN = kWaveN / 32, kSideK = kWaveK / 32;
+    constexpr int kThreads = 64 * kTeam;
+    constexpr int kChunks = kTile / 8, kRowsY = kThreads / kChunks, kPassY = kSteps / kRowsY;       // dy: eight columns per thread and pass
+    constexpr int kPieces = kTile / 16, kRowsX = kThreads / kPieces, kPassX = kSteps / kRowsX;      // x: sixteen codes
+    static_assert(kTeam / 2 * kWaveK == kTile, "square tiles");
     __shared__ __align__(16) uint8_t every[kTeams * 2 * kPlace];
-    const uint32_t tid = threadIdx.x % kBlock, team = __builtin_amdgcn_readfirstlane(threadIdx.x / kBlock);
+    const uint32_t tid = threadIdx.x % kThreads, team = __builtin_amdgcn_readfirstlane(threadIdx.x / kThreads);
     uint8_t *const lds = every + team * (2 * kPlace);
     uint32_t tn, tk;
     tile_of(blockIdx.x, p.tiles_n, p.tiles_k, tn, tk);
     const uint32_t n0 = tn * kTile, k0 = tk * kTile;
     const bool sums = p.db && tk == 0;
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(tid / 64);
-    const uint32_t wn = (wave & 1) * kWave, wk = (wave >> 1) * kWave;
+    const uint32_t wn = (wave & 1) * kWaveN, wk = (wave >> 1) * kWaveK;
     // the team's rows: whole steps of the part's, as many for each; the last team's may end, or lie, past the part's end
     const uint32_t begin = blockIdx.y * p.share, end = min(begin + p.share, p.rows), steps = (end - begin + kTeams * kSteps - 1) / (kTeams * kSteps);
     const uint32_t t0 = begin + team * steps * kSteps, t1 = min(t0 + steps * kSteps, end), lag = (kTeams - 1 - team) * steps * kSteps;   // lag: to the last team's
@@ -98,11 +105,11 @@ __global__ __launch_bounds__(kBlock * kTeams) void k_weight_grad(WeightGradArgs 
         y_next[i][0] = *(const u4e *)at;
         if constexpr (kParts > 1) y_next[i][1] = *(const u4e *)(at + 4);
     };
-    // Inside, where all rows asked for exist: a place that goes on by a step's rows, and the passes' distances from it
-    const T *y_at_next = (const T *)p.dy + (uint64_t)(t0 + 2 * kSteps + y_row) * p.ld + y_col;
-    const uint8_t *x_at_next = p.codes + (uint64_t)(t0 + 2 * kSteps + x_row) * p.code_stride + x_from;
-    const uint8_t *e_at_next = p.exps + (uint64_t)(t0 + 2 * kSteps + x_row) * p.exp_stride + x_from / kBlockCols;
-    auto store_y = [&](auto inside, int i, uint32_t place, uint32_t t) {
+    // Inside, where all rows asked for exist: a place for all lanes that goes on by a step's rows, and the lane's and pass's distances from it, in 32 bits
+    const uint8_t *y_from = (const uint8_t *)p.dy + ((uint64_t)(t0 + 2 * kSteps) * p.ld + n0) * sizeof(T);
+    const uint8_t *x_base = p.codes + (uint64_t)(t0 + 2 * kSteps) * p.code_stride, *e_base = p.exps + (uint64_t)(t0 + 2 * kSteps) * p.exp_stride;
+    uint32_t y_off = (uint32_t)((y_row * p.ld + y_chunk * 8) * sizeof(T)), x_off = x_row * (uint32_t)p.code_stride + x_from, e_off = x_row * p.exp_stride + x_from / kBlockCols;
+    auto store_y = [&](auto inside, auto sums, int i, uint32_t place, uint32_t t) {
         const uint32_t row = y_row + i * kRowsY, at = place * kPlace + row * kPitch + (y_chunk * 16 ^ (row & 3) * 64);
         const bool last = !decltype(inside)::value && (t + kSteps + 8 > p.rows || t + kSteps > t1);   // (the same for all)
         uint32_t beyond = 0;
@@ -143,115 +150,120 @@ __global__ __launch_bounds__(kBlock * kTeams) void k_weight_grad(WeightGradArgs 
             }
         }
     };
-    auto store_x = [&](auto inside, int i, uint32_t place, uint32_t t) {
+    auto store_x = [&](auto inside, int i, int half, uint32_t place, uint32_t t) {   // eight of the sixteen
         const uint32_t row = x_row + i * kRowsX, at = place * kPlace + kParts * kSteps * kPitch + row * kPitch + (x_piece * 32 ^ (row & 3) * 64);
         const float scale = exp_scale(e_next[i]);
-        u4 w[2], from = x_next[i];
-        if (!decltype(inside)::value && t + row >= t1) from = u4{0, 0, 0, 0};
+        u4 w;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const uint32_t c = from[j];
-            w[j / 2][j % 2 * 2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c, scale, false));
-            w[j / 2][j % 2 * 2 + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c, scale, true));
+        for (int j = 0; j < 2; ++j) {
+            const uint32_t c = !decltype(inside)::value && t + row >= t1 ? 0u : x_next[i][2 * half + j];
+            w[2 * j] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c, scale, false));
+            w[2 * j + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c, scale, true));
         }
-        *(u4 *)(lds + at) = w[0];
-        *(u4 *)(lds + at + 16) = w[1];
+        *(u4 *)(lds + at + 16 * half) = w;
     };
-    constexpr int kStaged = kPassY + kPassX;
+    // A step's staging in small pieces: stores, of dy's passes and of x's in halves, and as many loads
+    constexpr int kStaged = kPassY + 2 * kPassX;
+    auto store = [&](auto inside, auto sums, int i, uint32_t place, uint32_t t) {
+        if (i < kPassY) store_y(inside, sums, i, place, t);
+        else store_x(inside, (i - kPassY) / 2, (i - kPassY) % 2, place, t);
+    };
     auto load = [&](auto inside, int i, uint32_t t) {
-        if (i < kPassY) {
-            if constexpr (decltype(inside)::value) load_y_at(i, y_at_next + (uint64_t)(i * kRowsY) * p.ld);
-            else load_y_at(i, (const T *)p.dy + min(y_place(i, t), total - 8));
-        } else {
-            const int j = i - kPassY;
-            if constexpr (decltype(inside)::value) {
-                x_next[j] = *(const u4 *)(x_at_next + (uint64_t)(j * kRowsX) * p.code_stride);
-                e_next[j] = e_at_next[(uint64_t)(j * kRowsX) * p.exp_stride];
+        const int j = (i - kPassY) / 2;
+        if constexpr (decltype(inside)::value) {
+            // (an offset stays one register, which the load itself adds to a place for all lanes)
+            if (i < kPassY) {
+                asm("" : "+v"(y_off));
+                load_y_at(i, (const T *)(y_from + (uint64_t)(i * kRowsY) * p.ld * sizeof(T) + y_off));
+            } else if ((i - kPassY) % 2 == 0) {
+                asm("" : "+v"(x_off));
+                x_next[j] = *(const u4 *)(x_base + (uint64_t)(j * kRowsX) * p.code_stride + x_off);
             } else {
-                const uint64_t row = min(t + x_row + j * kRowsX, p.rows - 1);
-                x_next[j] = *(const u4 *)(p.codes + row * p.code_stride + x_from);
-                e_next[j] = p.exps[row * p.exp_stride + x_from / kBlockCols];
+                asm("" : "+v"(e_off));
+                e_next[j] = (e_base + (uint64_t)(j * kRowsX) * p.exp_stride)[e_off];
             }
+        } else if (i < kPassY) load_y_at(i, (const T *)p.dy + min(y_place(i, t), total - 8));
+        else {
+            const uint64_t row = min(t + x_row + j * kRowsX, p.rows - 1);
+            if ((i - kPassY) % 2 == 0) x_next[j] = *(const u4 *)(p.codes + row * p.code_stride + x_from);
+            else e_next[j] = p.exps[row * p.exp_stride + x_from / kBlockCols];
         }
     };
-    auto store = [&](auto inside, int i, uint32_t place, uint32_t t) {
-        if (i < kPassY) store_y(inside, i, place, t);
-        else store_x(inside, i - kPassY, place, t);
+
+    // all of it in an order in which a load comes right after the store from its registers
+    constexpr int kSlots = 2 * kStaged;
+    auto stage = [&](auto inside, auto sums, int i, uint32_t to, uint32_t t) {
+        const int j = i < 2 * kPassY ? i / 2 : kPassY + (i - 2 * kPassY) / 4 * 2 + i % 2;
+        if (i < 2 * kPassY ? i % 2 == 0 : (i - 2 * kPassY) % 4 < 2) store(inside, sums, j, to, t + kSteps);
+        else load(inside, j, t + 2 * kSteps);
     };
 
     // 32 x 32 x 16: lane: column lane % 32, rows 8 (lane / 32) + 0 .. 7 of the 16
     const uint32_t r = lane & 15, t_lane = (lane >> 5) * 8 + (r >> 2);
-    uint32_t y_at[kSide], x_at[kSide];
+    uint32_t y_at[kSideN], x_at[kSideK];
 #pragma unroll
-    for (int i = 0; i < kSide; ++i) {
-        const uint32_t col = 32 * i + (lane >> 4 & 1) * 16;
-        y_at[i] = t_lane * kPitch + (((wn + col) * 2) ^ ((r >> 2) * 64)) + (r & 3) * 8;
-        x_at[i] = kParts * kSteps * kPitch + t_lane * kPitch + (((wk + col) * 2) ^ ((r >> 2) * 64)) + (r & 3) * 8;
-    }
+    for (int i = 0; i < kSideN; ++i) y_at[i] = t_lane * kPitch + (((wn + 32 * i + (lane >> 4 & 1) * 16) * 2) ^ ((r >> 2) * 64)) + (r & 3) * 8;
+#pragma unroll
+    for (int i = 0; i < kSideK; ++i) x_at[i] = kParts * kSteps * kPitch + t_lane * kPitch + (((wk + 32 * i + (lane >> 4 & 1) * 16) * 2) ^ ((r >> 2) * 64)) + (r & 3) * 8;
     auto column = [&](uint32_t at) {
         typedef __attribute__((address_space(3))) s4 *Lds;
         const s4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(lds + at)), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(lds + at + 4 * kPitch));
         return __builtin_bit_cast(bf8, s8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]});
     };
-    constexpr int kReads = kSide * (1 + kParts), kProducts = kSide * kSide * kParts;
-    bf8 x[2][kSide], y[2][kParts][kSide];
+    constexpr int kReads = kSideK + kSideN * kParts, kProducts = kSideN * kSideK * kParts;
+    bf8 x[2][kSideK], y[2][kParts][kSideN];
     auto read = [&](int set, uint32_t place, int group, int i) {
         const uint32_t from = place * kPlace + group * 16 * kPitch;
-        if (i < kSide) x[set][i] = column(from + x_at[i]);
-        else y[set][i / kSide - 1][i % kSide] = column(from + (i / kSide - 1) * kSteps * kPitch + y_at[i % kSide]);
+        if (i < kSideK) x[set][i] = column(from + x_at[i]);
+        else y[set][(i - kSideK) / kSideN][(i - kSideK) % kSideN] = column(from + (i - kSideK) / kSideN * kSteps * kPitch + y_at[(i - kSideK) % kSideN]);
     };
-    f16 acc[kSide][kSide] = {};
+    f16 acc[kSideN][kSideK] = {};
     auto product = [&](int set, int i) {   // the smallest parts first
-        const int part = kParts - 1 - i / (kSide * kSide), n = i / kSide % kSide, k = i % kSide;
+        const int part = kParts - 1 - i / (kSideN * kSideK), n = i / kSideK % kSideN, k = i % kSideK;
         acc[n][k] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[set][k], y[set][part][n], acc[n][k], 0, 0, 0);
     };
 
     each<kStaged>([&](auto i) { load(std::false_type(), i, t0); });
-    each<kStaged>([&](auto i) {
-        store(std::false_type(), i, 0, t0);
-        load(std::false_type(), i, t0 + kSteps);
-    });
+    each<kSlots>([&](auto i) { stage(std::false_type(), sums, i, 0, t0 - kSteps); });
     __syncthreads();
     each<kReads>([&](auto i) { read(0, 0, 0, i); });
     uint32_t t = t0, place = 0, left = steps;   // (what the loops go by is the same for all teams, as the barriers need)
     typedef std::true_type Inside;
     typedef std::false_type Outside;
     const uint32_t margin = p.ld >= kTile ? 1 : kTile;   // rows after which a whole row of the tile exists, however narrow dy is
+    auto inside = [&](auto sums) {
+        if (p.ld >= 1u << 24) return;   // (distances within a step pass 32 bits)
 #pragma clang loop unroll(disable)
-    for (; left >= 2 && (uint64_t)t + lag + 2 * kSteps <= end && (uint64_t)t + lag + 3 * kSteps + margin <= p.rows; t += kSteps, place ^= 1, --left) {
-        each<4>([&](auto group) {
-            if constexpr (group == 3) {   // the next step's rows are stored, and this one's read
-                asm volatile("" ::: "memory");
-                __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt(0)
-                __builtin_amdgcn_s_barrier();
-                asm volatile("" ::: "memory");
-            }
-            each<kProducts>([&](auto i) {
-                product(group & 1, i);
-                constexpr int kFrom = i * kReads / kProducts, kTo = (i + 1) * kReads / kProducts;
-                each<kTo - kFrom>([&](auto j) { read(~group & 1, group == 3 ? place ^ 1 : place, (group + 1) & 3, kFrom + j); });
-                if constexpr (group < 3) {
-                    constexpr int kBegin = (group * kProducts + i) * kStaged / (3 * kProducts), kEnd = (group * kProducts + i + 1) * kStaged / (3 * kProducts);
-                    each<kEnd - kBegin>([&](auto j) {
-                        store(Inside(), kBegin + j, place ^ 1, t + kSteps);
-                        load(Inside(), kBegin + j, t + 2 * kSteps);
-                    });
+        for (; left >= 2 && (uint64_t)t + lag + 2 * kSteps <= end && (uint64_t)t + lag + 3 * kSteps + margin <= p.rows; t += kSteps, place ^= 1, --left) {
+            each<4>([&](auto group) {
+                if constexpr (group == 3) {   // the next step's rows are stored, and this one's read
+                    asm volatile("" ::: "memory");
+                    __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt(0)
+                    __builtin_amdgcn_s_barrier();
+                    asm volatile("" ::: "memory");
                 }
-                __builtin_amdgcn_sched_barrier(0);
+                each<kProducts>([&](auto i) {
+                    product(group & 1, i);
+                    constexpr int kFrom = i * kReads / kProducts, kTo = (i + 1) * kReads / kProducts;
+                    each<kTo - kFrom>([&](auto j) { read(~group & 1, group == 3 ? place ^ 1 : place, (group + 1) & 3, kFrom + j); });
+                    if constexpr (group < 3) {
+                        constexpr int kAt = group * kProducts + i, kBegin = kAt * kSlots / (3 * kProducts), kEnd = (kAt + 1) * kSlots / (3 * kProducts);
+                        each<kEnd - kBegin>([&](auto j) { stage(Inside(), sums, kBegin + j, place ^ 1, t); });
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                });
             });
-        });
-        y_at_next += (uint64_t)kSteps * p.ld;
-        x_at_next += (uint64_t)kSteps * p.code_stride;
-        e_at_next += (uint64_t)kSteps * p.exp_stride;
-    }
+            y_from += (uint64_t)kSteps * p.ld * sizeof(T);
+            x_base += (uint64_t)kSteps * p.code_stride;
+            e_base += (uint64_t)kSteps * p.exp_stride;
+        }
+    };
+    inside(sums);
     // the last steps, one thing after the other (past the end: rows that exist, and zeros in their place)
 #pragma clang loop unroll(disable)
     for (; left; t += kSteps, place ^= 1, --left) {
-        if (kWave > 64 || left > 1)   // (for the large tile, whose registers are full, without a branch)
-            each<kStaged>([&](auto i) {
-                store(Outside(), i, place ^ 1, t + kSteps);
-                load(Outside(), i, t + 2 * kSteps);
-            });
+        if (kWaveN > 64 || left > 1)   // (for the large tile, whose registers are full, without a branch)
+            each<kSlots>([&](auto i) { stage(Outside(), sums, i, place ^ 1, t); });
 #pragma clang loop unroll(disable)
         for (int group = 0; group < 4; ++group) {
             each<kReads>([&](auto i) { read(0, place, group, i); });
@@ -262,36 +274,36 @@ __global__ __launch_bounds__(kBlock * kTeams) void k_weight_grad(WeightGradArgs 
     __syncthreads();
 
     if constexpr (kTeams > 1) {
-        static_assert(kTeams == 2 && kWaves * kSide * kSide * 4096 <= 2 * kPlace, "room in a team's own");
-        f4 *const sums_here = (f4 *)(every + 2 * kPlace) + wave * (kSide * kSide * 256) + lane;
+        static_assert(kTeams == 2 && kTeam * kSideN * kSideK * 4096 <= 2 * kPlace, "room in a team's own");
+        f4 *const sums_here = (f4 *)(every + 2 * kPlace) + wave * (kSideN * kSideK * 256) + lane;
         if (team == 1) {
 #pragma unroll
-            for (int i = 0; i < kSide * kSide * 4; ++i) {
-                const f16 &v = acc[i / 4 / kSide][i / 4 % kSide];
+            for (int i = 0; i < kSideN * kSideK * 4; ++i) {
+                const f16 &v = acc[i / 4 / kSideK][i / 4 % kSideK];
                 sums_here[i * 64] = f4{v[i % 4 * 4], v[i % 4 * 4 + 1], v[i % 4 * 4 + 2], v[i % 4 * 4 + 3]};
             }
         }
         __syncthreads();
         if (team == 0) {
 #pragma unroll
-            for (int i = 0; i < kSide * kSide * 4; ++i) {
+            for (int i = 0; i < kSideN * kSideK * 4; ++i) {
                 const f4 v = sums_here[i * 64];
 #pragma unroll
-                for (int c = 0; c < 4; ++c) acc[i / 4 / kSide][i / 4 % kSide][i % 4 * 4 + c] += v[c];
+                for (int c = 0; c < 4; ++c) acc[i / 4 / kSideK][i / 4 % kSideK][i % 4 * 4 + c] += v[c];
             }
         }
         __syncthreads();
     }
     if (team == 0) {   // 32 rows at a time through LDS, each wavefront's for itself, to be stored in whole lines
-        constexpr int kRow = kWave + 4, kLanes = kWave / 4;   // kLanes: that a row takes
-        static_assert(kWaves * 32 * kRow * 4 <= 2 * kPlace, "room");
+        constexpr int kRow = kWaveK + 4, kLanes = kWaveK / 4;   // kLanes: that a row takes
+        static_assert(kTeam * 32 * kRow * 4 <= 2 * kPlace, "room");
         float *const mine = (float *)lds + wave * 32 * kRow;
         const uint32_t row0 = lane / kLanes, col = lane % kLanes * 4, k_here = k0 + wk + col;
         const int count = k_here < p.k ? (int)min(p.k - k_here, 4u) : 0;
 #pragma unroll
-        for (int i = 0; i < kSide; ++i) {
+        for (int i = 0; i < kSideN; ++i) {
 #pragma unroll
-            for (int j = 0; j < kSide; ++j)
+            for (int j = 0; j < kSideK; ++j)
 #pragma unroll
                 for (int c = 0; c < 4; ++c)
                     *(f4 *)(mine + (lane & 31) * kRow + 32 * j + 8 * c + 4 * (lane >> 5)) =
@@ -305,7 +317,7 @@ __global__ __launch_bounds__(kBlock * kTeams) void k_weight_grad(WeightGradArgs 
                 for (int s = 0; s < 32; s += 64 / kLanes) {
                     if (first + s >= p.n) break;
                     const f4 v = *(const f4 *)(line + s * kRow);
-                    if constexpr (kWave == 64) __builtin_nontemporal_store(v, (f4u *)(at + (uint64_t)s * p.k));
+                    if constexpr (kTile == 128) __builtin_nontemporal_store(v, (f4u *)(at + (uint64_t)s * p.k));
                     else *(f4u *)(at + (uint64_t)s * p.k) = v;
                 }
             } else
@@ -320,7 +332,7 @@ __global__ __launch_bounds__(kBlock * kTeams) void k_weight_grad(WeightGradArgs 
 #pragma unroll
     for (int j = 0; j < 8; ++j) part[(team * kRowsY + y_row) * kTile + y_chunk * 8 + j] = db[j];
     __syncthreads();
-    for (uint32_t c = threadIdx.x; c < kTile; c += kBlock * kTeams) {
+    for (uint32_t c = threadIdx.x; c < kTile; c += kThreads * kTeams) {
         float s = 0.f;
 #pragma unroll
         for (int i = 0; i < kTeams * kRowsY; ++i) s += part[i * kTile + c];
@@ -390,17 +402,17 @@ void launch_weight_grad(const void *dy, lgc_type type, uint32_t rows, uint32_t n
         return;
     }
     auto tiles = [&](uint32_t side) { return (uint64_t)((n + side - 1) / side) * ((k + side - 1) / side); };
-    // Large tiles where they leave no more than a third of the compute units idle, taken over all rounds of a tile per unit (us, small / large, 4096 rows:
-    // 2816 x 4096 132 / 135, 3000 x 4096 158 / 144, 4096 x 4864 211 / 237, 4096 x 5632 256 / 243; 8192 x 4096 x 16384 1216 / 960), and for rows that make the products last
-    // longer than a tile's stores, during which a block that has a compute unit for itself multiplies nothing (32 x 8192 x 8192 52 / 77, 400 x 8192 x 8192 119 / 134,
-    // 600 x 4096 x 5632 56 / 69, 1000 x 3000 x 4096 43 / 49, 800 x 8192 x 8192 171 / 167, 2000 x 4096 x 5632 132 / 142)
-    const uint64_t rounds = (tiles(256) + cus - 1) / cus;
-    const bool large = type == LGC_BF16 && rows > 1024 && 3 * tiles(256) >= 2 * rounds * (uint64_t)cus;
+    // Large tiles where small ones would not all be resident, two per compute unit, and rows make more than two steps (us, small / large: 32 x 8192 x 8192 46 / 58,
+    // 94 x 7539 x 8192 62 / 67, 200 x 8192 x 8192 89 / 86, 600 x 8192 x 8192 142 / 120, 2000 x 2500 x 4096 69 / 60, 4096 x 4096 x 4864 203 / 204, 8192 x 4096 x 16384
+    // 1216 / 890), and where they fill two thirds of the compute units with parts of 2048 rows (8192 x 2000 x 2500 128 / 95, 16384 x 1500 x 1500 108 / 90,
+    // 16384 x 2048 x 2048 157 / 147, 8192 x 2048 x 2048 82 / 85, 2000 x 1500 x 3500 40 / 46), unless small ones fill all, two per unit (8192 x 2048 x 4096 149 / 172)
+    const uint64_t small = tiles(128), most_parts = (uint64_t)cus / tiles(256);
+    const bool large = type == LGC_BF16 && (small > 2 * (uint64_t)cus ? rows > 128 : small < 2 * (uint64_t)cus && rows >= 2048 * most_parts && 3 * most_parts * tiles(256) >= 2 * (uint64_t)cus);
     const uint32_t side = large ? 256 : 128;
     // Few tiles: the rows in parts, a block per compute unit at most and 512 rows at least: the parts' sums go to memory and back, eight bytes per weight and part
     // (us with up to one / two blocks per compute unit: 3001 x 768 x 1280 21.7 / 22.8, 2048 x 2048 x 2048 28 / 40, 8192 x 1024 x 1024 33 / 37; with 256 rows at least:
-    // 512 x 768 x 1280 12.1 / 16.0).  Two blocks where one leaves over a third of the compute units idle and the rows are many (16384 x 1500 x 1500 135 / 113,
-    // 8192 x 1500 x 1500 73 / 65, 4096 x 1500 x 1500 41 / 41).
+    // 512 x 768 x 1280 12.1 / 16.0).  Two blocks where one leaves over a third of the compute units idle and the rows are many (8192 x 1500 x 1500 73 / 65,
+    // 4096 x 1500 x 1500 41 / 41).
     const uint64_t one = (uint64_t)cus / tiles(side), two = 2 * (uint64_t)cus / tiles(side);
     uint64_t parts = std::min({3 * one * tiles(side) < 2 * (uint64_t)cus && rows >= 2048 * two ? two : one, (uint64_t)(rows + 511) / 512, scratch_floats / count, (uint64_t)65535});
     parts = std::max<uint64_t>(parts, 1);
@@ -413,10 +425,10 @@ void launch_weight_grad(const void *dy, lgc_type type, uint32_t rows, uint32_t n
         if (db) p.db = scratch + count_w;
     }
     const dim3 grid((uint32_t)tiles(side), (uint32_t)parts);
-    if (type == LGC_FP32) k_weight_grad<float, 64, 1><<<grid, kBlock, 0, st>>>(p);
-    else if (large) k_weight_grad<Bf16, 128, 1><<<grid, kBlock, 0, st>>>(p);
-    else if (tiles(side) * parts > (uint64_t)cus) k_weight_grad<Bf16, 64, 1><<<grid, kBlock, 0, st>>>(p);   // (two blocks share a compute unit)
-    else k_weight_grad<Bf16, 64, 2><<<grid, 2 * kBlock, 0, st>>>(p);
+    if (type == LGC_FP32) k_weight_grad<float, 64, 64, 4, 1><<<grid, kBlock, 0, st>>>(p);
+    else if (large) k_weight_grad<Bf16, 128, 64, 8, 1><<<grid, 2 * kBlock, 0, st>>>(p);
+    else if (tiles(side) * parts > (uint64_t)cus) k_weight_grad<Bf16, 64, 64, 4, 1><<<grid, kBlock, 0, st>>>(p);   // (two blocks share a compute unit)
+    else k_weight_grad<Bf16, 64, 64, 4, 2><<<grid, 2 * kBlock, 0, st>>>(p);
     if (parts > 1) k_add_parts<<<add_grid, kBlock, 0, st>>>(scratch, (uint32_t)parts, count, dw, count_w, db, count);
 }
 

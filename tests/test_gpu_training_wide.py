@@ -149,3 +149,22 @@ def test_layer_norm_grad_of_many_rows(B, ctx, rows, cols, dtype):
     assert torch.equal(alone, dg)
     B.lgc_layer_norm_grad(ctx, dy, x, gamma, mean, rstd, again[0].zero_())
     assert torch.equal(again[0], dx)
+
+
+# Large tiles: two steps and three, rows in parts; rows of dy so far apart that a step's distances pass 32 bits
+@pytest.mark.parametrize("rows,n,k", [(128, 4200, 4100), (140, 4200, 4100), (6200, 1500, 3500)])
+def test_weight_grad_by_large_tiles(B, ctx, rows, n, k):
+    test_weight_grad(B, ctx, rows, n, k, torch.bfloat16)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_weight_grad_of_rows_far_apart(B, ctx, dtype):
+    rows, n, k, ld = 330, 130, 140, (1 << 24) + 8
+    x = as_blocks(B, ctx, rand((rows, k), 1))
+    dy = torch.empty(((rows - 1) * ld + n,), dtype=dtype, device="cuda").as_strided((rows, n), (ld, 1))
+    dy.copy_(rand((rows, n), 2, 1e-2, dtype))
+    xv, yv = ref.blocks_values(x).cuda(), dy.double()
+    dw, db = torch.empty((n, k), device="cuda"), torch.empty((n,), device="cuda")
+    B.lgc_weight_grad(ctx, dy, x, dw, db)
+    assert ((dw.double() - yv.t() @ xv).abs() <= (rows + 64) * U * (yv.abs().t() @ xv.abs()) + 1e-36).all()
+    assert ((db.double() - yv.sum(0)).abs() <= (rows + 64) * U * yv.abs().sum(0) + 1e-36).all()
