@@ -3,6 +3,9 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <algorithm>
+#include <cmath>
+
 #include "../../include/lgc.h"
 
 namespace lgc {
@@ -299,6 +302,13 @@ __host__ __device__ inline uint64_t block_count(uint64_t cols) { return (cols + 
 __host__ __device__ inline uint64_t codes_stride(uint64_t cols) { return block_count(cols) * kBlockCols; }
 __host__ __device__ inline uint64_t exps_stride(uint64_t cols) { return (block_count(cols) + 3) / 4 * 4; }
 constexpr size_t kTrainingFloats = (size_t)16 << 20;   // scratch of lgc_reserve_training: partial sums, never more of them than fit
+// In how many parts, `most` at most, to make sums that one part takes `work` us for, where tiles are fewer than compute units: the parts' sums go to memory and back, half
+// a microsecond per MB of each (measured: 4 parts of 1000 x 1000 9.4 us, 3 of 300 x 3000 8.5, 4 of 512 x 512 4.3 to 6, with the launch that adds them, of 4).
+inline uint64_t parts_of(double work, uint64_t results, uint64_t most) {
+    const double one = 2e-6 * (double)results;
+    const uint64_t parts = std::min(most, (uint64_t)std::sqrt(work / one));
+    return parts > 1 && work / (double)parts + one * (double)parts + 4 < work ? parts : 1;
+}
 // blocks.hip; tiles: an exponent is shared by 128 rows.  Pointers of what is not wanted are null
 void launch_quantize(const void *x, lgc_type type, uint32_t rows, uint32_t cols, uint64_t ld, uint8_t *codes, uint8_t *exps, hipStream_t st);
 void launch_dequantize(const uint8_t *codes, const uint8_t *exps, bool tiles, uint32_t rows, uint32_t cols, void *x, lgc_type type, uint64_t ld, hipStream_t st);

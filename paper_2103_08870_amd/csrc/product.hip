@@ -404,10 +404,11 @@ void launch_product(const uint8_t *a, const uint8_t *a_exps, const uint8_t *b, c
     // 4096 x 4864 x 4096 103 / 99, 4096 x 5632 x 4096 97 / 99, 8192 x 16384 x 4096 546 / 443)
     const bool large = type == LGC_BF16 && tiles(128) > 2 * (uint64_t)cus;
     const uint32_t side = large ? 256 : 128;
-    // Few tiles: the sum over k in parts, a block per compute unit, of 8 blocks of columns at least; two per compute unit where each keeps 32: the parts' sums go to
-    // memory and back (us with up to one / two: 2048 x 2048 x 2048 15.0 / 24.0, 1000 x 2500 x 1777 13.0 / 21.1, 512 x 4096 x 16384 52.3 / 46.2)
+    // Few tiles: the sum over k in parts, a block per compute unit at most, where that saves more of the 0.4 us (to fp32 0.7) that a block of columns takes than the parts'
+    // sums cost (us in one / that many parts: 2000 x 1000 x 2000 12.0 / 20.0 (not taken), 300 x 3000 x 3000 14.0 / 16.7 (not taken), to fp32 22.4 / 19.7,
+    // 512 x 512 x 4096 16.1 / 11.8); two blocks per compute unit where each keeps 32 blocks of columns (512 x 4096 x 16384 52.3 / 46.2 with one / two)
     const uint64_t twice = 2 * (uint64_t)cus / tiles(side);
-    split(twice && blocks / twice >= 32 ? twice : std::min<uint64_t>((uint64_t)cus / tiles(side), blocks / 8));
+    split(twice && blocks / twice >= 32 ? twice : parts_of((type == LGC_FP32 ? 0.7 : 0.4) * blocks, (uint64_t)m * n, std::min<uint64_t>((uint64_t)cus / tiles(side), blocks / 4)));
     p.tiles_m = (m + side - 1) / side;
     p.tiles_n = (n + side - 1) / side;
     const dim3 grid((uint32_t)tiles(side), (uint32_t)parts);

@@ -409,14 +409,15 @@ void launch_weight_grad(const void *dy, lgc_type type, uint32_t rows, uint32_t n
     const uint64_t small = tiles(128), most_parts = (uint64_t)cus / tiles(256);
     const bool large = type == LGC_BF16 && (small > 2 * (uint64_t)cus ? rows > 128 : small < 2 * (uint64_t)cus && rows >= 2048 * most_parts && 3 * most_parts * tiles(256) >= 2 * (uint64_t)cus);
     const uint32_t side = large ? 256 : 128;
-    // Few tiles: the rows in parts, a block per compute unit at most and 512 rows at least: the parts' sums go to memory and back, eight bytes per weight and part
-    // (us with up to one / two blocks per compute unit: 3001 x 768 x 1280 21.7 / 22.8, 2048 x 2048 x 2048 28 / 40, 8192 x 1024 x 1024 33 / 37; with 256 rows at least:
-    // 512 x 768 x 1280 12.1 / 16.0).  Two blocks where one leaves over a third of the compute units idle and the rows are many (8192 x 1500 x 1500 73 / 65,
-    // 4096 x 1500 x 1500 41 / 41).
+    // Few tiles: the rows in parts, a block per compute unit at most (3001 x 768 x 1280 21.7 us, with two 22.8; 2048 x 2048 x 2048 28 / 40), of 128 rows at least, where that
+    // saves more of the 8.4 us (in fp32 20) that 1000 rows take than the parts' sums cost (in one / so many parts: 1000 x 1000 x 1000 16.1 / 17.3 (not taken),
+    // 1000 x 300 x 260 15.4 / 11.8, 16000 x 256 x 256 41 / 14.5).  Two blocks where one leaves over a third of the compute units idle and the rows are many
+    // (8192 x 1500 x 1500 73 / 65, 4096 x 1500 x 1500 41 / 41).
     const uint64_t one = (uint64_t)cus / tiles(side), two = 2 * (uint64_t)cus / tiles(side);
-    uint64_t parts = std::min({3 * one * tiles(side) < 2 * (uint64_t)cus && rows >= 2048 * two ? two : one, (uint64_t)(rows + 511) / 512, scratch_floats / count, (uint64_t)65535});
+    uint64_t parts = large ? one : parts_of((type == LGC_FP32 ? 0.02 : 0.0084) * rows, count_w, 3 * one * tiles(side) < 2 * (uint64_t)cus && rows >= 2048 * two ? two : one);
+    parts = std::min({parts, (uint64_t)(rows + 127) / 128, scratch_floats / count, (uint64_t)65535});
     parts = std::max<uint64_t>(parts, 1);
-    p.share = (uint32_t)((rows + parts - 1) / parts + 63) / 64 * 64;
+    p.share = (uint32_t)((rows + parts - 1) / parts + 127) / 128 * 128;   // (a step of two teams)
     parts = (rows + p.share - 1) / p.share;
     p.tiles_n = (n + side - 1) / side;
     p.tiles_k = (k + side - 1) / side;
