@@ -405,9 +405,10 @@ void launch_weight_grad(const void *dy, lgc_type type, uint32_t rows, uint32_t n
     // Large tiles where small ones would not all be resident, two per compute unit, and rows make more than two steps (us, small / large: 32 x 8192 x 8192 46 / 58,
     // 94 x 7539 x 8192 62 / 67, 200 x 8192 x 8192 89 / 86, 600 x 8192 x 8192 142 / 120, 2000 x 2500 x 4096 69 / 60, 4096 x 4096 x 4864 203 / 204, 8192 x 4096 x 16384
     // 1216 / 890), and where they fill two thirds of the compute units with parts of 2048 rows (8192 x 2000 x 2500 128 / 95, 16384 x 1500 x 1500 108 / 90,
-    // 16384 x 2048 x 2048 157 / 147, 8192 x 2048 x 2048 82 / 85, 2000 x 1500 x 3500 40 / 46), unless small ones fill all, two per unit (8192 x 2048 x 4096 149 / 172)
+    // 16384 x 2048 x 2048 157 / 147, 8192 x 2048 x 2048 82 / 85, 2000 x 1500 x 3500 40 / 46), unless small ones fill all, two per unit (8192 x 2048 x 4096 149 / 172);
+    // never where half of a large tile would lie beyond dw (4096 x 32768 x 100 62 / 90, but x 384 142 / 133)
     const uint64_t small = tiles(128), most_parts = (uint64_t)cus / tiles(256);
-    const bool large = type == LGC_BF16 && (small > 2 * (uint64_t)cus ? rows > 128 : small < 2 * (uint64_t)cus && rows >= 2048 * most_parts && 3 * most_parts * tiles(256) >= 2 * (uint64_t)cus);
+    const bool large = type == LGC_BF16 && 2 * tiles(256) < small && (small > 2 * (uint64_t)cus ? rows > 128 : small < 2 * (uint64_t)cus && rows >= 2048 * most_parts && 3 * most_parts * tiles(256) >= 2 * (uint64_t)cus);
     const uint32_t side = large ? 256 : 128;
     // Few tiles: the rows in parts, a block per compute unit at most (3001 x 768 x 1280 21.7 us, with two 22.8; 2048 x 2048 x 2048 28 / 40), of 128 rows at least, where that
     // saves more of the 8.4 us (in fp32 20) that 1000 rows take than the parts' sums cost (in one / so many parts: 1000 x 1000 x 1000 16.1 / 17.3 (not taken),

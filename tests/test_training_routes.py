@@ -63,6 +63,8 @@ ROUTES = [
     (product, (0, 512, 4096, BF16), []),
     (weight_grad, (0, 100, 100, BF16), ["k_add_parts"]), (weight_grad, (1, 7, 100, BF16), ["k_weight_grad_small"]), (weight_grad, (1, 8, 100, BF16), ["k_weight_grad 64 64 4 2"]),
     (weight_grad, (100, 8, 100, FP32), ["k_weight_grad 64 64 4 1"]), (weight_grad, (128, 8192, 8192, BF16), ["k_weight_grad 64 64 4 1"]),
+    (weight_grad, (4096, 32768, 100, BF16), ["k_weight_grad 64 64 4 2"]), (weight_grad, (4096, 131072, 128, BF16), ["k_weight_grad 64 64 4 1"]),
+    (weight_grad, (4096, 131072, 129, BF16), ["k_weight_grad 128 64 8 1"]),
     (weight_grad, (129, 8192, 8192, BF16), ["k_weight_grad 128 64 8 1"]), (weight_grad, (3001, 777, 1300, BF16), ["k_weight_grad 64 64 4 2", "k_add_parts"]),
     (weight_grad, (8192, 2000, 2500, BF16), ["k_weight_grad 128 64 8 1", "k_add_parts"]), (weight_grad, (8192, 2048, 4096, BF16), ["k_weight_grad 64 64 4 1"]),
     (weight_grad, (8192, 1500, 1500, BF16), ["k_weight_grad 64 64 4 1", "k_add_parts"]), (weight_grad, (8192, 2000, 2500, FP32), ["k_weight_grad 64 64 4 1"]),
