@@ -406,7 +406,8 @@ lgc_status lgc_layer_norm(lgc_ctx *ctx, const void *x, lgc_type type, uint64_t r
  * Its gradient, from lgc_layer_norm's mean and rstd: with h = (x - mean) rstd and
  * q = dy gamma,  dx = rstd (q - mean(q) - h mean(q h)) (means over the row),
  * dgamma = sum over rows of dy h,  dbeta = sum over rows of dy.  Any of dx, dgamma
- * and dbeta may be NULL.
+ * and dbeta may be NULL.  dx overlaps neither dy nor x, which are still read for
+ * the sums while rows of dx are written (LGC_EINVAL where it begins where they do).
  */
 lgc_status lgc_layer_norm_grad(lgc_ctx *ctx, const void *dy, uint64_t ld_dy, const void *x, uint64_t ld, lgc_type type,
                                uint64_t rows, uint64_t cols, const float *gamma, const float *mean, const float *rstd, void *dx,

@@ -1563,7 +1563,8 @@ extern "C" lgc_status lgc_layer_norm_grad(lgc_ctx *ctx, const void *dy, uint64_t
                                           void *stream) {
     Check c(ctx);
     c.type(type).cols("cols", cols).rows("rows", rows, cols).maybe("gamma", gamma).maybe("dgamma", dgamma).maybe("dbeta", dbeta);
-    if (rows) c.plain("dy", dy, type, cols, ld_dy).plain("x", x, type, cols, ld).vector("mean", mean).vector("rstd", rstd).maybe("dx", dx, type, cols, ld_dx);
+    if (rows) c.plain("dy", dy, type, cols, ld_dy).plain("x", x, type, cols, ld).vector("mean", mean).vector("rstd", rstd).maybe("dx", dx, type, cols, ld_dx)
+        .need(!dx || (dx != dy && dx != x), "dx lies where %s does: the arrays of a call must not overlap", dx == dy ? "dy" : "x");
     c.reserved("lgc_layer_norm_grad");
     return launch(c, [&] {
         launch_norm_grad(dy, ld_dy, x, ld, type, (uint32_t)rows, (uint32_t)cols, gamma, mean, rstd, dx, ld_dx, dgamma, dbeta, ctx->training, kTrainingFloats, ctx->cus,

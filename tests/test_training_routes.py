@@ -22,7 +22,7 @@ def layer_norm(l, ctx, rows, cols, type):
 
 
 def layer_norm_grad(l, ctx, rows, cols, type, wants="xgb"):
-    dx, dg, db = (AT if w in wants else None for w in "xgb")
+    dx, dg, db = (p(1 << 41) if w in wants else None for w in "xgb")
     return l.lgc_layer_norm_grad(ctx, AT, u64(cols), AT, u64(cols), type, u64(rows), u64(cols), AT, AT, AT, dx, u64(cols), dg, db, None)
 
 
@@ -132,6 +132,10 @@ def test_reservation_is_made_once_and_no_call_allocates(answers):
     assert answers["reserved"] == [["malloc", 64 << 20]] and answers["again"] == [] and answers["allocated by calls"] == 0
 
 
+def test_a_gradient_in_place_is_refused(answers):
+    assert answers["in place"] == [1, 1, 0] and answers["launched in place"] == []
+
+
 if __name__ == "__main__":
     h = Host(sys.argv[1], sys.argv[2])
     h.train = h.ctx(1, 1, 1)
@@ -142,6 +146,12 @@ if __name__ == "__main__":
     out["again"] = h.log()
     out["routes"] = [launches(h, call, args) for call, args, _ in ROUTES]
     out["largest"] = [launches(h, call, args) for call, args in LARGEST]
+    h.log()
+    dy, x = p(1 << 41), p(1 << 42)
+    out["in place"] = [h.lib.lgc_layer_norm_grad(h.train, dy, u64(16), x, u64(16), FP32, rows, u64(16), AT, AT, AT, dx, u64(16), AT, AT, None)
+                       for dx, rows in ((dy, u64(8)), (x, u64(8)))]
+    out["launched in place"] = h.log()
+    out["in place"].append(h.lib.lgc_layer_norm_grad(h.train, dy, u64(16), x, u64(16), FP32, u64(0), u64(16), AT, AT, AT, dy, u64(16), AT, AT, None))
     h.log()
     out["allocated by calls"] = sum("malloc" in str(x) for x in out["routes"] + out["largest"])
     print(json.dumps(out))
