@@ -459,7 +459,7 @@ def _refuse(what: str):
     raise ValueError(f"liblgc binding: {what}")
 
 
-# (The calls below are short: what checks their arguments counts, by the tenth of a microsecond an attribute of a tensor, so each is asked for once.)
+# (The calls below are short: what checks their arguments counts, by the twentieth of a microsecond a question to a tensor and a call, so each is asked for once.)
 
 def _own(t: torch.Tensor, what: str):
     """(type, rows, columns, pointer, elements from row to row) of the plain matrix that gives a call its sizes."""
@@ -467,7 +467,12 @@ def _own(t: torch.Tensor, what: str):
     if kind is None or len(shape) != 2:
         _refuse(f"{what} must be a matrix of float32 or bfloat16")
     rows, cols = shape
-    return kind, rows, cols, *_rows(t, rows, cols, what)
+    ld, step = t.stride()
+    if step != 1 and cols > 1 and rows:
+        _refuse(f"{what} must have contiguous rows")
+    if not t.is_cuda:
+        raise ValueError("liblgc takes device tensors only")
+    return kind, rows, cols, t.data_ptr(), ld if rows > 1 else max(1, cols)
 
 
 def _matrix(t: Optional[torch.Tensor], rows: int, cols: int, dtype, what: str):
@@ -476,10 +481,6 @@ def _matrix(t: Optional[torch.Tensor], rows: int, cols: int, dtype, what: str):
         return None, 0
     if t.shape != (rows, cols) or t.dtype is not dtype:
         _refuse(f"{what} must be {(rows, cols)} of {dtype}")
-    return _rows(t, rows, cols, what)
-
-
-def _rows(t: torch.Tensor, rows: int, cols: int, what: str):
     ld, step = t.stride()
     if step != 1 and cols > 1 and rows:
         _refuse(f"{what} must have contiguous rows")
@@ -493,7 +494,9 @@ def _vector(t: Optional[torch.Tensor], n: int, what: str) -> Optional[int]:
         return None
     if t.numel() != n or not t.is_contiguous():
         _refuse(f"{what} must be contiguous with {n} elements")
-    return _ptr(t, _FP32)
+    if not t.is_cuda or t.dtype is not _FP32:
+        return _ptr(t, _FP32)   # (which says what is wrong)
+    return t.data_ptr()
 
 
 def _blocks(b: Optional[Blocks], rows: int, cols: int, what: str, tiles: bool = False):
