@@ -8,8 +8,8 @@ namespace {
 // All of these are bound by the bytes that they move, and small ones by the time to launch and to wait for memory once.  16 lanes take a block of 128 columns, eight
 // neighbouring ones each (16 or 32 bytes), so that the block's largest magnitude is found by four exchanges between registers and its codes leave as whole lines.
 // They handle kUnits blocks one after the other, with all loads queued first: four, or one where there are not more than are resident at once (509 x 5000 in fp32, SiLU
-// and its gradient: 7.7 and 7.1 us with four, 7.0 and 6.8 with one).  Measured, of what they read and write: 8192 x 16384 in bf16, GELU to plain and two of 8 bits
-// 115 us (5.9 TB/s), its gradient 130 us (5.2 TB/s); 8192 x 4096 from 8 bits to bf16 15.7 us (6.5 TB/s, partly from the caches); 3001 x 777 in fp32 to 8 bits 4.0 us,
+// and its gradient: 7.7 and 7.1 us with four, 7.0 and 6.8 with one).  Measured, of what they read and write: 8192 x 16384 in bf16, GELU with its input kept in 8 bits
+// 115 us (5.8 TB/s), its gradient 130 us (5.2 TB/s); 8192 x 4096 from 8 bits to bf16 15.7 us (6.5 TB/s, partly from the caches); 3001 x 777 in fp32 to 8 bits 4.0 us,
 // back 5.0.
 
 // One of the launch's blocks of 128 columns as 16 lanes see it: the lane's eight columns.
