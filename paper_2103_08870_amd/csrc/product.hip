@@ -406,9 +406,12 @@ void launch_product(const uint8_t *a, const uint8_t *a_exps, const uint8_t *b, c
     const uint32_t side = large ? 256 : 128;
     // Few tiles: the sum over k in parts, a block per compute unit at most, where that saves more of the 0.4 us (to fp32 0.7) that a block of columns takes than the parts'
     // sums cost (us in one / that many parts: 2000 x 1000 x 2000 12.0 / 20.0 (not taken), 300 x 3000 x 3000 14.0 / 16.7 (not taken), to fp32 22.4 / 19.7,
-    // 512 x 512 x 4096 16.1 / 11.8); two blocks per compute unit where each keeps 32 blocks of columns (512 x 4096 x 16384 52.3 / 46.2 with one / two)
+    // 512 x 512 x 4096 16.1 / 11.8); two blocks per compute unit where each keeps 32 blocks of columns (512 x 4096 x 16384 52.3 / 46.2 with one / two).
+    // Large tiles are never split: they store the product's own type, of which parts cannot be, and a compute unit holds one block of them, so that two parts run one after
+    // the other (whole / in parts that store fp32: 280 x 28672 x 8192 112 / 133, 700 x 11000 x 14000 169 / 177, 513 x 15000 x 16384 185 / 214; in three, which end sooner,
+    // 129 x 32800 x 12288 166 / 152, not taken for a kernel more).
     const uint64_t twice = 2 * (uint64_t)cus / tiles(side);
-    split(twice && blocks / twice >= 32 ? twice : parts_of((type == LGC_FP32 ? 0.7 : 0.4) * blocks, (uint64_t)m * n, std::min<uint64_t>((uint64_t)cus / tiles(side), blocks / 4)));
+    split(large ? 1 : twice && blocks / twice >= 32 ? twice : parts_of((type == LGC_FP32 ? 0.7 : 0.4) * blocks, (uint64_t)m * n, std::min<uint64_t>((uint64_t)cus / tiles(side), blocks / 4)));
     p.tiles_m = (m + side - 1) / side;
     p.tiles_n = (n + side - 1) / side;
     const dim3 grid((uint32_t)tiles(side), (uint32_t)parts);
