@@ -353,7 +353,9 @@ lgc_status lgc_reserve(lgc_ctx *ctx, const lgc_ae *ae /* nullable */, uint64_t k
  *          every value is zero or a normal number of bf16 and fp32).  Codes are
  *          rounded to nearest, ties to even: an element is off by at most 2^-4 of
  *          itself or 2^-17 of the block's largest (2^-127 absolute in a block
- *          below 448 * 2^-117).  Infinities and NaNs become NaN.
+ *          below 448 * 2^-117).  Infinities and NaNs become NaN.  Finite numbers stay
+ *          finite: where E is 247, its largest, codes end at 240 (256 would stand
+ *          for 2^128).
  *
  * Limits: columns (cols, n, k) from 1 to 2^20; rows below 2^31, and rows times
  * blocks of 128 columns below 2^30.  rows == 0 is valid: nothing is computed, and

@@ -107,6 +107,7 @@ __device__ __forceinline__ uint32_t max_of_16(uint32_t x) {
 
 constexpr uint32_t kInfKey = 0x7f800000u;
 constexpr uint32_t kLeastExp = 10;
+constexpr uint32_t kMostExp = 247;   // of the block whose largest magnitude passes 1.75 * 2^127
 
 // The exponent byte of a block whose largest finite magnitude has this key: the least E, from kLeastExp on, with magnitude <= 448 * 2^(E - 127)
 // (448 = 1.75 * 2^8 is the largest code).  A scale that is a power of two makes the division exact, so that each element is rounded once, and it
@@ -135,14 +136,19 @@ __device__ __forceinline__ uint32_t most_of_16(const float (&x)[8]) {
     }
     return most;
 }
-// Codes of eight elements divided by the block's scale, rounded to the nearest (ties to even); the conversion turns infinities into NaN codes.
-__device__ __forceinline__ u2 codes_of(const float (&x)[8], float scale) {
+// Codes of eight elements divided by the block's scale 2^(e - 127), rounded to the nearest (ties to even); the conversion turns infinities into NaN codes.
+// At the largest e a number may round to code 256 (0x78), whose value is beyond fp32 and bf16: it becomes 240, which is still within 2^-4 of it.
+__device__ __forceinline__ u2 codes_of(const float (&x)[8], uint32_t e) {
+    const float scale = exp_scale(e);
     u2 r;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         const s2 lo = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(s2{0, 0}, x[4 * i], x[4 * i + 1], scale, false);
         r[i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(lo, x[4 * i + 2], x[4 * i + 3], scale, true));
     }
+    if (e == kMostExp)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) r[i] -= ((0x80808080u - ((r[i] & 0x7f7f7f7fu) ^ 0x78787878u)) & 0x80808080u) >> 7;   // (of four bytes, 1 from those that are 0x78)
     return r;
 }
 __device__ __forceinline__ void values_of(const u2 codes, float scale, float (&x)[8]) {
@@ -157,7 +163,7 @@ __device__ __forceinline__ void values_of(const u2 codes, float scale, float (&x
 // Elements that do not exist are zeros.  All 16 lanes must be active.
 __device__ __forceinline__ void store_block(const float (&x)[8], uint8_t *codes, uint8_t *exp) {
     const uint32_t e = block_exp(most_of_16(x));
-    *(u2 *)codes = codes_of(x, exp_scale(e));
+    *(u2 *)codes = codes_of(x, e);
     if ((threadIdx.x & 15) == 0) *exp = (uint8_t)e;
 }
 

@@ -112,11 +112,10 @@ __global__ __launch_bounds__(kBlock) void k_quantize_tiles(const T *w, uint64_t 
 #pragma unroll
     for (int i = 0; i < kWaves; ++i) all = most[i] > all ? most[i] : all;
     const uint32_t e = block_exp(all);
-    const float scale = exp_scale(e);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const uint32_t r = threadIdx.x / 16 + 16 * i;
-        const u2 c = codes_of(v[i], scale);
+        const u2 c = codes_of(v[i], e);
         if (r0 + r < rows) *(u2 *)(codes + (uint64_t)(r0 + r) * code_stride + col) = c;
         if (codes_t)
 #pragma unroll
