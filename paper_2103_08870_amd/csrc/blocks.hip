@@ -24,8 +24,11 @@ __device__ __forceinline__ Place place_of(uint32_t unit, const Divide &blocks, u
     p.count = count_at(p.col, cols);
     return p;
 }
+constexpr uint32_t kAcross = 1u << 20;   // blocks in a launch's first dimension at most, whose threads are counted in 32 bits
 template <int kUnits>
-__device__ __forceinline__ uint32_t first_unit() { return blockIdx.x * (uint32_t)(kUnits * kBlock / 16) + threadIdx.x / 16; }
+__device__ __forceinline__ uint32_t first_unit() {
+    return (blockIdx.x + blockIdx.y * kAcross) * (uint32_t)(kUnits * kBlock / 16) + threadIdx.x / 16;   // (below 2^30 + 2^26)
+}
 
 template <typename T, int kUnits>
 __global__ __launch_bounds__(kBlock) void k_quantize(const T *x, uint64_t ld, uint32_t cols, Divide blocks, uint32_t units, uint8_t *codes, uint8_t *exps,
@@ -236,8 +239,9 @@ __global__ __launch_bounds__(kBlock) void k_activate_grad(const T *dz, uint64_t 
 constexpr uint32_t kResident = 256 * 2048 / 16;   // groups of 16 lanes that the device holds
 template <typename F>
 void with_units(uint32_t units, F &&f) {   // f(units per 16 lanes, grid)
-    if (units <= kResident) f(std::integral_constant<int, 1>(), (units + kBlock / 16 - 1) / (kBlock / 16));
-    else f(std::integral_constant<int, 4>(), (units + 4 * (kBlock / 16) - 1) / (4 * (kBlock / 16)));
+    auto grid = [](uint32_t blocks) { return dim3(std::min(blocks, kAcross), (blocks + kAcross - 1) / kAcross); };
+    if (units <= kResident) f(std::integral_constant<int, 1>(), grid((units + kBlock / 16 - 1) / (kBlock / 16)));
+    else f(std::integral_constant<int, 4>(), grid((units + 4 * (kBlock / 16) - 1) / (4 * (kBlock / 16))));
 }
 
 template <typename F>
@@ -258,7 +262,7 @@ void launch_quantize(const void *x, lgc_type type, uint32_t rows, uint32_t cols,
     const uint32_t blocks = (uint32_t)block_count(cols), units = rows * blocks;
     with_type(type, [&](auto *t) {
         typedef std::remove_pointer_t<decltype(t)> T;
-        with_units(units, [&](auto n, uint32_t grid) {
+        with_units(units, [&](auto n, dim3 grid) {
             k_quantize<T, n><<<grid, kBlock, 0, st>>>((const T *)x, ld, cols, divide_by(blocks), units, codes, exps, (uint32_t)exps_stride(cols));
         });
     });
@@ -268,7 +272,7 @@ void launch_dequantize(const uint8_t *codes, const uint8_t *exps, bool tiles, ui
     const uint32_t blocks = (uint32_t)block_count(cols), units = rows * blocks;
     with_type(type, [&](auto *t) {
         typedef std::remove_pointer_t<decltype(t)> T;
-        with_units(units, [&](auto n, uint32_t grid) {
+        with_units(units, [&](auto n, dim3 grid) {
             k_dequantize<T, n><<<grid, kBlock, 0, st>>>(codes, exps, (uint32_t)exps_stride(cols), tiles ? 1 : 0, cols, divide_by(blocks), units, (T *)x, ld);
         });
     });
@@ -290,7 +294,7 @@ void launch_activate(lgc_act act, const void *a, lgc_type type, uint32_t rows, u
     with_type(type, [&](auto *t) {
         typedef std::remove_pointer_t<decltype(t)> T;
         with_act<T>(act, [&](auto kind) {
-            with_units(units, [&](auto n, uint32_t grid) {
+            with_units(units, [&](auto n, dim3 grid) {
                 k_activate<T, kind, n><<<grid, kBlock, 0, st>>>((const T *)a, ld, cols, divide_by(blocks), units, (T *)z, ld_z, a_codes, a_exps, z_codes, z_exps, (uint32_t)exps_stride(cols));
             });
         });
@@ -303,7 +307,7 @@ void launch_activate_grad(lgc_act act, const void *dz, lgc_type type, uint32_t r
     with_type(type, [&](auto *t) {
         typedef std::remove_pointer_t<decltype(t)> T;
         with_act<T>(act, [&](auto kind) {
-            with_units(units, [&](auto n, uint32_t grid) {
+            with_units(units, [&](auto n, dim3 grid) {
                 k_activate_grad<T, kind, n><<<grid, kBlock, 0, st>>>((const T *)dz, ld, cols, divide_by(blocks), units, a_codes, a_exps, (T *)da, ld_da, da_codes, da_exps, (uint32_t)exps_stride(cols));
             });
         });

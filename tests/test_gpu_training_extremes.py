@@ -141,3 +141,26 @@ def test_weight_grad(B, ctx, dtype):
     want = torch.zeros((40, 140), dtype=torch.float64)
     want[:, 9] = -TOP / 4
     assert torch.equal(dw.cpu().double(), want)
+
+
+def test_more_blocks_than_a_launch_s_first_dimension_has(B, ctx):
+    """2^26 rows of one column and some: 8.6 GB of codes, in two rows of a launch's blocks; the last rows of the first and all of the second against the same alone."""
+    rows, first = (1 << 26) + 70, (1 << 26) - 30
+    x = torch.zeros((rows, 1), dtype=torch.bfloat16, device="cuda")
+    x[first:] = torch.randn((rows - first, 1), generator=torch.Generator().manual_seed(1)).to(torch.bfloat16).cuda()
+    last = x[first:].clone()
+    big, small = B.Blocks(rows, 1), B.Blocks(rows - first, 1)
+    out, z = torch.full_like(x, 7.0), torch.empty_like(last)
+    B.lgc_quantize(ctx, last, small)
+    check(small, last.cpu(), 1)
+    B.lgc_quantize(ctx, x, big)
+    assert torch.equal(big.codes[first:], small.codes) and torch.equal(big.exps[first:, 0], small.exps[:, 0]) and bool((big.exps[:first, 0] == 10).all())
+    assert not any(bool(part.any()) for part in big.codes[:first].split(1 << 22))
+    for large, alone in ((lambda: B.lgc_dequantize(ctx, big, out), lambda: B.lgc_dequantize(ctx, small, z)),
+                         (lambda: B.lgc_activate(ctx, "gelu", x, z=out, a_blocks=big), lambda: B.lgc_activate(ctx, "gelu", last, z=z)),
+                         (lambda: B.lgc_activate_grad(ctx, "gelu", x, big, da=out), lambda: B.lgc_activate_grad(ctx, "gelu", last, small, da=z))):
+        out.fill_(7.0)
+        large()
+        alone()
+        assert torch.equal(out[first:], z) and not out[:first].any()
+    assert torch.equal(big.codes[first:], small.codes)

@@ -10,7 +10,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 if HERE not in sys.path:
     sys.path.insert(0, HERE)
 from test_host_routes import Host, ROOT   # noqa: E402,F401  (puts the repository's root in sys.path)
-from test_training_routes import BF16, FP32, product, weight_grad   # noqa: E402
+from test_training_routes import AT, BF16, FP32, product, quantize, u64, weight_grad   # noqa: E402
 
 # rows from one to many, widths that models have and others, sums short and long: either side of every rule of launch_product
 M = [1, 16, 17, 64, 65, 128, 129, 160, 257, 280, 300, 400, 513, 641, 700, 900, 1100, 2000, 2049, 4100, 8192]
@@ -33,6 +33,22 @@ def output_type(name):
     length = "".join(c for c in rest[:2] if c.isdigit())
     rest = rest[len(length) + int(length):]
     return "fp32" if rest.startswith("If") else "bf16" if rest.startswith("INS_4Bf16E") else rest
+
+
+def dequantize(l, ctx, rows, cols, type):
+    return l.lgc_dequantize(ctx, AT, AT, 1, u64(rows), u64(cols), AT, type, u64(cols), None)
+
+
+def activate(l, ctx, rows, cols, type):
+    return l.lgc_activate(ctx, 1, AT, type, u64(rows), u64(cols), u64(cols), AT, u64(cols), AT, AT, AT, AT, None)
+
+
+def activate_grad(l, ctx, rows, cols, type):
+    return l.lgc_activate_grad(ctx, 2, AT, type, u64(rows), u64(cols), u64(cols), AT, AT, AT, u64(cols), AT, AT, None)
+
+
+# blocks of 128 columns: up to the most that the calls take, and either side of where a launch's second dimension begins
+BLOCKS = [(rows, cols) for rows in ((1 << 30) - 1, (1 << 30) - 63, (1 << 30) - 64, (1 << 30) - 65, (1 << 26) + 1, 1 << 26) for cols in (1, 128)] + [((1 << 29) - 1, 129), ((1 << 17) - 1, 1 << 20)]
 
 
 @pytest.fixture(scope="module")
@@ -68,6 +84,14 @@ def test_parts_of_a_weight_gradient_are_summed(answers):
         assert len(got) == 1 or "k_add_parts" in got[1][0]
 
 
+def test_grids_hold_every_block_and_a_launch_s_threads(answers):
+    """A launch's dimension has fewer than 2^32 threads; 64 blocks of 128 columns, one of kernels' 256 threads."""
+    for rows, cols, got in answers["blocks"]:
+        (_, (x, y, z)), = got
+        assert x * 256 < 1 << 32 and y <= 65535 and z == 1, (rows, cols, got)
+        assert rows * ((cols + 127) // 128) <= 64 * x * y < rows * ((cols + 127) // 128) + (64 << 20), (rows, cols, got)
+
+
 if __name__ == "__main__":
     h = Host(sys.argv[1], sys.argv[2])
     h.train = h.ctx(1, 1, 1)
@@ -77,4 +101,5 @@ if __name__ == "__main__":
     out = {"products": [[m, n, k, name, lines(h, product, m, n, k, type)] for m, n, k in shapes for name, type in types],
            "weight_grads": [[t, n, k, name, lines(h, weight_grad, t, n, k, type)] for t in (8, 100, 1000, 3001, 8192, 40000) for n in N for k in (100, 1000, 4096, 16384)
                             for name, type in types]}
+    out["blocks"] = [[rows, cols, lines(h, call, rows, cols, type)] for rows, cols in BLOCKS for call in (quantize, dequantize, activate, activate_grad) for type in (FP32, BF16)]
     print(json.dumps(out))
