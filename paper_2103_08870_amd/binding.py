@@ -260,18 +260,28 @@ class Segments:
 
 class Blocks:
     """A matrix [rows][cols] in 8 bits: e4m3 codes (columns padded to a multiple of 128) and one exponent byte per row and
-    128 columns or, with ``tiles`` (weights), per 128 x 128.  Makes the two arrays, or takes a caller's."""
+    128 columns or, with ``tiles`` (weights), per 128 x 128.  Makes the two arrays, or takes a caller's; ``codes`` and ``exps``
+    may be exchanged for others that fit, sizes and form stay."""
 
     def __init__(self, rows: int, cols: int, tiles: bool = False, device="cuda", codes: Optional[torch.Tensor] = None,
                  exps: Optional[torch.Tensor] = None):
         wide = (cols + 127) // 128
-        self.rows, self.cols, self.tiles = rows, cols, tiles
-        shape = (rows, 128 * wide), ((rows + 127) // 128 if tiles else rows, (wide + 3) // 4 * 4)
-        self.codes = torch.empty(shape[0], dtype=torch.uint8, device=device) if codes is None else codes
-        self.exps = torch.empty(shape[1], dtype=torch.uint8, device=device) if exps is None else exps
-        for t, s in zip((self.codes, self.exps), shape):
-            _require(t.is_contiguous() and tuple(t.shape) == s and t.dtype == torch.uint8, f"an array of a Blocks is contiguous uint8 of shape {s}")
-        self.at = _ptr(self.codes), _ptr(self.exps)
+        self._rows, self._cols, self._tiles = rows, cols, tiles
+        self._shapes = (rows, 128 * wide), ((rows + 127) // 128 if tiles else rows, (wide + 3) // 4 * 4)
+        self._take(torch.empty(self._shapes[0], dtype=torch.uint8, device=device) if codes is None else codes,
+                   torch.empty(self._shapes[1], dtype=torch.uint8, device=device) if exps is None else exps)
+
+    rows, cols, tiles = (property(lambda self, name=name: getattr(self, name)) for name in ("_rows", "_cols", "_tiles"))
+    codes = property(lambda self: self._codes, lambda self, t: self._take(t, self._exps))
+    exps = property(lambda self: self._exps, lambda self, t: self._take(self._codes, t))
+
+    def _take(self, codes: torch.Tensor, exps: torch.Tensor) -> None:
+        for t, s in zip((codes, exps), self._shapes):
+            _require(isinstance(t, torch.Tensor) and t.is_contiguous() and tuple(t.shape) == s and t.dtype == torch.uint8,
+                     f"an array of a Blocks is contiguous uint8 of shape {s}")
+        at = _ptr(codes), _ptr(exps)
+        _require(all(t.untyped_storage().nbytes() >= t.storage_offset() + t.numel() for t in (codes, exps)), "an array of a Blocks has lost its memory")
+        self._codes, self._exps, self._at = codes, exps, at
 
 
 # ---------------------------------------------------------------------------- entry points
@@ -502,9 +512,12 @@ def _vector(t: Optional[torch.Tensor], n: int, what: str) -> Optional[int]:
 def _blocks(b: Optional[Blocks], rows: int, cols: int, what: str, tiles: bool = False):
     if b is None:
         return _NONE
-    if b.rows != rows or b.cols != cols or b.tiles != tiles:
+    if b._rows != rows or b._cols != cols or b._tiles != tiles:
         _refuse(f"{what} must be Blocks of {(rows, cols)} with an exponent per " + ("128 x 128" if tiles else "row and 128 columns"))
-    return b.at
+    at = b._codes.data_ptr(), b._exps.data_ptr()
+    if at != b._at:   # (a tensor's memory may have been exchanged since it was looked at)
+        b._take(b._codes, b._exps)
+    return at
 
 
 def lgc_codes_stride(cols: int) -> int:
@@ -538,8 +551,8 @@ def lgc_quantize_weights(ctx: Context, w: torch.Tensor, out: Blocks, transposed:
 def lgc_dequantize(ctx: Context, blocks: Blocks, out: torch.Tensor) -> None:
     """out [rows][cols] <- the values of blocks, exactly."""
     kind, rows, cols, at, ld = _own(out, "out")
-    codes, exps = _blocks(blocks, rows, cols, "blocks", blocks.tiles)
-    _check(lib().lgc_dequantize(ctx.h, codes, exps, 128 if blocks.tiles else 1, rows, cols, at, kind, ld, _stream()), ctx.h)
+    codes, exps = _blocks(blocks, rows, cols, "blocks", blocks._tiles)
+    _check(lib().lgc_dequantize(ctx.h, codes, exps, 128 if blocks._tiles else 1, rows, cols, at, kind, ld, _stream()), ctx.h)
 
 
 def lgc_layer_norm(ctx: Context, x: torch.Tensor, gamma: Optional[torch.Tensor], beta: Optional[torch.Tensor], eps: float,
@@ -592,13 +605,13 @@ def lgc_activate_grad(ctx: Context, act: str, dz: torch.Tensor, a_blocks: Blocks
 def lgc_product(ctx: Context, a: Blocks, b: Blocks, bias: Optional[torch.Tensor], y: torch.Tensor) -> None:
     """y [m][n] <- a [m][k] b [n][k]^T + bias [n]; b with an exponent per 128 x 128."""
     kind, m, n, at, ld = _own(y, "y")
-    a_codes, a_exps = _blocks(a, m, a.cols, "a")
-    b_codes, b_exps = _blocks(b, n, a.cols, "b", True)
-    _check(lib().lgc_product(ctx.h, a_codes, a_exps, m, b_codes, b_exps, n, a.cols, _vector(bias, n, "bias"), at, kind, ld, _stream()), ctx.h)
+    a_codes, a_exps = _blocks(a, m, a._cols, "a")
+    b_codes, b_exps = _blocks(b, n, a._cols, "b", True)
+    _check(lib().lgc_product(ctx.h, a_codes, a_exps, m, b_codes, b_exps, n, a._cols, _vector(bias, n, "bias"), at, kind, ld, _stream()), ctx.h)
 
 
 def lgc_weight_grad(ctx: Context, dy: torch.Tensor, x: Blocks, dw: torch.Tensor, db: Optional[torch.Tensor] = None) -> None:
     """dw [n][k] <- dy [rows][n]^T x [rows][k], db [n] <- the columns' sums of dy; dw anywhere in a flat fp32 gradient."""
     kind, rows, n, at, ld = _own(dy, "dy")
-    codes, exps = _blocks(x, rows, x.cols, "x")
-    _check(lib().lgc_weight_grad(ctx.h, at, kind, rows, n, ld, codes, exps, x.cols, _vector(dw, n * x.cols, "dw"), _vector(db, n, "db"), _stream()), ctx.h)
+    codes, exps = _blocks(x, rows, x._cols, "x")
+    _check(lib().lgc_weight_grad(ctx.h, at, kind, rows, n, ld, codes, exps, x._cols, _vector(dw, n * x._cols, "dw"), _vector(db, n, "db"), _stream()), ctx.h)
