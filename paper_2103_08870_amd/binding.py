@@ -614,4 +614,6 @@ def lgc_weight_grad(ctx: Context, dy: torch.Tensor, x: Blocks, dw: torch.Tensor,
     """dw [n][k] <- dy [rows][n]^T x [rows][k], db [n] <- the columns' sums of dy; dw anywhere in a flat fp32 gradient."""
     kind, rows, n, at, ld = _own(dy, "dy")
     codes, exps = _blocks(x, rows, x._cols, "x")
+    if dw is not None and dw.dim() == 2 and dw.shape != (n, x._cols):   # (as many elements, but rows of another length)
+        _refuse(f"dw must be {(n, x._cols)}, or flat")
     _check(lib().lgc_weight_grad(ctx.h, at, kind, rows, n, ld, codes, exps, x._cols, _vector(dw, n * x._cols, "dw"), _vector(db, n, "db"), _stream()), ctx.h)

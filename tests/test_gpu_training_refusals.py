@@ -79,3 +79,23 @@ def test_the_binding_refuses_tensors_that_do_not_fit(B):
         with pytest.raises(ValueError):
             call()
     ctx.close()
+
+
+def test_a_weight_gradient_laid_out_as_the_transpose_is_refused(B):
+    """dw is [n][k], or that many elements in a row: a matrix of another shape with as many elements would get its rows cut in the wrong places."""
+    ctx = B.Context(1, 1, 1)
+    B.lgc_reserve_training(ctx)
+    gen = torch.Generator().manual_seed(1)
+    dy, b = torch.randn((4, 64), generator=gen).cuda(), B.Blocks(4, 200)
+    B.lgc_quantize(ctx, torch.randn((4, 200), generator=gen).cuda(), b)
+    for shape in ((200, 64), (128, 100), (1, 12800), (12800, 1)):
+        dw = torch.full(shape, 7.0, device="cuda")
+        with pytest.raises(ValueError):
+            B.lgc_weight_grad(ctx, dy, b, dw)
+        torch.cuda.synchronize()
+        assert bool((dw == 7.0).all())
+    same = [torch.empty(shape, device="cuda") for shape in ((64, 200), (12800,), (64, 8, 25), (2, 32, 200))]
+    for dw in same:
+        B.lgc_weight_grad(ctx, dy, b, dw)
+        assert torch.equal(dw.view(64, 200), same[0]) and bool(dw.any())
+    ctx.close()
