@@ -10,7 +10,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 if HERE not in sys.path:
     sys.path.insert(0, HERE)
 from test_host_routes import Host, ROOT   # noqa: E402,F401  (puts the repository's root in sys.path)
-from test_training_routes import AT, BF16, FP32, product, quantize, u64, weight_grad   # noqa: E402
+import test_gpu_training_reach as reach   # noqa: E402
+from test_training_routes import AT, BF16, FP32, launches, layer_norm, layer_norm_grad, product, quantize, u64, weight_grad   # noqa: E402
 
 # rows from one to many, widths that models have and others, sums short and long: either side of every rule of launch_product
 M = [1, 16, 17, 64, 65, 128, 129, 160, 257, 280, 300, 400, 513, 641, 700, 900, 1100, 2000, 2049, 4100, 8192]
@@ -92,6 +93,20 @@ def test_grids_hold_every_block_and_a_launch_s_threads(answers):
         assert rows * ((cols + 127) // 128) <= 64 * x * y < rows * ((cols + 127) // 128) + (64 << 20), (rows, cols, got)
 
 
+def test_sizes_of_the_tests_reach_the_kernels_that_they_are_meant_for(answers):
+    for rows, cols, want, got in answers["norms"]:
+        (name, (blocks, _, _)), = got
+        assert name == want and blocks * (4 if " 64 " in want else 1) < rows, (rows, cols, got)
+    for rows, cols, want, got in answers["norm_grads"]:
+        blocks = [grid[1 if "columns" in want else 0] for name, grid in got if name.startswith(want)]
+        assert len(blocks) == 1 and blocks[0] < rows, (rows, cols, got)
+    for rows, n, k, want, got in answers["reach"]:
+        assert got[0][0].startswith(want), (rows, n, k, got)
+    for got in answers["groups"]:
+        (name, (x, y, z)), = got
+        assert name.split()[-1] == "4" and 64 * x - 63 <= 36891 < 64 * x, got
+
+
 if __name__ == "__main__":
     h = Host(sys.argv[1], sys.argv[2])
     h.train = h.ctx(1, 1, 1)
@@ -102,4 +117,8 @@ if __name__ == "__main__":
            "weight_grads": [[t, n, k, name, lines(h, weight_grad, t, n, k, type)] for t in (8, 100, 1000, 3001, 8192, 40000) for n in N for k in (100, 1000, 4096, 16384)
                             for name, type in types]}
     out["blocks"] = [[rows, cols, lines(h, call, rows, cols, type)] for rows, cols in BLOCKS for call in (quantize, dequantize, activate, activate_grad) for type in (FP32, BF16)]
+    out["norms"] = [[rows, cols, want, launches(h, layer_norm, (rows, cols, type))[1]] for (rows, cols), want in reach.NORMS.items() for type in (FP32, BF16)]
+    out["norm_grads"] = [[rows, cols, want, launches(h, layer_norm_grad, (rows, cols, type))[1]] for (rows, cols), want in reach.NORM_GRADS.items() for type in (FP32, BF16)]
+    out["reach"] = [[*shape, want, launches(h, weight_grad, (*shape, type))[1]] for shape, want in reach.WEIGHT_GRADS.items() for type in (FP32, BF16)]
+    out["groups"] = [launches(h, call, (*reach.GROUPS, type))[1] for call in (quantize, dequantize, activate, activate_grad) for type in (FP32, BF16)]
     print(json.dumps(out))
