@@ -416,7 +416,9 @@ lgc_status lgc_layer_norm_grad(lgc_ctx *ctx, const void *dy, uint64_t ld_dy, con
                                uint64_t ld_dx, float *dgamma, float *dbeta, void *stream);
 
 /* z <- f(a) elementwise; a in 8 bits (the checkpoint) and z in 8 bits (for the next
- * product).  Any of the three outputs may be NULL (codes with its exps). */
+ * product).  Any of the three outputs may be NULL (codes with its exps).  In fp32, off
+ * by 1e-6 of the result from a = -2 on (LGC_GELU; LGC_SILU 3e-7), in the tail by some
+ * a^2 2^-24 (LGC_SILU |a| 2^-24) of it. */
 lgc_status lgc_activate(lgc_ctx *ctx, lgc_act act, const void *a, lgc_type type, uint64_t rows, uint64_t cols, uint64_t ld,
                         void *z, uint64_t ld_z, uint8_t *a_codes, uint8_t *a_exps, uint8_t *z_codes, uint8_t *z_exps,
                         void *stream);
@@ -434,8 +436,9 @@ lgc_status lgc_activate_grad(lgc_ctx *ctx, lgc_act act, const void *dz, lgc_type
  * that lgc_quantize_weights makes.  Precision by the type of y.  LGC_BF16: the
  * matrix cores' products of 8-bit codes, which add eight neighbouring products with
  * some 14 bits below the largest and go on in fp32; about 2^-16 of the result for
- * inputs of one size, below what rounding to bf16 costs.  LGC_FP32: exact products,
- * added in fp32, at a lower rate.
+ * inputs of one size, below what rounding to bf16 costs.  Where large products
+ * cancel, the loss is 2^-16 of these, not of what is left.  LGC_FP32: exact products,
+ * added in fp32, at a lower rate, for such sums too.
  */
 lgc_status lgc_product(lgc_ctx *ctx, const uint8_t *a_codes, const uint8_t *a_exps, uint64_t m, const uint8_t *b_codes,
                        const uint8_t *b_exps, uint64_t n, uint64_t k, const float *bias, void *y, lgc_type type, uint64_t ld,

@@ -64,7 +64,7 @@ __device__ __forceinline__ void each(F &&f) { each_of(std::make_integer_sequence
 // 128 x 128: 940 us, with two of 128 x 64 890, though these read half as much again; 4096 cubed 142 and 125).
 // LDS rows lie a multiple of 256 bytes apart; pieces of 32 bytes are exchanged within a row by (row & 3), so that these four rows meet all banks.
 //
-// Bound by the matrix instructions and LDS where rows are many (8192 x 4096 x 16384, dy in bf16: 865 - 890 us, 1.25 PFLOP/s), by the stores of dw where they are few
+// Bound by the matrix instructions and LDS where rows are many (8192 x 4096 x 16384, dy in bf16: 865 - 897 us, 1.25 PFLOP/s), by the stores of dw where they are few
 // (32 x 8192 x 8192: 46 us, 5.9 TB/s of dw), and between by the time that a tile's first rows take to come and its sums to leave (3001 x 777 x 1300: 22.3 us).
 //
 // kTeams teams of kTeam wavefronts do this for a part of the block's rows each, and their sums meet in LDS: with small tiles, two teams of four are those two wavefronts
@@ -405,7 +405,8 @@ void launch_weight_grad(const void *dy, lgc_type type, uint32_t rows, uint32_t n
     // Large tiles where small ones would not all be resident, two per compute unit, and rows make more than two steps (us, small / large: 32 x 8192 x 8192 46 / 58,
     // 94 x 7539 x 8192 62 / 67, 200 x 8192 x 8192 89 / 86, 600 x 8192 x 8192 142 / 120, 2000 x 2500 x 4096 69 / 60, 4096 x 4096 x 4864 203 / 204, 8192 x 4096 x 16384
     // 1216 / 890), and where they fill two thirds of the compute units with parts of 2048 rows (8192 x 2000 x 2500 128 / 95, 16384 x 1500 x 1500 108 / 90,
-    // 16384 x 2048 x 2048 157 / 147, 8192 x 2048 x 2048 82 / 85, 2000 x 1500 x 3500 40 / 46), unless small ones fill all, two per unit (8192 x 2048 x 4096 149 / 172);
+    // 16384 x 2048 x 2048 149 / 132, with db, for which the scratch holds a part less, 149 / 142; 2000 x 1500 x 3500 40 / 46; the rule's edge, 8192 x 2048 x 2048, goes large
+    // all the same, 77 / 81: in three parts with db, which leave a quarter of the compute units idle), unless small ones fill all, two per unit (8192 x 2048 x 4096 149 / 172);
     // never where half of a large tile would lie beyond dw (4096 x 32768 x 100 62 / 90, but x 384 142 / 133)
     const uint64_t small = tiles(128), most_parts = (uint64_t)cus / tiles(256);
     const bool large = type == LGC_BF16 && 2 * tiles(256) < small && (small > 2 * (uint64_t)cus ? rows > 128 : small < 2 * (uint64_t)cus && rows >= 2048 * most_parts && 3 * most_parts * tiles(256) >= 2 * (uint64_t)cus);
