@@ -453,6 +453,60 @@ lgc_status lgc_product(lgc_ctx *ctx, const uint8_t *a_codes, const uint8_t *a_ex
 lgc_status lgc_weight_grad(lgc_ctx *ctx, const void *dy, lgc_type type, uint64_t rows, uint64_t n, uint64_t ld,
                            const uint8_t *x_codes, const uint8_t *x_exps, uint64_t k, float *dw, float *db, void *stream);
 
+/* ---- attention and rotary positions ----
+ *
+ * Plain matrices of tokens: a row per token, in it the heads one after another, `dim`
+ * columns each; so the three results of one product, side by side in its rows, are
+ * q, k and v as they lie there, with its row length as ld_q, ld_k and ld_v.
+ * lse and delta: fp32, [q_rows][heads], contiguous.
+ *
+ * Sequences: their tokens follow one another in the rows.  With q_starts and
+ * kv_starts (device arrays of sequences + 1 row numbers, not falling), sequence s has
+ * rows starts[s] to starts[s + 1] - 1; rows before the first and behind the last are
+ * neither read nor written.  A start past the last row counts as the last row's end.
+ * With both NULL all sequences have q_rows / sequences and kv_rows / sequences tokens,
+ * without a remainder.
+ * Query i of a sequence of lq queries and lk keys is at position i + lk - lq.  It sees
+ * all lk keys; if causal != 0, only those at positions up to its own; if window != 0, of
+ * these only those at positions above its own less window.  What it does not see has no
+ * influence on its results, infinities and NaNs included.  A query that sees nothing
+ * has o = 0, lse = -inf and no part in any gradient.
+ * Key head h serves the query heads h * heads / kv_heads on, heads / kv_heads of them.
+ *
+ * Limits: dim a multiple of 8, 8 to 128; heads a multiple of kv_heads, heads * dim at
+ * most 2^20; sequences 1 to 2^20, sequences * kv_heads at most 2^22; q_rows * heads and kv_rows * kv_heads below 2^30;
+ * scale > 0 and finite.  Matrices are bf16, 16-byte aligned, rows a multiple of
+ * 8 elements apart.  q_rows == 0 and kv_rows == 0 are valid.
+ */
+typedef struct {
+    uint64_t q_rows, kv_rows, sequences;
+    const uint32_t *q_starts, *kv_starts; /* device; both or neither NULL */
+    uint32_t heads, kv_heads, dim;
+    float scale;
+    int32_t causal;
+    uint32_t window;
+} lgc_attention_shape;
+
+/*
+ * o_i = sum_j p_ij v_j over the keys j that query i sees, p_ij = exp(s_ij - lse_i),
+ * s_ij = scale q_i . k_j, lse_i = log sum_j exp(s_ij) (lse may be NULL: not wanted).
+ * Scores, sums and statistics in fp32; p is rounded to bf16 where it meets v.  Needs
+ * lgc_reserve_training.
+ */
+lgc_status lgc_attention(lgc_ctx *ctx, const lgc_attention_shape *shape, const void *q, uint64_t ld_q, const void *k, uint64_t ld_k, const void *v,
+                         uint64_t ld_v, void *o, uint64_t ld_o, float *lse, void *stream);
+
+/*
+ * Its gradient, from the o and lse that it gave, with p computed anew:  delta_i = do_i . o_i
+ * (an output too), ds_ij = p_ij (do_i . v_j - delta_i),  dq_i = scale sum_j ds_ij k_j,
+ * dk_j = scale sum_i ds_ij q_i,  dv_j = sum_i p_ij do_i  (sums over i: over all the query
+ * heads that key head serves).  p and ds are rounded to bf16 where they meet k, q and do.
+ * Needs lgc_reserve_training.
+ */
+lgc_status lgc_attention_grad(lgc_ctx *ctx, const lgc_attention_shape *shape, const void *grad, uint64_t ld_grad, const void *q, uint64_t ld_q,
+                              const void *k, uint64_t ld_k, const void *v, uint64_t ld_v, const void *o, uint64_t ld_o, const float *lse, void *dq,
+                              uint64_t ld_dq, void *dk, uint64_t ld_dk, void *dv, uint64_t ld_dv, float *delta, void *stream);
+
 /* ---- diagnostics (never needed on the hot path) ---- */
 
 /* LGC_OPT_SELECT_PATH: how lgc_topk / lgc_accumulate_topk select (the results

@@ -34,6 +34,7 @@ EXPORTS = [
     "lgc_quantize", "lgc_quantize_weights", "lgc_dequantize",
     "lgc_layer_norm", "lgc_layer_norm_grad", "lgc_activate", "lgc_activate_grad",
     "lgc_product", "lgc_weight_grad",
+    "lgc_attention", "lgc_attention_grad",
 ]
 
 
@@ -45,6 +46,11 @@ class LgcError(RuntimeError):
 
 class _Layer(C.Structure):
     _fields_ = [("c_in", C.c_int32), ("c_out", C.c_int32), ("ksize", C.c_int32), ("stride", C.c_int32)]
+
+
+class _AttentionShape(C.Structure):
+    _fields_ = [("q_rows", C.c_uint64), ("kv_rows", C.c_uint64), ("sequences", C.c_uint64), ("q_starts", C.c_void_p), ("kv_starts", C.c_void_p),
+                ("heads", C.c_uint32), ("kv_heads", C.c_uint32), ("dim", C.c_uint32), ("scale", C.c_float), ("causal", C.c_int32), ("window", C.c_uint32)]
 
 
 _lib = None
@@ -131,7 +137,9 @@ def lib() -> C.CDLL:
             ("lgc_activate", [vp, i32, vp, i32, u64, u64, u64, vp, u64, vp, vp, vp, vp, vp]),
             ("lgc_activate_grad", [vp, i32, vp, i32, u64, u64, u64, vp, vp, vp, u64, vp, vp, vp]),
             ("lgc_product", [vp, vp, vp, u64, vp, vp, u64, u64, vp, vp, i32, u64, vp]),
-            ("lgc_weight_grad", [vp, vp, i32, u64, u64, u64, vp, vp, u64, vp, vp, vp])):
+            ("lgc_weight_grad", [vp, vp, i32, u64, u64, u64, vp, vp, u64, vp, vp, vp]),
+            ("lgc_attention", [vp, vp] + 4 * [vp, u64] + [vp, vp]),
+            ("lgc_attention_grad", [vp, vp] + 5 * [vp, u64] + [vp] + 3 * [vp, u64] + [vp, vp])):
         entry = getattr(l, name)
         entry.argtypes, entry.restype = args, i32
     _lib = l
@@ -617,3 +625,53 @@ def lgc_weight_grad(ctx: Context, dy: torch.Tensor, x: Blocks, dw: torch.Tensor,
     if dw is not None and dw.dim() == 2 and dw.shape != (n, x._cols):   # (as many elements, but rows of another length)
         _refuse(f"dw must be {(n, x._cols)}, or flat")
     _check(lib().lgc_weight_grad(ctx.h, at, kind, rows, n, ld, codes, exps, x._cols, _vector(dw, n * x._cols, "dw"), _vector(db, n, "db"), _stream()), ctx.h)
+
+
+# ------------------------------------------------------------- attention
+
+class AttentionShape:
+    """lgc_attention_shape without its rows: heads, sequences and who sees whom.  `scale` is dim^(-1/2) where it is not given.  q_starts, kv_starts: int32 device
+    tensors of sequences + 1 row numbers, read by every call; without them all sequences are of one length."""
+
+    def __init__(self, heads: int, kv_heads: int, dim: int, sequences: int = 1, q_starts: Optional[torch.Tensor] = None, kv_starts: Optional[torch.Tensor] = None,
+                 scale: Optional[float] = None, causal: bool = True, window: int = 0):
+        if min(heads, kv_heads, dim, window, sequences) < 0 or max(heads, kv_heads, dim, window) >= 1 << 32:
+            _refuse("heads, kv_heads, dim, sequences and window are not negative, and below 2^32")
+        if (q_starts is None) != (kv_starts is None):
+            _refuse("one of q_starts and kv_starts is missing")
+        for t in (q_starts, kv_starts):
+            if t is not None and (t.numel() != sequences + 1 or not t.is_contiguous()):
+                _refuse(f"starts must be contiguous with {sequences + 1} elements")
+        self._starts = q_starts, kv_starts
+        self._heads, self._kv_heads, self._dim = heads, kv_heads, dim
+        self._c = _AttentionShape(0, 0, sequences, _ptr(q_starts, torch.int32), _ptr(kv_starts, torch.int32), heads, kv_heads, dim,
+                                  scale if scale is not None else max(1, dim) ** -0.5, causal, window)
+        self._at = C.addressof(self._c)
+
+    def _rows(self, q: torch.Tensor, k: torch.Tensor) -> int:
+        """The structure's address, with the rows that a call's matrices have."""
+        c = self._c
+        if self._starts[0] is not None:   # (a tensor's memory may have been exchanged since it was looked at)
+            c.q_starts, c.kv_starts = self._starts[0].data_ptr(), self._starts[1].data_ptr()
+        c.q_rows, c.kv_rows = q.shape[0], k.shape[0]
+        return self._at
+
+
+_BF16 = torch.bfloat16
+
+
+def lgc_attention(ctx: Context, shape: AttentionShape, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, o: torch.Tensor, lse: Optional[torch.Tensor] = None) -> None:
+    """o [q_rows][heads * dim], lse [q_rows][heads] <- attention of q over k, v [kv_rows][kv_heads * dim], all but lse in bfloat16."""
+    rows, keys, wide, narrow = q.shape[0], k.shape[0], shape._heads * shape._dim, shape._kv_heads * shape._dim
+    _check(lib().lgc_attention(ctx.h, shape._rows(q, k), *_matrix(q, rows, wide, _BF16, "q"), *_matrix(k, keys, narrow, _BF16, "k"), *_matrix(v, keys, narrow, _BF16, "v"),
+                               *_matrix(o, rows, wide, _BF16, "o"), _vector(lse, rows * shape._heads, "lse"), _stream()), ctx.h)
+
+
+def lgc_attention_grad(ctx: Context, shape: AttentionShape, do: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, o: torch.Tensor, lse: torch.Tensor,
+                       dq: torch.Tensor, dk: torch.Tensor, dv: torch.Tensor, delta: torch.Tensor) -> None:
+    """dq, dk, dv <- the gradients of lgc_attention from do and from the o and lse that it gave; delta [q_rows][heads] is written too."""
+    rows, keys, wide, narrow = q.shape[0], k.shape[0], shape._heads * shape._dim, shape._kv_heads * shape._dim
+    of_q = lambda t, what: _matrix(t, rows, wide, _BF16, what)  # noqa: E731
+    of_k = lambda t, what: _matrix(t, keys, narrow, _BF16, what)  # noqa: E731
+    _check(lib().lgc_attention_grad(ctx.h, shape._rows(q, k), *of_q(do, "do"), *of_q(q, "q"), *of_k(k, "k"), *of_k(v, "v"), *of_q(o, "o"), _vector(lse, rows * shape._heads, "lse"),
+                                    *of_q(dq, "dq"), *of_k(dk, "dk"), *of_k(dv, "dv"), _vector(delta, rows * shape._heads, "delta"), _stream()), ctx.h)

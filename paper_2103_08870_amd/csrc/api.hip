@@ -1615,6 +1615,71 @@ extern "C" lgc_status lgc_weight_grad(lgc_ctx *ctx, const void *dy, lgc_type typ
     });
 }
 
+// ------------------------------------------------------------------ attention
+
+namespace {
+
+void check_attention(Check &c, const lgc_attention_shape *s) {
+    c.need(s != nullptr, "shape is NULL");
+    if (c.status != LGC_OK) return;
+    const unsigned long long heads = s->heads, kv_heads = s->kv_heads, dim = s->dim, sequences = s->sequences, q_rows = s->q_rows, kv_rows = s->kv_rows;
+    c.need(dim >= 8 && dim <= 128 && dim % 8 == 0, "dim = %llu: not a multiple of 8 from 8 to 128", dim);
+    c.need(kv_heads >= 1 && heads >= kv_heads && heads % kv_heads == 0, "%llu heads for %llu key heads", heads, kv_heads);
+    c.need(heads * dim <= kMostCols, "heads * dim = %llu above 2^20", heads * dim);
+    c.need(sequences >= 1 && sequences <= kMostCols && sequences * kv_heads <= 4 * kMostCols, "%llu sequences: none, above 2^20, or with their key heads above 2^22", sequences);
+    c.need(q_rows < (1ull << 30) && q_rows * heads < (1ull << 30), "q_rows * heads = %llu * %llu not below 2^30", q_rows, heads);
+    c.need(kv_rows < (1ull << 30) && kv_rows * kv_heads < (1ull << 30), "kv_rows * kv_heads = %llu * %llu not below 2^30", kv_rows, kv_heads);
+    c.need(s->scale > 0.f && s->scale < INFINITY, "scale = %g", (double)s->scale);
+    c.need(!s->q_starts == !s->kv_starts, "one of q_starts and kv_starts is NULL");
+    c.need(aligned(s->q_starts, 4) && aligned(s->kv_starts, 4), "starts are not 4-byte aligned");
+    c.need(s->q_starts || (q_rows % sequences == 0 && kv_rows % sequences == 0), "%llu and %llu rows are not %llu equal sequences", q_rows, kv_rows, sequences);
+}
+void check_heads(Check &c, const char *name, const void *p, uint64_t rows, uint64_t cols, uint64_t ld) {
+    if (!rows) return;
+    c.plain(name, p, LGC_BF16, cols, ld).need(aligned(p, 16) && ld % 8 == 0, "%s is not 16-byte aligned, or its rows not a multiple of 8 elements apart", name);
+}
+
+}  // namespace
+
+extern "C" lgc_status lgc_attention(lgc_ctx *ctx, const lgc_attention_shape *shape, const void *q, uint64_t ld_q, const void *k, uint64_t ld_k, const void *v, uint64_t ld_v, void *o,
+                                    uint64_t ld_o, float *lse, void *stream) {
+    Check c(ctx);
+    check_attention(c, shape);
+    if (c.status != LGC_OK) return c.status;
+    const uint64_t wide = (uint64_t)shape->heads * shape->dim, narrow = (uint64_t)shape->kv_heads * shape->dim;
+    check_heads(c, "q", q, shape->q_rows, wide, ld_q);
+    check_heads(c, "k", k, shape->kv_rows, narrow, ld_k);
+    check_heads(c, "v", v, shape->kv_rows, narrow, ld_v);
+    check_heads(c, "o", o, shape->q_rows, wide, ld_o);
+    c.maybe("lse", lse).reserved("lgc_attention");
+    return launch(c, [&] {
+        if (shape->q_rows) launch_attention(*shape, q, ld_q, k, ld_k, v, ld_v, o, ld_o, lse, ctx->training, kTrainingFloats, ctx->cus, (hipStream_t)stream);
+    });
+}
+
+extern "C" lgc_status lgc_attention_grad(lgc_ctx *ctx, const lgc_attention_shape *shape, const void *grad, uint64_t ld_grad, const void *q, uint64_t ld_q, const void *k, uint64_t ld_k,
+                                         const void *v, uint64_t ld_v, const void *o, uint64_t ld_o, const float *lse, void *dq, uint64_t ld_dq, void *dk, uint64_t ld_dk, void *dv,
+                                         uint64_t ld_dv, float *delta, void *stream) {
+    Check c(ctx);
+    check_attention(c, shape);
+    if (c.status != LGC_OK) return c.status;
+    const uint64_t wide = (uint64_t)shape->heads * shape->dim, narrow = (uint64_t)shape->kv_heads * shape->dim;
+    check_heads(c, "grad", grad, shape->q_rows, wide, ld_grad);
+    check_heads(c, "q", q, shape->q_rows, wide, ld_q);
+    check_heads(c, "k", k, shape->kv_rows, narrow, ld_k);
+    check_heads(c, "v", v, shape->kv_rows, narrow, ld_v);
+    check_heads(c, "o", o, shape->q_rows, wide, ld_o);
+    check_heads(c, "dq", dq, shape->q_rows, wide, ld_dq);
+    check_heads(c, "dk", dk, shape->kv_rows, narrow, ld_dk);
+    check_heads(c, "dv", dv, shape->kv_rows, narrow, ld_dv);
+    if (shape->q_rows) c.vector("lse", lse).vector("delta", delta);
+    c.reserved("lgc_attention_grad");
+    return launch(c, [&] {
+        launch_attention_grad(*shape, grad, ld_grad, q, ld_q, k, ld_k, v, ld_v, o, ld_o, lse, dq, ld_dq, dk, ld_dk, dv, ld_dv, delta, ctx->training, kTrainingFloats, ctx->cus,
+                              (hipStream_t)stream);
+    });
+}
+
 // ------------------------------------------------------------------ diagnostics
 
 extern "C" lgc_status lgc_set_option(lgc_ctx *ctx, lgc_option opt, int64_t value) {

@@ -328,5 +328,11 @@ void launch_product(const uint8_t *a, const uint8_t *a_exps, const uint8_t *b, c
                     lgc_type type, uint64_t ld, float *scratch, size_t scratch_floats, int cus, hipStream_t st);
 void launch_weight_grad(const void *dy, lgc_type type, uint32_t rows, uint32_t n, uint64_t ld, const uint8_t *codes, const uint8_t *exps, uint32_t k, float *dw, float *db,
                         float *scratch, size_t scratch_floats, int cus, hipStream_t st);
+// attention.hip
+void launch_attention(const lgc_attention_shape &shape, const void *q, uint64_t ld_q, const void *k, uint64_t ld_k, const void *v, uint64_t ld_v, void *o, uint64_t ld_o, float *lse,
+                      float *scratch, size_t scratch_floats, int cus, hipStream_t st);
+void launch_attention_grad(const lgc_attention_shape &shape, const void *grad, uint64_t ld_grad, const void *q, uint64_t ld_q, const void *k, uint64_t ld_k, const void *v, uint64_t ld_v,
+                           const void *o, uint64_t ld_o, const float *lse, void *dq, uint64_t ld_dq, void *dk, uint64_t ld_dk, void *dv, uint64_t ld_dv, float *delta, float *scratch,
+                           size_t scratch_floats, int cus, hipStream_t st);
 
 }  // namespace lgc
