@@ -364,7 +364,7 @@ lgc_status lgc_reserve(lgc_ctx *ctx, const lgc_ae *ae /* nullable */, uint64_t k
  */
 
 typedef enum { LGC_FP32 = 0, LGC_BF16 = 1 } lgc_type;
-typedef enum { LGC_RELU = 0, LGC_GELU = 1 /* with the normal distribution's function */, LGC_SILU = 2 } lgc_act;
+typedef enum { LGC_RELU = 0, LGC_GELU = 1 /* with the normal distribution's function */, LGC_SILU = 2, LGC_LINEAR = 3 /* lgc_product_activate only */ } lgc_act;
 
 /* bytes from row to row of the codes and of the exponents of a matrix of `cols` columns (0 for 0) */
 uint64_t lgc_codes_stride(uint64_t cols);
@@ -445,6 +445,19 @@ lgc_status lgc_product(lgc_ctx *ctx, const uint8_t *a_codes, const uint8_t *a_ex
                        void *stream);
 
 /*
+ * The same product with what follows it in one call:  t = a b^T + bias,
+ * z = f(t) + residual (act: LGC_LINEAR: z = t + residual; residual [m][n], NULL: 0),
+ * rounded once.  z: plain; t in 8 bits (the checkpoint that lgc_activate_grad reads) and
+ * z in 8 bits (for the next product; not with a residual): an exponent per row and 128
+ * columns.  Any of the three may be NULL.  residual has z's type, by which precision goes
+ * as with lgc_product (also where z is NULL), f's as with lgc_activate.  The residual may be z itself.
+ * Needs lgc_reserve_training.
+ */
+lgc_status lgc_product_activate(lgc_ctx *ctx, const uint8_t *a_codes, const uint8_t *a_exps, uint64_t m, const uint8_t *b_codes, const uint8_t *b_exps,
+                                uint64_t n, uint64_t k, const float *bias, lgc_act act, const void *residual, uint64_t ld_residual, void *z,
+                                lgc_type type, uint64_t ld, uint8_t *t_codes, uint8_t *t_exps, uint8_t *z_codes, uint8_t *z_exps, void *stream);
+
+/*
  * dw[n][k] = sum over rows t of dy[t][n] x[t][k] and db[n] = sum over rows of dy[t][n]
  * (NULL: not wanted): the gradient of a linear layer's weights and bias, from dy as it
  * is and the layer's input in 8 bits (an exponent per row and 128 columns).  dw is
@@ -453,7 +466,34 @@ lgc_status lgc_product(lgc_ctx *ctx, const uint8_t *a_codes, const uint8_t *a_ex
 lgc_status lgc_weight_grad(lgc_ctx *ctx, const void *dy, lgc_type type, uint64_t rows, uint64_t n, uint64_t ld,
                            const uint8_t *x_codes, const uint8_t *x_exps, uint64_t k, float *dw, float *db, void *stream);
 
-/* ---- attention and rotary positions ----
+/* ---- rotary positions ---- */
+
+/* which columns of a head turn together: i and i + dims / 2, or 2 i and 2 i + 1 */
+typedef enum { LGC_HALVES = 0, LGC_NEIGHBOURS = 1 } lgc_pairs;
+
+/*
+ * freqs (HOST memory, [dims / 2]) <- radians per position, f_i = base^(-2 i / dims), for
+ * contexts `factor` times as long as they were trained on:  f_i (w + (1 - w) / factor),
+ * w = (turns - low) / (high - low) held to [0, 1], turns = length f_i / 2 pi those of a
+ * context of the trained length.  length == 0: w = 0, every frequency is divided by
+ * factor (1: none is changed).  Needs no context.
+ */
+lgc_status lgc_rotary_frequencies(double *freqs, uint32_t dims, double base, double factor, double length, double low, double high);
+
+/*
+ * Every head's first `dims` columns turned pair by pair, by the angle t = position * freqs[i]:
+ * (a, b) -> amplitude (a cos t - b sin t, a sin t + b cos t); the other columns are copied.
+ * inverse != 0: by -t, which is the gradient: dx from dy.  x, y: [rows][heads * dim], a row per
+ * token and the heads one after another (queries and keys, side by side, in one call); y may be x, with
+ * the same distance from row to row, and overlaps it in no other way.  positions: device [rows], any sign (NULL: row modulo
+ * period; 0: the row).  freqs: device [dims / 2].  dims: even, 2 to dim.  Angles are worked out in 64 bits, so that far positions
+ * keep their precision, the rest in fp32, rounded once.  rows below 2^24.
+ */
+lgc_status lgc_rotate(lgc_ctx *ctx, const void *x, lgc_type type, uint64_t rows, uint64_t ld, uint32_t heads, uint32_t dim, const int32_t *positions,
+                      uint64_t period, const double *freqs, uint32_t dims, lgc_pairs pairs, float amplitude, int inverse, void *y, uint64_t ld_y,
+                      void *stream);
+
+/* ---- attention ----
  *
  * Plain matrices of tokens: a row per token, in it the heads one after another, `dim`
  * columns each; so the three results of one product, side by side in its rows, are

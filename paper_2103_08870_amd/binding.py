@@ -18,7 +18,8 @@ LIB_PATH = os.path.join(_HERE, "liblgc.so")
 
 LGC_OK, LGC_EINVAL, LGC_ENOMEM, LGC_EHIP, LGC_EDEVICE = range(5)
 LGC_FP32, LGC_BF16 = 0, 1
-LGC_RELU, LGC_GELU, LGC_SILU = 0, 1, 2
+LGC_RELU, LGC_GELU, LGC_SILU, LGC_LINEAR = 0, 1, 2, 3
+LGC_HALVES, LGC_NEIGHBOURS = 0, 1
 LGC_OPT_SELECT_PATH, LGC_OPT_PROFILE, LGC_OPT_CARRY_THRESHOLD = 0, 1, 2
 
 EXPORTS = [
@@ -33,8 +34,8 @@ EXPORTS = [
     "lgc_codes_stride", "lgc_exps_stride", "lgc_reserve_training",
     "lgc_quantize", "lgc_quantize_weights", "lgc_dequantize",
     "lgc_layer_norm", "lgc_layer_norm_grad", "lgc_activate", "lgc_activate_grad",
-    "lgc_product", "lgc_weight_grad",
-    "lgc_attention", "lgc_attention_grad",
+    "lgc_product", "lgc_product_activate", "lgc_weight_grad",
+    "lgc_rotary_frequencies", "lgc_rotate", "lgc_attention", "lgc_attention_grad",
 ]
 
 
@@ -138,6 +139,9 @@ def lib() -> C.CDLL:
             ("lgc_activate_grad", [vp, i32, vp, i32, u64, u64, u64, vp, vp, vp, u64, vp, vp, vp]),
             ("lgc_product", [vp, vp, vp, u64, vp, vp, u64, u64, vp, vp, i32, u64, vp]),
             ("lgc_weight_grad", [vp, vp, i32, u64, u64, u64, vp, vp, u64, vp, vp, vp]),
+            ("lgc_product_activate", [vp, vp, vp, u64, vp, vp, u64, u64, vp, i32, vp, u64, vp, i32, u64, vp, vp, vp, vp, vp]),
+            ("lgc_rotary_frequencies", [vp, C.c_uint32] + 5 * [C.c_double]),
+            ("lgc_rotate", [vp, vp, i32, u64, u64, C.c_uint32, C.c_uint32, vp, u64, vp, C.c_uint32, i32, f32, i32, vp, u64, vp]),
             ("lgc_attention", [vp, vp] + 4 * [vp, u64] + [vp, vp]),
             ("lgc_attention_grad", [vp, vp] + 5 * [vp, u64] + [vp] + 3 * [vp, u64] + [vp, vp])):
         entry = getattr(l, name)
@@ -470,7 +474,7 @@ def lgc_profile_read(ctx: Context) -> Tuple[float, int]:
 _TYPES = {torch.float32: LGC_FP32, torch.bfloat16: LGC_BF16}
 _ACTS = {"relu": LGC_RELU, "gelu": LGC_GELU, "silu": LGC_SILU}
 _NONE = None, None
-_FP32 = torch.float32
+_FP32, _BF16 = torch.float32, torch.bfloat16
 
 
 def _refuse(what: str):
@@ -618,6 +622,23 @@ def lgc_product(ctx: Context, a: Blocks, b: Blocks, bias: Optional[torch.Tensor]
     _check(lib().lgc_product(ctx.h, a_codes, a_exps, m, b_codes, b_exps, n, a._cols, _vector(bias, n, "bias"), at, kind, ld, _stream()), ctx.h)
 
 
+def lgc_product_activate(ctx: Context, a: Blocks, b: Blocks, bias: Optional[torch.Tensor], act: Optional[str] = None, residual: Optional[torch.Tensor] = None,
+                         z: Optional[torch.Tensor] = None, t_blocks: Optional[Blocks] = None, z_blocks: Optional[Blocks] = None) -> None:
+    """t = a [m][k] b [n][k]^T + bias [n]; z, z_blocks (z in 8 bits) <- f(t) + residual, t_blocks (t in 8 bits, for lgc_activate_grad) <- t; act: None (z = t + residual),
+    "relu", "gelu" or "silu".  What is None is left out; without z, in bfloat16's precision."""
+    m, n = a._rows, b._rows
+    out, ld, kind = None, 0, LGC_BF16
+    if z is not None:
+        kind, rows, cols, out, ld = _own(z, "z")
+        if rows != m or cols != n:
+            _refuse(f"z must be {(m, n)}")
+    other, ld_other = _matrix(residual, m, n, z.dtype if z is not None else _BF16, "residual")
+    a_codes, a_exps = _blocks(a, m, a._cols, "a")
+    b_codes, b_exps = _blocks(b, n, a._cols, "b", True)
+    _check(lib().lgc_product_activate(ctx.h, a_codes, a_exps, m, b_codes, b_exps, n, a._cols, _vector(bias, n, "bias"), LGC_LINEAR if act is None else _act(act), other, ld_other,
+                                      out, kind, ld, *_blocks(t_blocks, m, n, "t_blocks"), *_blocks(z_blocks, m, n, "z_blocks"), _stream()), ctx.h)
+
+
 def lgc_weight_grad(ctx: Context, dy: torch.Tensor, x: Blocks, dw: torch.Tensor, db: Optional[torch.Tensor] = None) -> None:
     """dw [n][k] <- dy [rows][n]^T x [rows][k], db [n] <- the columns' sums of dy; dw anywhere in a flat fp32 gradient."""
     kind, rows, n, at, ld = _own(dy, "dy")
@@ -627,7 +648,38 @@ def lgc_weight_grad(ctx: Context, dy: torch.Tensor, x: Blocks, dw: torch.Tensor,
     _check(lib().lgc_weight_grad(ctx.h, at, kind, rows, n, ld, codes, exps, x._cols, _vector(dw, n * x._cols, "dw"), _vector(db, n, "db"), _stream()), ctx.h)
 
 
-# ------------------------------------------------------------- attention
+# ------------------------------------------------------------- rotary positions and attention
+
+_PAIRS = {"halves": LGC_HALVES, "neighbours": LGC_NEIGHBOURS}
+
+
+def lgc_rotary_frequencies(dims: int, base: float = 10000.0, factor: float = 1.0, length: float = 0.0, low: float = 1.0, high: float = 4.0) -> torch.Tensor:
+    """[dims / 2] in float64, in host memory: radians per position of each pair, for contexts `factor` times as long as the trained `length`."""
+    if not 0 <= dims < 1 << 32:
+        _refuse("dims is even, and 2 to 2^20")
+    freqs = torch.empty(dims // 2, dtype=torch.float64)
+    _check(lib().lgc_rotary_frequencies(freqs.data_ptr() if dims > 1 else None, dims, base, factor, length, low, high))
+    return freqs
+
+
+def lgc_rotate(ctx: Context, x: torch.Tensor, heads: int, freqs: torch.Tensor, y: Optional[torch.Tensor] = None, positions: Optional[torch.Tensor] = None, period: int = 0,
+               layout: str = "halves", amplitude: float = 1.0, inverse: bool = False) -> None:
+    """y (None: x itself) <- the heads of x [rows][heads * dim], each with its first 2 * len(freqs) columns turned by its token's position; inverse: the gradient.
+    positions: int32 [rows], or row modulo period (0: the row)."""
+    kind, rows, cols, at, ld = _own(x, "x")
+    if heads < 1 or cols % heads:
+        _refuse(f"{cols} columns are not {heads} heads")
+    to, ld_y = _matrix(x if y is None else y, rows, cols, x.dtype, "y")
+    if positions is not None and (positions.numel() != rows or not positions.is_contiguous()):
+        _refuse(f"positions must be contiguous with {rows} elements")
+    if not freqs.is_contiguous() or period < 0:
+        _refuse("freqs must be contiguous, and period not negative")
+    pairs = _PAIRS.get(layout)
+    if pairs is None:
+        _refuse(f"layout is one of {', '.join(_PAIRS)}")
+    _check(lib().lgc_rotate(ctx.h, at, kind, rows, ld, heads, cols // heads, _ptr(positions, torch.int32), period, _ptr(freqs, torch.float64), 2 * freqs.numel(), pairs, amplitude,
+                            inverse, to, ld_y, _stream()), ctx.h)
+
 
 class AttentionShape:
     """lgc_attention_shape without its rows: heads, sequences and who sees whom.  `scale` is dim^(-1/2) where it is not given.  q_starts, kv_starts: int32 device
@@ -655,9 +707,6 @@ class AttentionShape:
             c.q_starts, c.kv_starts = self._starts[0].data_ptr(), self._starts[1].data_ptr()
         c.q_rows, c.kv_rows = q.shape[0], k.shape[0]
         return self._at
-
-
-_BF16 = torch.bfloat16
 
 
 def lgc_attention(ctx: Context, shape: AttentionShape, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, o: torch.Tensor, lse: Optional[torch.Tensor] = None) -> None:

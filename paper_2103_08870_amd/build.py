@@ -16,7 +16,7 @@ LIB_SHORT_WAIT = os.path.join(HERE, "liblgc_short_wait.so")
 ROOT = os.path.dirname(HERE)
 HBM_RATES = os.path.join(ROOT, "hbm_rates")
 SOURCES = ["api.hip", "streaming.hip", "topk.hip", "small.hip", "segmented.hip", "autoencoder.hip", "ae_mfma.hip", "ae_fused.hip",
-           "blocks.hip", "norm.hip", "product.hip", "weight_grad.hip", "attention.hip"]
+           "blocks.hip", "norm.hip", "product.hip", "weight_grad.hip", "rotary.hip", "attention.hip"]
 HEADERS = [os.path.join(CSRC, "lgc_internal.h"), os.path.join(CSRC, "device_helpers.h"), os.path.join(CSRC, "carry.h"), os.path.join(CSRC, "blocks.h"),
            os.path.join(os.path.dirname(HERE), "include", "lgc.h")]
 

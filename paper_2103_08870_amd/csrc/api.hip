@@ -1599,8 +1599,27 @@ extern "C" lgc_status lgc_product(lgc_ctx *ctx, const uint8_t *a_codes, const ui
     if (m) c.blocks("a", a_codes, a_exps).blocks("b", b_codes, b_exps).plain("y", y, type, n, ld);
     c.reserved("lgc_product");
     return launch(c, [&] {
-        if (m) launch_product(a_codes, a_exps, b_codes, b_exps, (uint32_t)m, (uint32_t)n, (uint32_t)k, bias, y, type, ld, ctx->training, kTrainingFloats, ctx->cus,
+        if (m) launch_product(a_codes, a_exps, b_codes, b_exps, (uint32_t)m, (uint32_t)n, (uint32_t)k, bias, y, type, ld, nullptr, ctx->training, kTrainingFloats, ctx->cus,
                               (hipStream_t)stream);
+    });
+}
+
+extern "C" lgc_status lgc_product_activate(lgc_ctx *ctx, const uint8_t *a_codes, const uint8_t *a_exps, uint64_t m, const uint8_t *b_codes, const uint8_t *b_exps, uint64_t n, uint64_t k,
+                                           const float *bias, lgc_act act, const void *residual, uint64_t ld_residual, void *z, lgc_type type, uint64_t ld, uint8_t *t_codes,
+                                           uint8_t *t_exps, uint8_t *z_codes, uint8_t *z_exps, void *stream) {
+    Check c(ctx);
+    if (act != LGC_LINEAR) c.act(act);
+    c.type(type).cols("n", n).cols("k", k).rows("m", m, k).rows("m", m, n).rows("n", n, k).maybe("bias", bias);
+    if (m) c.blocks("a", a_codes, a_exps).blocks("b", b_codes, b_exps).maybe("residual", residual, type, n, ld_residual).maybe("z", z, type, n, ld)
+        .maybe_blocks("t", t_codes, t_exps).maybe_blocks("z", z_codes, z_exps)
+        .need(!residual || z, "a residual, and no z to which it goes")
+        .need(!residual || !(z_codes || z_exps), "z in 8 bits is not made with a residual");
+    c.reserved("lgc_product_activate");
+    return launch(c, [&] {
+        const ProductEpilogue after{act, residual, ld_residual, t_codes, t_exps, z_codes, z_exps};
+        if (m && (z || t_codes || z_codes))
+            launch_product(a_codes, a_exps, b_codes, b_exps, (uint32_t)m, (uint32_t)n, (uint32_t)k, bias, z, type, ld, &after, ctx->training, kTrainingFloats, ctx->cus,
+                           (hipStream_t)stream);
     });
 }
 
@@ -1615,7 +1634,36 @@ extern "C" lgc_status lgc_weight_grad(lgc_ctx *ctx, const void *dy, lgc_type typ
     });
 }
 
-// ------------------------------------------------------------------ attention
+// ------------------------------------------------------------------ rotary positions and attention
+
+extern "C" lgc_status lgc_rotary_frequencies(double *freqs, uint32_t dims, double base, double factor, double length, double low, double high) {
+    if (!freqs) return fail(nullptr, LGC_EINVAL, "freqs is NULL");
+    if (dims < 2 || dims % 2 || dims > kMostCols) return fail(nullptr, LGC_EINVAL, "dims = %u: not even, or outside [2, 2^20]", dims);
+    if (!(base > 0 && base < INFINITY && factor > 0 && factor < INFINITY && length >= 0 && length < INFINITY))
+        return fail(nullptr, LGC_EINVAL, "base = %g, factor = %g, length = %g", base, factor, length);
+    if (length > 0 && !(low >= 0 && low < high && high < INFINITY)) return fail(nullptr, LGC_EINVAL, "from %g to %g turns", low, high);
+    for (uint32_t i = 0; i < dims / 2; ++i) {
+        const double f = std::pow(base, -2.0 * i / dims), turns = length * f / 6.283185307179586476925;
+        const double kept = length > 0 ? std::min(1.0, std::max(0.0, (turns - low) / (high - low))) : 0.0;
+        freqs[i] = f * (kept + (1.0 - kept) / factor);
+    }
+    return LGC_OK;
+}
+
+extern "C" lgc_status lgc_rotate(lgc_ctx *ctx, const void *x, lgc_type type, uint64_t rows, uint64_t ld, uint32_t heads, uint32_t dim, const int32_t *positions, uint64_t period,
+                                 const double *freqs, uint32_t dims, lgc_pairs pairs, float amplitude, int inverse, void *y, uint64_t ld_y, void *stream) {
+    Check c(ctx);
+    const uint64_t cols = (uint64_t)heads * dim;
+    c.type(type).cols("heads * dim", cols).rows("rows", rows, cols).need(rows < (1ull << 24), "rows = %llu not below 2^24", (unsigned long long)rows);
+    c.need(dims >= 2 && dims % 2 == 0 && dims <= dim, "dims = %u: not even, or outside [2, dim = %u]", dims, dim);
+    c.need(pairs == LGC_HALVES || pairs == LGC_NEIGHBOURS, "unknown pairs %d", (int)pairs);
+    c.need(period < (1ull << 31), "period = %llu not below 2^31", (unsigned long long)period).need(amplitude > -INFINITY && amplitude < INFINITY, "amplitude = %g", (double)amplitude);
+    c.need(freqs && aligned(freqs, 8), "freqs is NULL or not 8-byte aligned").need(aligned(positions, 4), "positions are not 4-byte aligned");
+    if (rows) c.plain("x", x, type, cols, ld).plain("y", y, type, cols, ld_y).need(x != y || ld == ld_y || rows == 1, "y lies where x does, with rows another distance apart");
+    return launch(c, [&] {
+        if (rows) launch_rotate(x, type, (uint32_t)rows, ld, heads, dim, positions, (uint32_t)period, freqs, dims, pairs, amplitude, inverse != 0, y, ld_y, (hipStream_t)stream);
+    });
+}
 
 namespace {
 

@@ -26,7 +26,7 @@ typedef const __attribute__((address_space(1))) void *Global;
 
 constexpr int kTileKeys = 64;     // keys (forward, dq) or rows (dk, dv) that are in LDS at a time
 constexpr int kThreads = 256;
-constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+constexpr float kLn2 = 0.69314718055994530942f;
 // The running maximum is followed only when it grows by more than this many powers of two: p up to 2^8 loses nothing in fp32 or bf16, and sums are rarely scaled anew.
 constexpr float kSlack = 8.f;
 

@@ -139,43 +139,6 @@ __global__ __launch_bounds__(kBlock) void k_quantize_tiles(const T *w, uint64_t 
 
 // ---------------------------------------------------------------- non-linearities
 
-// Normal distribution's function below -|x|, over exp(-x^2 / 2): t * (c0 + c1 t + .. + c6 t^6) with t = 1 / (1 + p |x|), fitted (least largest relative
-// error, by reweighted least squares) for 0 <= |x| <= 13.5, where it is off by 5.3e-7 at most; the tail keeps its relative precision, since nothing is
-// subtracted from 1.  Measured, GELU is off by 1e-6 of the result at most from -2 on (fp32 with an exact erf: 1.5e-7 around 0, 5e-2 of the result at -5), by 2e-6 at -5
-// and 8e-6 at -13, where the exponential's argument is rounded at its size; its slope by 4e-7, absolute.  One exponential and one reciprocal, for results that mostly go on
-// to bf16 or 8 bits.
-__device__ __forceinline__ float normal_below(float size, float gauss) {
-    const float t = __builtin_amdgcn_rcpf(1.f + 0.26390194744793544f * size);
-    float s = -0.0694093182682991f;
-    s = fmaf(s, t, 0.20417608320713043f);
-    s = fmaf(s, t, -0.07719594985246658f);
-    s = fmaf(s, t, 0.14925582706928253f);
-    s = fmaf(s, t, 0.08022129535675049f);
-    s = fmaf(s, t, 0.10782003402709961f);
-    s = fmaf(s, t, 0.10513176769018173f);
-    return s * t * gauss;
-}
-
-constexpr float kLog2e = 1.4426950408889634f;
-
-template <int kAct>
-__device__ __forceinline__ float act(float x) {
-    if constexpr (kAct == LGC_RELU) return x < 0.f ? 0.f : x;   // (a NaN stays)
-    if constexpr (kAct == LGC_SILU) return x * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-kLog2e * x));
-    const float below = normal_below(fabsf(x), __builtin_amdgcn_exp2f(-0.5f * kLog2e * x * x));
-    return x * (x < 0.f ? below : 1.f - below);
-}
-template <int kAct>
-__device__ __forceinline__ float act_slope(float x) {
-    if constexpr (kAct == LGC_RELU) return x > 0.f ? 1.f : x <= 0.f ? 0.f : x;
-    if constexpr (kAct == LGC_SILU) {
-        const float p = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-kLog2e * x));
-        return fmaf(x * p, 1.f - p, p);
-    }
-    const float gauss = __builtin_amdgcn_exp2f(-0.5f * kLog2e * x * x), below = normal_below(fabsf(x), gauss);
-    return fmaf(x * gauss, 0.3989422804014327f, x < 0.f ? below : 1.f - below);
-}
-
 // z = f(a), and a and z in 8 bits; what is null is left out
 template <typename T, int kAct, int kUnits>
 __global__ __launch_bounds__(kBlock) void k_activate(const T *a, uint64_t ld, uint32_t cols, Divide blocks, uint32_t units, T *z, uint64_t ld_z, uint8_t *a_codes,

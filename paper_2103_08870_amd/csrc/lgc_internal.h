@@ -324,10 +324,19 @@ void launch_norm(const void *x, lgc_type type, uint32_t rows, uint32_t cols, uin
 void launch_norm_grad(const void *dy, uint64_t ld_dy, const void *x, uint64_t ld, lgc_type type, uint32_t rows, uint32_t cols, const float *gamma, const float *mean,
                       const float *rstd, void *dx, uint64_t ld_dx, float *dgamma, float *dbeta, float *scratch, size_t scratch_floats, int cus, hipStream_t st);
 // product.hip, weight_grad.hip
+struct ProductEpilogue {   // y = f(the sum) + residual, the sum and f of it in 8 bits; what is null is left out (y too)
+    lgc_act act;
+    const void *residual;
+    uint64_t ld_residual;
+    uint8_t *t_codes, *t_exps, *z_codes, *z_exps;
+};
 void launch_product(const uint8_t *a, const uint8_t *a_exps, const uint8_t *b, const uint8_t *b_exps, uint32_t m, uint32_t n, uint32_t k, const float *bias, void *y,
-                    lgc_type type, uint64_t ld, float *scratch, size_t scratch_floats, int cus, hipStream_t st);
+                    lgc_type type, uint64_t ld, const ProductEpilogue *after /* nullable */, float *scratch, size_t scratch_floats, int cus, hipStream_t st);
 void launch_weight_grad(const void *dy, lgc_type type, uint32_t rows, uint32_t n, uint64_t ld, const uint8_t *codes, const uint8_t *exps, uint32_t k, float *dw, float *db,
                         float *scratch, size_t scratch_floats, int cus, hipStream_t st);
+// rotary.hip
+void launch_rotate(const void *x, lgc_type type, uint32_t rows, uint64_t ld, uint32_t heads, uint32_t dim, const int32_t *positions, uint32_t period, const double *freqs, uint32_t dims,
+                   lgc_pairs pairs, float amplitude, bool inverse, void *y, uint64_t ld_y, hipStream_t st);
 // attention.hip
 void launch_attention(const lgc_attention_shape &shape, const void *q, uint64_t ld_q, const void *k, uint64_t ld_k, const void *v, uint64_t ld_v, void *o, uint64_t ld_o, float *lse,
                       float *scratch, size_t scratch_floats, int cus, hipStream_t st);

@@ -24,6 +24,28 @@ struct ProductArgs {
     uint64_t ld;
 };
 
+// What becomes of a sum t = A B^T + bias before it is stored: z = f(t) + residual, z as the product's own type, t and z in 8 bits; what is null is left out.
+struct Epilogue {
+    int act;                 // lgc_act
+    const void *residual;
+    uint64_t ld_residual;
+    uint8_t *t_codes, *t_exps, *z_codes, *z_exps;
+};
+
+struct Plain {};   // (the sum is stored as it is)
+
+// f of numbers at once: which f is the same for all lanes, and asked for once
+template <int kCount>
+__device__ __forceinline__ void activate(int act_of, float (&x)[kCount]) {
+    auto all = [&](auto kind) {
+#pragma unroll
+        for (int i = 0; i < kCount; ++i) x[i] = act<decltype(kind)::value>(x[i]);
+    };
+    if (act_of == LGC_RELU) all(std::integral_constant<int, LGC_RELU>());
+    else if (act_of == LGC_GELU) all(std::integral_constant<int, LGC_GELU>());
+    else if (act_of == LGC_SILU) all(std::integral_constant<int, LGC_SILU>());
+}
+
 // Eight values as bf16, exactly.
 __device__ __forceinline__ bf8 bf16_of(int lo, int hi, float scale) {
     const bf2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((uint32_t)lo, scale, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((uint32_t)lo, scale, true);
@@ -60,8 +82,8 @@ __device__ __forceinline__ void tile_of(uint32_t id, uint32_t tiles_m, uint32_t 
 // A tile of kWavesM x kWavesN wavefronts' tiles of 32 kSideM x 32 kSideN per block.  Blocks of 128 columns are loaded straight to LDS, whole lines of 128
 // bytes at a time, into two places in turn: while one is multiplied, the other's loads are under way.  The fragments of one half of a block are read while the
 // products of the half before run.  A row's eight pieces of 16 bytes are exchanged in LDS by its number, so that 8 and 16 neighbouring rows' pieces meet all banks.
-template <typename T, int kSideM, int kSideN, int kWavesM, int kWavesN, bool kExact>
-__global__ __launch_bounds__(64 * kWavesM * kWavesN) void k_product(ProductArgs p) {
+template <typename T, int kSideM, int kSideN, int kWavesM, int kWavesN, bool kExact, typename E = Plain>
+__global__ __launch_bounds__(64 * kWavesM * kWavesN) void k_product(ProductArgs p, E ep) {
     constexpr int kWaveM = 32 * kSideM, kWaveN = 32 * kSideN, kTile = kWaveM * kWavesM, kAll = kWavesM * kWavesN;
     constexpr int kHalf = kTile * kBlockCols, kPlace = 2 * kHalf, kLoads = kPlace / (kAll * 1024), kExps = 2 * kTile * 4;
     constexpr int kPer = 16 / (int)sizeof(T), kPitch = 64 + kPer, kRows = kAll * 32 * kPitch * (int)sizeof(T), kBias = kTile * 4;
@@ -197,6 +219,95 @@ __global__ __launch_bounds__(64 * kWavesM * kWavesN) void k_product(ProductArgs 
     }
     meet();   // nothing may arrive any more where the rows go
 
+    // With an epilogue, 32 rows of 64 columns at a time go through LDS in fp32, each wavefront's for itself, and a lane takes eight columns of a row on from there.  The exponents of 8-bit
+    // results are found before, from the sums in registers: two wavefronts have the 128 columns that share one.
+    if constexpr (std::is_same_v<E, Epilogue>) {
+        static_assert(kSideN == 2 && sizeof(f4) * kAll * 32 * 17 + 2 * kAll * kWaveM * 4 <= 2 * kPlace, "room");
+        float *const out = (float *)places + wave * 32 * 68;
+        uint32_t *const most = (uint32_t *)(places + kAll * 32 * 68 * 4);   // [of t, of z][wavefront][row]
+        f4 bias[2][4];
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) bias[j][c] = *(const f4 *)((const float *)biases + wn + 32 * j + 8 * c + 4 * g);
+        const bool all_cols = n0 + wn + 64 <= p.n;
+        auto sums = [&](int i, int j, int c, float (&t)[4]) {   // columns that do not exist are zeros
+            const f4 q = bias[j][c] + f4{acc[i][j][4 * c], acc[i][j][4 * c + 1], acc[i][j][4 * c + 2], acc[i][j][4 * c + 3]};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) t[e] = all_cols || n0 + wn + 32 * j + 8 * c + 4 * g + e < p.n ? q[e] : 0.f;
+        };
+        if (ep.t_codes || ep.z_codes) {
+#pragma unroll
+            for (int i = 0; i < kSideM; ++i) {
+                uint32_t most_t = 0, most_z = 0;
+                auto larger = [](uint32_t m, float x) { const uint32_t k = key_of(x); return k < kInfKey && k > m ? k : m; };
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        float t[4];
+                        sums(i, j, c, t);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) most_t = larger(most_t, t[e]);
+                        if (ep.z_codes) {
+                            activate(ep.act, t);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) most_z = larger(most_z, t[e]);
+                        }
+                    }
+                most_t = max(most_t, (uint32_t)__shfl_xor((int)most_t, 32));
+                most_z = max(most_z, (uint32_t)__shfl_xor((int)most_z, 32));
+                if (g == 0) {
+                    most[wave * kWaveM + 32 * i + r] = most_t;
+                    most[(kAll + wave) * kWaveM + 32 * i + r] = most_z;
+                }
+            }
+        }
+        __syncthreads();
+        const uint32_t row = lane / 8, col = lane % 8 * 8, other = (wave / kWavesM ^ 1) * kWavesM + wave % kWavesM;   // other: the wavefront beside, in the same 128 columns
+        const uint32_t n = n0 + wn + col, codes_to = (uint32_t)block_count(p.n) * kBlockCols, code_exps = (uint32_t)exps_stride(p.n);
+        const int count = count_at(n, p.n);
+#pragma unroll
+        for (int i = 0; i < kSideM; ++i) {
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    float t[4];
+                    sums(i, j, c, t);
+                    *(f4 *)(out + r * 68 + 32 * j + 8 * c + 4 * g) = f4{t[0], t[1], t[2], t[3]};
+                }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma clang loop unroll(disable)
+            for (int s = 0; s < 4; ++s) {
+                const uint32_t of_wave = 32 * i + 8 * s + row, m = m0 + wm + of_wave;
+                float v[8];
+                const f4 lo = *(const f4 *)(out + (8 * s + row) * 68 + col), hi = *(const f4 *)(out + (8 * s + row) * 68 + col + 4);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) { v[e] = lo[e]; v[4 + e] = hi[e]; }
+                auto store_codes = [&](uint8_t *codes, uint8_t *exps, const uint32_t *most) {
+                    const uint32_t e = block_exp(max(most[wave * kWaveM + of_wave], most[other * kWaveM + of_wave]));
+                    if (m >= p.m || n >= codes_to) return;
+                    *(u2 *)(codes + (uint64_t)m * codes_to + n) = codes_of(v, e);
+                    if (col == 0 && wave / kWavesM % 2 == 0) exps[(uint64_t)m * code_exps + n / kBlockCols] = (uint8_t)e;
+                };
+                if (ep.t_codes) store_codes(ep.t_codes, ep.t_exps, most);
+                activate(ep.act, v);
+                if (ep.z_codes) store_codes(ep.z_codes, ep.z_exps, most + kAll * kWaveM);
+                if (!p.y || m >= p.m || !count) continue;
+                if (ep.residual) {
+                    float x[8];
+                    load_chunk((const T *)ep.residual + (uint64_t)m * ep.ld_residual, n, p.n, x);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] += x[e];
+                }
+                store_chunk((T *)p.y + (uint64_t)m * p.ld + n, count, v);
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        }
+        return;
+    }
+
     // Lane: row r of 32, columns 8 c + 4 g + 0 .. 3 of 32.  32 rows of 64 columns at a time go through LDS, each wavefront's for itself, to be stored in
     // whole lines.
     const uint32_t row = lane / (64 / kPer), col = lane % (64 / kPer) * kPer;
@@ -258,8 +369,8 @@ __global__ __launch_bounds__(64 * kWavesM * kWavesN) void k_product(ProductArgs 
 // Few rows of A (16 kM at most): the time is that of reading B once (1 x 8192 x 4096 7.3 us, 4.6 TB/s; 1 x 16384 x 16384 57 us, 4.7 TB/s), so B goes from memory to registers, whole lines of 128 bytes, with no LDS and nothing
 // to wait for together.  A block has 16 kN rows of B; its kFew wavefronts take groups of four blocks of 128 columns in turn, a group's loads all at once, and their
 // sums meet in LDS.
-template <typename T, int kM, int kN, int kFew, bool kExact>
-__global__ __launch_bounds__(64 * kFew) void k_product_few(ProductArgs p) {
+template <typename T, int kM, int kN, int kFew, bool kExact, typename E = Plain>
+__global__ __launch_bounds__(64 * kFew) void k_product_few(ProductArgs p, E ep) {
     __shared__ __align__(16) f4 part[kFew][kM * kN][64];
     const uint32_t n0 = blockIdx.x * 16 * kN, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), r = lane & 15, g = lane >> 4;
     const uint64_t stride = (uint64_t)p.blocks * kBlockCols;
@@ -321,6 +432,18 @@ __global__ __launch_bounds__(64 * kFew) void k_product_few(ProductArgs p) {
 #pragma unroll
         for (int w = 1; w < kFew; ++w) s += part[w][tile][lane];
         if (m >= p.m || n >= p.n) continue;
+        if constexpr (std::is_same_v<E, Epilogue>) {
+            float v[4];
+            const T *const from = (const T *)ep.residual + (uint64_t)m * ep.ld_residual + n;
+#pragma unroll
+            for (int d = 0; d < 4; ++d) v[d] = s[d] + (p.bias && n + d < p.n ? p.bias[n + d] : 0.f);
+            activate(ep.act, v);
+            T *const to = (T *)p.y + (uint64_t)m * p.ld + n;
+#pragma unroll
+            for (int d = 0; d < 4; ++d)
+                if (n + d < p.n) store_one(to + d, v[d] + (ep.residual ? to_float(from[d]) : 0.f));
+            continue;
+        }
         T *at = (T *)p.y + ((gridDim.y > 1 ? (uint64_t)blockIdx.y * p.m : 0) + m) * p.ld + n;
         if (n + 4 <= p.n) {
             if (p.bias) s += *(const f4u *)(p.bias + n);
@@ -351,13 +474,45 @@ __global__ __launch_bounds__(kBlock) void k_join(const float *part, uint32_t par
     store_chunk(y + (uint64_t)row * ld + col, count, s);
 }
 
+// The epilogue of t = bias + the sum of `parts` arrays [m][n], in their order: 16 lanes per 128 columns
+template <typename T>
+__global__ __launch_bounds__(kBlock) void k_epilogue(const float *part, uint32_t parts, uint32_t m, uint32_t n, Divide blocks, const float *bias, T *z, uint64_t ld, Epilogue ep) {
+    const uint32_t unit = blockIdx.x * (kBlock / 16) + threadIdx.x / 16;
+    if (unit >= m * blocks.by) return;
+    const uint32_t row = quotient(unit, blocks), col = (unit - row * blocks.by) * kBlockCols + (threadIdx.x & 15) * kChunkCols, exp_stride = (uint32_t)exps_stride(n);
+    const int count = count_at(col, n);
+    float s[8] = {}, v[8];
+    if (count) {
+        if (bias) load_chunk(bias, col, n, s);
+#pragma unroll 4
+        for (uint32_t i = 0; i < parts; ++i) {
+            load_chunk(part + ((uint64_t)i * m + row) * n, col, n, v);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) s[j] += v[j];
+        }
+    }
+    const uint64_t code = (uint64_t)unit * kBlockCols + (threadIdx.x & 15) * kChunkCols, exp = (uint64_t)row * exp_stride + col / kBlockCols;
+    if (ep.t_codes) store_block(s, ep.t_codes + code, ep.t_exps + exp);
+    activate(ep.act, s);   // (f(0) = 0: columns that do not exist stay zeros)
+    if (ep.z_codes) store_block(s, ep.z_codes + code, ep.z_exps + exp);
+    if (!z || !count) return;
+    if (ep.residual) {
+        load_chunk((const T *)ep.residual + (uint64_t)row * ep.ld_residual, col, n, v);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) s[j] += v[j];
+    }
+    store_chunk(z + (uint64_t)row * ld + col, count, s);
+}
+
 }  // namespace
 
 void launch_product(const uint8_t *a, const uint8_t *a_exps, const uint8_t *b, const uint8_t *b_exps, uint32_t m, uint32_t n, uint32_t k, const float *bias, void *y,
-                    lgc_type type, uint64_t ld, float *scratch, size_t scratch_floats, int cus, hipStream_t st) {
+                    lgc_type type, uint64_t ld, const ProductEpilogue *after, float *scratch, size_t scratch_floats, int cus, hipStream_t st) {
     auto tiles = [&](uint32_t side) { return (uint64_t)((m + side - 1) / side) * ((n + side - 1) / side); };
-    const uint32_t blocks = (uint32_t)block_count(k);
+    const uint32_t blocks = (uint32_t)block_count(k), blocks_of_n = (uint32_t)block_count(n);
     ProductArgs p{a, a_exps, b, b_exps, m, n, blocks, (uint32_t)exps_stride(k), 0, 0, 0, bias, y, ld};
+    const Epilogue ep = after ? Epilogue{after->act, after->residual, after->ld_residual, after->t_codes, after->t_exps, after->z_codes, after->z_exps} : Epilogue{};
+    const bool codes = ep.t_codes || ep.z_codes;
     uint64_t parts = 1;
     auto split = [&](uint64_t want) {   // the sum over k in `want` parts, in whole groups of four blocks, where there is room for their sums
         parts = std::max<uint64_t>(1, std::min(want, scratch_floats / ((uint64_t)m * n)));
@@ -366,7 +521,13 @@ void launch_product(const uint8_t *a, const uint8_t *a_exps, const uint8_t *b, c
         if (parts > 1) { p.bias = nullptr; p.y = scratch; p.ld = n; }
     };
     auto join = [&] {
-        if (parts == 1) return;
+        if (p.y != scratch) return;
+        if (after) {
+            const uint32_t units = m * blocks_of_n, grid = (units + kBlock / 16 - 1) / (kBlock / 16);
+            if (type == LGC_FP32) k_epilogue<float><<<grid, kBlock, 0, st>>>(scratch, (uint32_t)parts, m, n, divide_by(blocks_of_n), bias, (float *)y, ld, ep);
+            else k_epilogue<Bf16><<<grid, kBlock, 0, st>>>(scratch, (uint32_t)parts, m, n, divide_by(blocks_of_n), bias, (Bf16 *)y, ld, ep);
+            return;
+        }
         const uint32_t chunks = (n + 7) / 8, grid = (uint32_t)(((uint64_t)m * chunks + kBlock - 1) / kBlock);
         if (type == LGC_FP32) k_join<float><<<grid, kBlock, 0, st>>>(scratch, (uint32_t)parts, m, n, divide_by(chunks), bias, (float *)y, ld);
         else k_join<Bf16><<<grid, kBlock, 0, st>>>(scratch, (uint32_t)parts, m, n, divide_by(chunks), bias, (Bf16 *)y, ld);
@@ -377,15 +538,20 @@ void launch_product(const uint8_t *a, const uint8_t *a_exps, const uint8_t *b, c
     // Every block reads all of A, from an L2: tiles are faster for over 32 rows where that is 64 MB and more (us, few rows / tiles: 48 x 8192 x 4096 13.8 / 15.5,
     // 64 x 1024 x 1024 5.0 / 6.7, 64 x 4096 x 4096 12.7 / 13.4, 64 x 8192 x 4096 15.4 / 15.0, 64 x 2048 x 16384 25.9 / 17.7, 64 x 12000 x 4096 26.1 / 19.4), and not
     // before (32 x 16384 x 4096 18.8 / 22.4, 32 x 8192 x 8192 22.3 / 22.7)
-    if (m <= 32 || (m <= 64 && (uint64_t)(n / (wide ? 32 : 16)) * m * k < 1u << 26)) {
+    // (an exponent is shared by more columns than a block has here: 8-bit results are made from the sums in the scratch, if it holds them)
+    if ((m <= 32 || (m <= 64 && (uint64_t)(n / (wide ? 32 : 16)) * m * k < 1u << 26)) && (!codes || (uint64_t)m * n <= scratch_floats)) {
         auto few = [&](auto rows, auto cols, auto team) {
             constexpr int kM = decltype(rows)::value, kN = decltype(cols)::value, kFew = decltype(team)::value;
             const uint32_t own = (n + 16 * kN - 1) / (16 * kN);
             split(own < (uint32_t)cus ? std::min<uint64_t>(2 * cus / own, blocks / (4 * kFew)) : 1);
+            if (codes && parts == 1) { p.bias = nullptr; p.y = scratch; p.ld = n; }
             const dim3 grid(own, (uint32_t)parts);
-            if (type == LGC_FP32) k_product_few<float, kM, kN, kFew, true><<<grid, 64 * kFew, 0, st>>>(p);
-            else if (parts > 1) k_product_few<float, kM, kN, kFew, false><<<grid, 64 * kFew, 0, st>>>(p);
-            else k_product_few<Bf16, kM, kN, kFew, false><<<grid, 64 * kFew, 0, st>>>(p);
+            const bool here = after && p.y != scratch;   // the epilogue, in the product's launch
+            if (type == LGC_FP32 && here) k_product_few<float, kM, kN, kFew, true, Epilogue><<<grid, 64 * kFew, 0, st>>>(p, ep);
+            else if (type == LGC_FP32) k_product_few<float, kM, kN, kFew, true><<<grid, 64 * kFew, 0, st>>>(p, Plain());
+            else if (p.y == scratch) k_product_few<float, kM, kN, kFew, false><<<grid, 64 * kFew, 0, st>>>(p, Plain());
+            else if (here) k_product_few<Bf16, kM, kN, kFew, false, Epilogue><<<grid, 64 * kFew, 0, st>>>(p, ep);
+            else k_product_few<Bf16, kM, kN, kFew, false><<<grid, 64 * kFew, 0, st>>>(p, Plain());
             join();
         };
         typedef std::integral_constant<int, 1> One;
@@ -415,10 +581,16 @@ void launch_product(const uint8_t *a, const uint8_t *a_exps, const uint8_t *b, c
     p.tiles_m = (m + side - 1) / side;
     p.tiles_n = (n + side - 1) / side;
     const dim3 grid((uint32_t)tiles(side), (uint32_t)parts);
-    if (large) k_product<Bf16, 4, 2, 2, 4, false><<<grid, 512, 0, st>>>(p);
-    else if (type == LGC_FP32) k_product<float, 2, 2, 2, 2, true><<<grid, 256, 0, st>>>(p);
-    else if (parts > 1) k_product<float, 2, 2, 2, 2, false><<<grid, 256, 0, st>>>(p);
-    else k_product<Bf16, 2, 2, 2, 2, false><<<grid, 256, 0, st>>>(p);
+    if (after && p.y != scratch) {
+        if (large) k_product<Bf16, 4, 2, 2, 4, false, Epilogue><<<grid, 512, 0, st>>>(p, ep);
+        else if (type == LGC_FP32) k_product<float, 2, 2, 2, 2, true, Epilogue><<<grid, 256, 0, st>>>(p, ep);
+        else k_product<Bf16, 2, 2, 2, 2, false, Epilogue><<<grid, 256, 0, st>>>(p, ep);
+        return;
+    }
+    if (large) k_product<Bf16, 4, 2, 2, 4, false><<<grid, 512, 0, st>>>(p, Plain());
+    else if (type == LGC_FP32) k_product<float, 2, 2, 2, 2, true><<<grid, 256, 0, st>>>(p, Plain());
+    else if (parts > 1) k_product<float, 2, 2, 2, 2, false><<<grid, 256, 0, st>>>(p, Plain());
+    else k_product<Bf16, 2, 2, 2, 2, false><<<grid, 256, 0, st>>>(p, Plain());
     join();
 }
 
