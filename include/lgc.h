@@ -514,9 +514,9 @@ lgc_status lgc_rotate(lgc_ctx *ctx, const void *x, lgc_type type, uint64_t rows,
  * Key head h serves the query heads h * heads / kv_heads on, heads / kv_heads of them.
  *
  * Limits: dim a multiple of 8, 8 to 128; heads a multiple of kv_heads, heads * dim at
- * most 2^20; sequences 1 to 2^20, sequences * kv_heads at most 2^22; q_rows * heads and kv_rows * kv_heads below 2^30;
+ * most 2^20; sequences 1 to 2^20, sequences * kv_heads at most 2^22; q_rows * heads and kv_rows * kv_heads below 2^29;
  * scale > 0 and finite.  Matrices are bf16, 16-byte aligned, rows a multiple of
- * 8 elements apart.  q_rows == 0 and kv_rows == 0 are valid.
+ * 8 elements apart, 2^24 at most.  q_rows == 0 and kv_rows == 0 are valid.
  */
 typedef struct {
     uint64_t q_rows, kv_rows, sequences;

@@ -1675,8 +1675,8 @@ void check_attention(Check &c, const lgc_attention_shape *s) {
     c.need(kv_heads >= 1 && heads >= kv_heads && heads % kv_heads == 0, "%llu heads for %llu key heads", heads, kv_heads);
     c.need(heads * dim <= kMostCols, "heads * dim = %llu above 2^20", heads * dim);
     c.need(sequences >= 1 && sequences <= kMostCols && sequences * kv_heads <= 4 * kMostCols, "%llu sequences: none, above 2^20, or with their key heads above 2^22", sequences);
-    c.need(q_rows < (1ull << 30) && q_rows * heads < (1ull << 30), "q_rows * heads = %llu * %llu not below 2^30", q_rows, heads);
-    c.need(kv_rows < (1ull << 30) && kv_rows * kv_heads < (1ull << 30), "kv_rows * kv_heads = %llu * %llu not below 2^30", kv_rows, kv_heads);
+    c.need(q_rows < (1ull << 29) && q_rows * heads < (1ull << 29), "q_rows * heads = %llu * %llu not below 2^29", q_rows, heads);
+    c.need(kv_rows < (1ull << 29) && kv_rows * kv_heads < (1ull << 29), "kv_rows * kv_heads = %llu * %llu not below 2^29", kv_rows, kv_heads);
     c.need(s->scale > 0.f && s->scale < INFINITY, "scale = %g", (double)s->scale);
     c.need(!s->q_starts == !s->kv_starts, "one of q_starts and kv_starts is NULL");
     c.need(aligned(s->q_starts, 4) && aligned(s->kv_starts, 4), "starts are not 4-byte aligned");
@@ -1684,7 +1684,8 @@ void check_attention(Check &c, const lgc_attention_shape *s) {
 }
 void check_heads(Check &c, const char *name, const void *p, uint64_t rows, uint64_t cols, uint64_t ld) {
     if (!rows) return;
-    c.plain(name, p, LGC_BF16, cols, ld).need(aligned(p, 16) && ld % 8 == 0, "%s is not 16-byte aligned, or its rows not a multiple of 8 elements apart", name);
+    c.plain(name, p, LGC_BF16, cols, ld);
+    c.need(aligned(p, 16) && ld % 8 == 0 && ld <= (1u << 24), "%s is not 16-byte aligned, or its rows not a multiple of 8 elements apart, 2^24 at most", name);
 }
 
 }  // namespace

@@ -22,10 +22,8 @@ typedef short s8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf8 __attribute__((ext_vector_type(8)));
 typedef float f16 __attribute__((ext_vector_type(16)));
 typedef __attribute__((address_space(3))) void *Lds;
-typedef const __attribute__((address_space(1))) void *Global;
 
 constexpr int kTileKeys = 64;     // keys (forward, dq) or rows (dk, dv) that are in LDS at a time
-constexpr int kThreads = 256;
 constexpr float kLn2 = 0.69314718055994530942f;
 // The running maximum is followed only when it grows by more than this many powers of two: p up to 2^8 loses nothing in fp32 or bf16, and sums are rarely scaled anew.
 constexpr float kSlack = 8.f;
@@ -36,9 +34,10 @@ struct AttentionArgs {
     const uint32_t *q_starts, *kv_starts;
     uint32_t q_rows, kv_rows, sequences, heads, kv_heads, dim;
     uint32_t lq, lk;              // of every sequence, where there are no starts
-    uint32_t causal, window;
+    int causal, window;
     float scale;
-    Divide group, per_sequence, tiles;   // query heads per key head; tiles of a sequence, where there are no starts; tiles of a key head
+    Divide group, pairs;          // query heads per key head; heads, times sequences where there are no starts
+    uint32_t tiles;               // of each of these
     uint32_t parts;               // blockIdx.y: which part of the sum's tiles
     uint16_t *out, *dk, *dv;      // out: o or dq
     uint64_t ld_out, ld_dk, ld_dv;
@@ -48,12 +47,6 @@ struct AttentionArgs {
 
 __device__ __align__(16) const uint32_t kZeros[4] = {};   // what is loaded in the place of what does not exist
 
-// Blocks go to the eight XCDs in turn: each XCD gets neighbours, whose keys its L2 holds.
-__device__ __forceinline__ uint32_t neighbours(uint32_t id, uint32_t all) {
-    const uint32_t xcd = id & 7, q = all >> 3, r = all & 7;
-    return xcd * q + min(xcd, r) + (id >> 3);
-}
-
 struct Place {
     uint32_t head;      // key head
     uint32_t tile;      // of the sequence's rows (forward, dq: kTile of length times group; dk, dv: kTile keys)
@@ -61,21 +54,24 @@ struct Place {
     bool none;
 };
 
-// Which tile of which sequence a block works on; the last ones first, which under a causal mask have the most to do.  With starts, tile number starts[s] * group / kTile + s is the first of
-// sequence s: that leaves each sequence as many as it can need, and a block finds its sequence without a table.
+// Which tile of which sequence and key head a block works on.  Blocks go to the compute units in their order, and to the eight XCDs in turn.  So the heads (and sequences, if they have one length)
+// come in turn too, which gives most XCDs few of them, whose keys its L2 holds; and of each the tile first that has the most to do under a causal mask, so that short ones fill the end (a
+// head's tiles one sequence after the other, XCD by XCD: 4 x 4096 tokens, 32 / 8 heads of 128: forward 604 us, backward 3148).
+// With starts, tile number starts[s] * group / kTile + s is the first of sequence s: that leaves each sequence as many as it can need, and a block finds its sequence without a table.
 __device__ __forceinline__ Place place_of(const AttentionArgs &p, bool by_keys, uint32_t tile_rows) {
-    const uint32_t id = neighbours(blockIdx.x, gridDim.x);
+    const uint32_t rank = quotient(blockIdx.x, p.pairs), pair = blockIdx.x - rank * p.pairs.by;
+    const bool down = !by_keys || !p.causal;   // (of keys, the first are seen by the most queries)
     Place at;
-    at.head = quotient(id, p.tiles);
-    uint32_t tile = id - at.head * p.tiles.by;
-    if (!by_keys || !p.causal) tile = p.tiles.by - 1 - tile;   // (keys: the first are seen by the most queries)
     at.none = false;
     if (!p.q_starts) {
-        const uint32_t s = quotient(tile, p.per_sequence);
-        at.tile = tile - s * p.per_sequence.by;
+        const uint32_t s = pair / p.kv_heads;
+        at.head = pair - s * p.kv_heads;
+        at.tile = down ? p.tiles - 1 - rank : rank;
         at.q0 = s * p.lq; at.lq = p.lq; at.k0 = s * p.lk; at.lk = p.lk;
         return at;
     }
+    at.head = pair;
+    const uint32_t tile = down ? p.tiles - 1 - rank : rank;
     const uint32_t *starts = by_keys ? p.kv_starts : p.q_starts, rows = by_keys ? p.kv_rows : p.q_rows, group = by_keys ? 1 : p.group.by;
     auto first = [&](uint32_t s) { return (uint32_t)((uint64_t)min(starts[s], rows) * group / tile_rows) + s; };
     uint32_t lo = 0, n = p.sequences;   // sequences before lo begin at or before the tile; of the n from lo on it is open
@@ -94,55 +90,136 @@ __device__ __forceinline__ Place place_of(const AttentionArgs &p, bool by_keys, 
     return at;
 }
 
-// Keys [lo, hi) that query t of a sequence sees
+// Keys [lo, hi) that query t of a sequence sees (tokens are fewer than 2^29, and a window is held to that: all fits)
 struct Seen { int lo, hi; };
 __device__ __forceinline__ Seen seen_by(const AttentionArgs &p, const Place &at, uint32_t t) {
-    const int64_t pos = (int64_t)t + at.lk - at.lq;
-    const int hi = p.causal ? (int)max((int64_t)0, min(pos + 1, (int64_t)at.lk)) : (int)at.lk;
-    const int lo = p.window ? (int)max((int64_t)0, min(pos + 1 - p.window, (int64_t)at.lk)) : 0;
-    return Seen{lo, hi};
+    const int lk = (int)at.lk, pos = (int)t + lk - (int)at.lq;
+    return Seen{p.window ? max(0, min(pos + 1 - p.window, lk)) : 0, p.causal ? max(0, min(pos + 1, lk)) : lk};
 }
 
-// A tile of kTileKeys rows of kDim elements in LDS.  A row's pieces of 16 bytes are exchanged by its number, so that eight neighbouring rows' pieces (a plain read) and four rows' pieces of
-// 32 bytes (a turned one) meet all banks.
+// Tiles of keys that a block's rows see together, [from, to), and what a wavefront's see of each: bounds do not fall from row to row
+struct Range {
+    Seen block_first, block_last, first, last;
+    uint32_t from, to;
+    // whether the wavefront's rows each see all of a tile's keys, and the block's
+    __device__ __forceinline__ bool all_of(int key0) const { return key0 >= last.lo && key0 + kTileKeys <= first.hi; }
+    __device__ __forceinline__ bool block_all_of(int key0) const { return key0 >= block_last.lo && key0 + kTileKeys <= block_first.hi; }
+};
+__device__ __forceinline__ Range range_of(const AttentionArgs &p, const Place &at, uint32_t rows, uint32_t row0, uint32_t wave, uint32_t tile_rows) {
+    auto seen_at = [&](uint32_t row) { return seen_by(p, at, quotient(min(row, rows - 1), p.group)); };
+    Range x{seen_at(row0), seen_at(row0 + tile_rows - 1), seen_at(row0 + wave * 32), seen_at(row0 + wave * 32 + 31)};
+    x.from = (uint32_t)x.block_first.lo / kTileKeys;
+    x.to = max(x.from, ((uint32_t)x.block_last.hi + kTileKeys - 1) / kTileKeys);
+    return x;
+}
+
+// A tile of rows of kDim elements in LDS.  A row's pieces of 16 bytes are exchanged by its number, so that 16 neighbouring rows' pieces of one column (a plain read) and four rows' four
+// neighbouring pieces (a turned one) meet all 64 banks.
 template <int kDim>
-__device__ __forceinline__ uint32_t exchange(uint32_t row) { return (row & 3) << 1 | (row >> 2 & 1) | (kDim == 128 ? row & 8 : 0); }
+__device__ __forceinline__ uint32_t exchange(uint32_t row) { return (kDim == 128 ? row & 3 : row >> 1 & 1) << 2 | (row >> 2 & 3); }
 
-// Loads rows [row0, row0 + kTileKeys) straight to LDS; where(row): the address of a row that exists, or null.
-template <int kDim, typename F>
-__device__ __forceinline__ void load_tile(uint8_t *to, uint32_t dim, F &&where) {
-    constexpr int kPieces = kDim / 8, kPass = kThreads / kPieces;
-    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), slot = threadIdx.x % kPieces;
-#pragma unroll
-    for (int i = 0; i < kTileKeys / kPass; ++i) {
-        const uint32_t row = i * kPass + threadIdx.x / kPieces, piece = slot ^ exchange<kDim>(row);
-        const uint16_t *at = where(row);
-        at = at && piece * 8 < dim ? at + piece * 8 : (const uint16_t *)kZeros;
-        __builtin_amdgcn_global_load_lds((Global)at, (Lds)(to + (i * kThreads + wave * 64) * 16), 16, 0, 0);
-    }
+// 16 bytes per lane from memory straight to LDS, `to` (the same for all lanes) on.  The compiler, which cannot tell what is under way from what is read, would wait for such loads of its own before
+// every turned read of LDS; here arrived() waits for them, in its place.  No register waits for them.
+__device__ __forceinline__ void bring(uint32_t to, const void *base, uint32_t offset) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(to), "v"(offset), "s"(base));
 }
-// Every wavefront's loads have arrived and its reads are done.
-__device__ __forceinline__ void meet() {
+__device__ __forceinline__ void bring(uint32_t to, const void *at) { asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(to), "v"(at)); }
+
+// How a block loads tiles of kRows rows to LDS: a lane takes one piece of every kPass-th row.  Tiles whose rows all exist, of which there are `whole`, cost it three instructions a load; columns
+// that the head does not have are zeroed in LDS once, and left by lanes that are switched off.
+template <int kDim, int kRows, int kThreads>
+struct Loader {
+    static constexpr int kPieces = kDim / 8, kPass = kThreads / kPieces, kLoads = kRows / kPass;
+    static_assert(kPass % 16 == 0 && kRows % kPass == 0, "the exchange is the same for all of a lane's rows");
+    const uint16_t *base;
+    uint32_t ld, rows, whole, row, piece, offset, wave;
+    bool there;   // the head has the piece's columns
+    __device__ __forceinline__ Loader(const uint16_t *base_, uint64_t ld_, uint32_t rows_, uint32_t dim) : base(base_), ld((uint32_t)ld_), rows(rows_) {
+        wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64) * 1024;
+        row = threadIdx.x / kPieces;
+        piece = (threadIdx.x % kPieces ^ exchange<kDim>(row)) * 8;
+        offset = (row * ld + piece) * 2;
+        there = piece < dim;
+        whole = rows / kRows;
+    }
+    // The zeros, in `stages` places that lie one after the other
+    __device__ __forceinline__ void pad(uint8_t *place, int stages) const {
+        if (!there)
+            for (int i = 0; i < stages * kLoads; ++i) *((u4 *)place + i * kThreads + threadIdx.x) = u4{};
+    }
+    __device__ __forceinline__ const uint16_t *tile(uint32_t number) const { return base + (uint64_t)number * kRows * ld; }
+    // A whole tile's, from its place in memory on
+    __device__ __forceinline__ void load_whole(uint32_t place, const uint16_t *from) const {
+        if (there)
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) bring(place + wave + i * kThreads * 16, from + (uint64_t)(i * kPass) * ld, offset);
+    }
+    // Any tile's: zeros for columns that the head does not have, and for rows that do not exist
+    __device__ __forceinline__ void load_any(uint32_t place, uint32_t number) const {
+        const uint16_t *const from = tile(number);
+        uint32_t mine = row;
+        asm("" : "+v"(mine) : "s"(number));   // (worked out here, not kept in registers for every load)
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i, mine += kPass)
+            bring(place + wave + i * kThreads * 16, there && number * kRows + mine < rows ? from + (uint64_t)mine * ld + piece : (const uint16_t *)kZeros);
+    }
+};
+// The wavefront's own loads have arrived.
+__device__ __forceinline__ void arrived() {
+    __builtin_amdgcn_sched_barrier(0);
     asm volatile("" ::: "memory");
-    __builtin_amdgcn_s_waitcnt(0x0070);   // vmcnt(0), lgkmcnt(0)
+    __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0)
+    asm volatile("" ::: "memory");
+}
+// A barrier behind each wavefront's own accesses to LDS; nothing is moved across.
+__device__ __forceinline__ void meet() {
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt(0)
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
 }
 
+// Where the compiler is to place the reads of LDS of kProducts products: kReads of them with every kPer products, kAhead such groups before their use.
+template <int kProducts, int kPer, int kReads, int kAhead>
+__device__ __forceinline__ void pace() {
+#pragma unroll
+    for (int i = 0; i < kProducts / kPer + kAhead; ++i) {
+        if (i >= kAhead) __builtin_amdgcn_sched_group_barrier(0x008, kPer, 0);
+        if (i < kProducts / kPer) __builtin_amdgcn_sched_group_barrier(0x100, kReads, 0);
+    }
+}
+
+// Addresses in LDS are numbers here: a tile's, and a lane's own part, from which each read's is made by one instruction where it is read (kept in registers over the loops they would fill them).
+typedef const __attribute__((address_space(3))) uint8_t *InLds;
+__device__ __forceinline__ uint32_t address(const void *p) { return (uint32_t)(uintptr_t)(Lds)p; }
+__device__ __forceinline__ uint32_t anew(uint32_t x) {
+    asm("" : "+v"(x));
+    return x;
+}
 // Rows 32 half + lane % 32 of a tile, elements 16 step + 8 (lane / 32) + 0 .. 7 of each
 template <int kDim>
-__device__ __forceinline__ bf8 rows_of(const uint8_t *tile, int half, int step) {
-    const uint32_t lane = threadIdx.x & 63, r = lane & 31, g = lane >> 5;
-    return *(const bf8 *)(tile + (32 * half + r) * (2 * kDim) + (((2 * step + g) ^ exchange<kDim>(r)) << 4));
+__device__ __forceinline__ uint32_t lane_rows() {
+    const uint32_t r = threadIdx.x & 31, g = threadIdx.x >> 5 & 1;
+    return r * (2 * kDim) + ((g ^ exchange<kDim>(r)) << 4);
+}
+template <int kDim>
+__device__ __forceinline__ bf8 rows_of(uint32_t tile, uint32_t lane, int half, int step) {
+    typedef const __attribute__((address_space(3))) bf8 *At;
+    return *(At)((InLds)(uintptr_t)(tile + (lane ^ 32 * step)) + 64 * kDim * half);
 }
 // Column 32 d + lane % 32 of a tile, rows 16 t + 4 (lane / 32) + 0 .. 3 and 8 further
 template <int kDim>
-__device__ __forceinline__ bf8 columns_of(const uint8_t *tile, int t, int d) {
-    const uint32_t lane = threadIdx.x & 63, i = lane & 15, g = lane >> 5, piece = 4 * d + (lane >> 4 & 1) * 2 + (i >> 1 & 1), row = 4 * g + (i >> 2);
+__device__ __forceinline__ uint32_t lane_columns() {
+    const uint32_t lane = threadIdx.x & 63, i = lane & 15, row = 4 * (lane >> 5) + (i >> 2), piece = (lane >> 4 & 1) * 2 + (i >> 1 & 1);
+    return row * (2 * kDim) + ((piece ^ exchange<kDim>(row)) << 4) + (i & 1) * 8;   // (8 rows on, the exchange differs by 2)
+}
+template <int kDim>
+__device__ __forceinline__ bf8 columns_of(uint32_t tile, uint32_t lane, int t, int d) {
     typedef __attribute__((address_space(3))) s4 *At;
-    const uint8_t *lo = tile + (16 * t + row) * (2 * kDim) + ((piece ^ exchange<kDim>(row)) << 4) + (i & 1) * 8;
-    const uint8_t *hi = tile + (16 * t + 8 + row) * (2 * kDim) + ((piece ^ exchange<kDim>(row + 8)) << 4) + (i & 1) * 8;
-    const s4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((At)lo), b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((At)hi);
+    const s4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((At)((InLds)(uintptr_t)(tile + (lane ^ 64 * d)) + 32 * kDim * t));
+    const s4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((At)((InLds)(uintptr_t)(tile + (lane ^ 64 * d ^ 32)) + 32 * kDim * t + 16 * kDim));
     return __builtin_bit_cast(bf8, s8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]});
 }
 __device__ __forceinline__ f16 product(bf8 a, bf8 b, f16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
@@ -154,13 +231,13 @@ __device__ __forceinline__ bf8 eight_of(const f16 &x, int half) {
     for (int i = 0; i < 4; ++i) r[i] = bf16_pair(x[8 * half + 2 * i], x[8 * half + 2 * i + 1]);
     return __builtin_bit_cast(bf8, r);
 }
-// Where some rows of a block do not see some keys of a tile, a probability of zero must not meet infinities and NaNs of the tile's: zeros take their place in LDS.  True: there were some, and
-// the results that do feel them are to be made NaNs after the last tile.
-template <int kDim>
+// Where some rows of a block do not see some keys of a tile, a probability of zero must not meet infinities and NaNs of the tile's: zeros take their place in LDS.  A thread
+// looks at what it has loaded itself.  True: there were some, and the results that do feel them are to be made NaNs after the last tile.
+template <int kBytes, int kThreads>
 __device__ __forceinline__ bool clean(uint8_t *tile) {
     uint32_t bad = 0;
 #pragma unroll
-    for (int i = 0; i < kTileKeys * kDim * 2 / (kThreads * 16); ++i) {
+    for (int i = 0; i < kBytes / (kThreads * 16); ++i) {
         u4 *const at = (u4 *)tile + i * kThreads + threadIdx.x, v = *at;
         u4 w = v;
 #pragma unroll
@@ -170,12 +247,6 @@ __device__ __forceinline__ bool clean(uint8_t *tile) {
         bad |= changed;
     }
     return bad != 0;
-}
-__device__ __forceinline__ void meet_in_lds() {
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt(0)
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
 }
 // x <- NaN where a row of another matrix that x depends on (`sees`) is not finite; x: a lane's results of columns 32 d + 8 c + 4 g + 0 .. 3
 template <int kDim>
@@ -192,24 +263,39 @@ __device__ __forceinline__ void spoil(f16 (&x)[kDim / 32], const uint16_t *row, 
             }
 }
 // A lane's other half: what lane + 32 (- 32) has
-__device__ __forceinline__ float across(float x) { return __shfl_xor(x, 32); }
+__device__ __forceinline__ float across(float x) {
+    const uint32_t v = __float_as_uint(x);
+    const auto both = __builtin_amdgcn_permlane32_swap(v, v, false, false);   // (its low lanes everywhere, and its high ones)
+    return __uint_as_float(threadIdx.x & 32 ? both[0] : both[1]);
+}
 
 // Eight elements from a row's place on, zeros where there is no row or the head has fewer
 __device__ __forceinline__ bf8 piece_of(const uint16_t *row, uint32_t from, uint32_t dim) {
     const u4 zero = {};
     return __builtin_bit_cast(bf8, row && from < dim ? *(const u4 *)(row + from) : zero);
 }
-// Stores a lane's results of columns 32 d + 8 c + 4 g + 0 .. 3, d = 0 .. kDim / 32 - 1, of a row
-template <int kDim>
-__device__ __forceinline__ void store_row(uint16_t *row, const f16 (&x)[kDim / 32], float by, uint32_t dim) {
-    const uint32_t g = threadIdx.x >> 5 & 1;
+// Stores a wavefront's 32 rows of results, of which a lane has columns 32 d + 8 c + 4 g + 0 .. 3 of row lane % 32, times `by`: through LDS (`room`, of the wavefront's own), in whole lines.
+// where(row): the row's place, or null.
+template <int kDim, typename F>
+__device__ __forceinline__ void store_rows(uint8_t *room, const f16 (&x)[kDim / 32], float by, uint32_t dim, F &&where) {
+    constexpr int kPieces = kDim / 8, kPass = 64 / kPieces;
+    const uint32_t lane = threadIdx.x & 63, r = lane & 31, g = lane >> 5;
 #pragma unroll
     for (int d = 0; d < kDim / 32; ++d)
 #pragma unroll
         for (int c = 0; c < 4; ++c)
-            if (32 * d + 8 * c < (int)dim)
-                *(u2 *)(row + 32 * d + 8 * c + 4 * g) = u2{bf16_pair(x[d][4 * c] * by, x[d][4 * c + 1] * by), bf16_pair(x[d][4 * c + 2] * by, x[d][4 * c + 3] * by)};
+            *(u2 *)(room + r * (2 * kDim) + ((4 * d + c) ^ (r & (kPieces - 1))) * 16 + 8 * g) = u2{bf16_pair(x[d][4 * c] * by, x[d][4 * c + 1] * by), bf16_pair(x[d][4 * c + 2] * by, x[d][4 * c + 3] * by)};
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll 4
+    for (int i = 0; i < 32 / kPass; ++i) {
+        const uint32_t row = i * kPass + lane / kPieces, piece = lane % kPieces;
+        const u4 v = *(const u4 *)(room + row * (2 * kDim) + (piece ^ (row & (kPieces - 1))) * 16);
+        uint16_t *const to = where(row);
+        if (to && piece * 8 < dim) *(u4 *)(to + piece * 8) = v;
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 }
+// The same of partial results, in fp32, by each lane for itself
 template <int kDim>
 __device__ __forceinline__ void store_row(float *row, const f16 (&x)[kDim / 32], float by, uint32_t dim) {
     const uint32_t g = threadIdx.x >> 5 & 1;
@@ -229,148 +315,145 @@ __device__ __forceinline__ void part_of(uint32_t parts, uint32_t &from, uint32_t
     to = min(from + share, end);
 }
 
-// o and lse.  A wavefront has kGroups times 32 rows, a block 4 wavefronts; keys and values come in tiles of 64, the next one's loads under way while one is used.
-template <int kDim, int kGroups>
-__global__ __launch_bounds__(kThreads, kDim * kGroups > 128 ? 1 : 2) void k_attention(AttentionArgs p) {
-    constexpr int kSteps = kDim / 16, kWide = kDim / 32, kBytes = kTileKeys * kDim * 2, kRows = 32 * kGroups, kTile = 4 * kRows;
-    __shared__ __align__(16) uint8_t lds[4 * kBytes];
+// o and lse.  A block has 256 rows, a wavefront 32; keys and values come in tiles of 64.  The two wavefronts of a SIMD take turns: while one makes scores and joins values on the matrix cores, the
+// other makes probabilities of its scores, and all change places at a barrier.  A tile's keys are loaded two tiles ahead of their use, its values, which are used a tile later, one ahead.
+template <int kDim, int kWaves>
+__global__ __launch_bounds__(64 * kWaves, kDim == 64 ? 3 : 2) void k_attention(AttentionArgs p) {
+    constexpr int kThreads = 64 * kWaves, kTile = 32 * kWaves, kSteps = kDim / 16, kWide = kDim / 32, kBytes = kTileKeys * kDim * 2, kStages = 2;
+    __shared__ __align__(16) uint8_t lds[2 * kStages * kBytes];
     const Place at = place_of(p, false, kTile);
     if (at.none) return;
     const uint32_t rows = at.lq * p.group.by, row0 = at.tile * kTile;
     if (row0 >= rows) return;
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), r = lane & 31, g = lane >> 5;
     const float c = p.scale * kLog2e;
-
-    // rows that do not exist are the last one again, and not stored
-    bf8 q[kGroups][kSteps];
-    Seen seen[kGroups];
-    uint32_t token[kGroups], head[kGroups];
-#pragma unroll
-    for (int i = 0; i < kGroups; ++i) {
-        const uint32_t row = min(row0 + wave * kRows + 32 * i + r, rows - 1);
-        token[i] = quotient(row, p.group);
-        head[i] = at.head * p.group.by + row - token[i] * p.group.by;
-        const uint16_t *from = p.q + (uint64_t)(at.q0 + token[i]) * p.ld_q + head[i] * p.dim;
-#pragma unroll
-        for (int s = 0; s < kSteps; ++s) q[i][s] = piece_of(from, 16 * s + 8 * g, p.dim);
-        seen[i] = seen_by(p, at, token[i]);
-    }
-    // what the wavefront's and the block's rows see together: bounds do not fall from row to row
-    auto token_at = [&](uint32_t row) { return quotient(min(row, rows - 1), p.group); };
-    const Seen block_first = seen_by(p, at, token_at(row0)), block_last = seen_by(p, at, token_at(row0 + kTile - 1));
-    const Seen first = seen_by(p, at, token_at(row0 + wave * kRows)), last = seen_by(p, at, token_at(row0 + wave * kRows + kRows - 1));
-    uint32_t from = (uint32_t)block_first.lo / kTileKeys, to = ((uint32_t)block_last.hi + kTileKeys - 1) / kTileKeys;
-    if (to < from) to = from;
+    const Range range = range_of(p, at, rows, row0, wave, kTile);
+    uint32_t from = range.from, to = range.to;
     part_of(p.parts, from, to);
 
     const uint16_t *const k = p.k + (uint64_t)at.k0 * p.ld_k + at.head * p.dim, *const v = p.v + (uint64_t)at.k0 * p.ld_v + at.head * p.dim;
-    auto load = [&](uint32_t tile) {
-        uint8_t *const to = lds + (tile & 1) * (2 * kBytes);
-        load_tile<kDim>(to, p.dim, [&](uint32_t row) { const uint32_t key = tile * kTileKeys + row; return key < at.lk ? k + (uint64_t)key * p.ld_k : nullptr; });
-        load_tile<kDim>(to + kBytes, p.dim, [&](uint32_t row) { const uint32_t key = tile * kTileKeys + row; return key < at.lk ? v + (uint64_t)key * p.ld_v : nullptr; });
+    typedef Loader<kDim, kTileKeys, kThreads> Tiles;
+    const Tiles of_keys(k, p.ld_k, at.lk, p.dim), of_values(v, p.ld_v, at.lk, p.dim);
+    const uint16_t *next_keys = of_keys.tile(from), *next_values = of_values.tile(from);
+    const uint32_t keys = address(lds), values = keys + kStages * kBytes, lane_rows_at = lane_rows<kDim>(), lane_columns_at = lane_columns<kDim>();
+    auto load_keys = [&](uint32_t tile) {
+        const uint32_t place = keys + ((tile - from) & 1) * kBytes;
+        if (tile < min(to, of_keys.whole))
+            of_keys.load_whole(place, next_keys);
+        else if (tile < to) of_keys.load_any(place, tile);
+        next_keys += kTileKeys * (uint64_t)of_keys.ld;
     };
+    auto load_values = [&](uint32_t tile) {
+        const uint32_t place = values + ((tile - from) & 1) * kBytes;
+        if (tile < min(to, of_values.whole))
+            of_values.load_whole(place, next_values);
+        else if (tile < to) of_values.load_any(place, tile);
+        next_values += kTileKeys * (uint64_t)of_values.ld;
+    };
+    of_keys.pad(lds, 2 * kStages);
+    load_keys(from);
+    // rows that do not exist are the last one again, and not stored
+    auto token_of = [&](uint32_t row) { return quotient(min(row, rows - 1), p.group); };
+    const uint32_t row = min(row0 + wave * 32 + r, rows - 1), token = token_of(row), head = at.head * p.group.by + row - token * p.group.by;
+    bf8 q[kSteps];
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) q[s] = piece_of(p.q + (uint64_t)(at.q0 + token) * p.ld_q + head * p.dim, 16 * s + 8 * g, p.dim);
+    const Seen seen = seen_by(p, at, token);
 
-    f16 o[kGroups][kWide] = {};
-    float most[kGroups], sum[kGroups];
+    f16 o[kWide] = {}, s[2], ahead[2];   // ahead: the next tile's scores
+    bf8 prob[4];
+    float most = -INFINITY, sum = 0.f;
+    auto scores = [&](uint32_t tile) {
+        const uint32_t at = anew(lane_rows_at);
+        ahead[0] = ahead[1] = f16{};
 #pragma unroll
-    for (int i = 0; i < kGroups; ++i) { most[i] = -INFINITY; sum[i] = 0.f; }
-
-    bool bad = false;
-    auto work = [&](bool masked, const uint8_t *keys, const uint8_t *values, int key0) {
-        f16 s[kGroups][2] = {};
+        for (int step = 0; step < kSteps; ++step)
 #pragma unroll
-        for (int half = 0; half < 2; ++half)
-#pragma unroll
-            for (int step = 0; step < kSteps; ++step) {
-                const bf8 a = rows_of<kDim>(keys, half, step);
-#pragma unroll
-                for (int i = 0; i < kGroups; ++i) s[i][half] = product(a, q[i][step], s[i][half]);
-            }
-        bf8 prob[kGroups][4];
-#pragma unroll
-        for (int i = 0; i < kGroups; ++i) {
-            if (masked)
-#pragma unroll
-                for (int e = 0; e < 32; ++e) {
-                    const int key = key0 + e / 16 * 32 + e % 16 / 4 * 8 + 4 * (int)g + e % 4;
-                    s[i][e / 16][e % 16] = key >= seen[i].lo && key < seen[i].hi ? s[i][e / 16][e % 16] : -INFINITY;
-                }
-            float m = s[i][0][0];
-#pragma unroll
-            for (int e = 1; e < 32; ++e) m = fmaxf(m, s[i][e / 16][e % 16]);
-            m = fmaxf(m, across(m));
-            const bool more = m > most[i] + kSlack / c;   // (false for a NaN, and where nothing is seen yet)
-            if (__ballot(more)) {
-                const float by = more ? __builtin_amdgcn_exp2f((most[i] - m) * c) : 1.f;
-                most[i] = more ? m : most[i];
-                sum[i] *= by;
-#pragma unroll
-                for (int d = 0; d < kWide; ++d)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) o[i][d][e] *= by;
-            }
-            const float off = most[i] == -INFINITY ? 0.f : most[i] * c;
+            for (int half = 0; half < 2; ++half) ahead[half] = product(rows_of<kDim>(tile, at, half, step), q[step], ahead[half]);
+    };
+    auto probabilities = [&](int key0) {
+        if (!range.all_of(key0))
 #pragma unroll
             for (int e = 0; e < 32; ++e) {
-                const float x = __builtin_amdgcn_exp2f(fmaf(s[i][e / 16][e % 16], c, -off));
-                s[i][e / 16][e % 16] = x;
-                sum[i] += x;
+                const int key = key0 + e / 16 * 32 + e % 16 / 4 * 8 + 4 * (int)g + e % 4;
+                s[e / 16][e % 16] = key >= seen.lo && key < seen.hi ? s[e / 16][e % 16] : -INFINITY;
             }
-            // probabilities meet the values in bf16: 2^-9 of each, as the values have them themselves
+        float m = s[0][0];
 #pragma unroll
-            for (int t = 0; t < 4; ++t) prob[i][t] = eight_of(s[i][t / 2], t & 1);
+        for (int e = 1; e < 32; ++e) m = fmaxf(m, s[e / 16][e % 16]);
+        m = fmaxf(m, across(m));
+        const bool more = m > most + kSlack / c;   // (false for a NaN, and where nothing is seen yet)
+        if (__builtin_expect(__ballot(more) != 0, 0)) {
+            const float by = more ? __builtin_amdgcn_exp2f((most - m) * c) : 1.f;
+            most = more ? m : most;
+            sum *= by;
+#pragma unroll
+            for (int d = 0; d < kWide; ++d)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) o[d][e] *= by;
         }
+        const float off = most == -INFINITY ? 0.f : most * c;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+#pragma unroll
+            for (int e = 8 * t; e < 8 * t + 8; ++e) {
+                const float x = __builtin_amdgcn_exp2f(fmaf(s[e / 16][e % 16], c, -off));
+                s[e / 16][e % 16] = x;
+                sum += x;
+            }
+            prob[t] = eight_of(s[t / 2], t & 1);   // probabilities meet the values in bf16: 2^-9 of each, as the values have them themselves
+        }
+    };
+    auto join = [&](uint32_t tile) {
+        const uint32_t at = anew(lane_columns_at);
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
-            for (int d = 0; d < kWide; ++d) {
-                const bf8 a = columns_of<kDim>(values, t, d);
-#pragma unroll
-                for (int i = 0; i < kGroups; ++i) o[i][d] = product(a, prob[i][t], o[i][d]);
-            }
+            for (int d = 0; d < kWide; ++d) o[d] = product(columns_of<kDim>(tile, at, t, d), prob[t], o[d]);
     };
 
-    // whether the wavefront's rows see none, or each all, of a tile's keys, and the block's all
-    auto none_of = [&](int key0) { return key0 >= last.hi || key0 + kTileKeys <= first.lo; };
-    auto all_of = [&](int key0) { return key0 >= last.lo && key0 + kTileKeys <= first.hi; };
-    auto block_all_of = [&](int key0) { return key0 >= block_last.lo && key0 + kTileKeys <= block_first.hi; };
-    if (from < to) load(from);
-    for (uint32_t tile = from; tile < to; ++tile) {
+    bool bad = false;
+    if (from < to) {
+        arrived();
         meet();
-        if (tile + 1 < to) load(tile + 1);
-        const int key0 = (int)(tile * kTileKeys);
-        uint8_t *const keys = lds + (tile & 1) * (2 * kBytes);
-        if (!block_all_of(key0)) {
-            bad |= clean<kDim>(keys + kBytes);
-            meet_in_lds();
-        }
-        if (none_of(key0)) continue;
-        work(!all_of(key0), keys, keys + kBytes, key0);
+        load_values(from);
+        load_keys(from + 1);
+        scores(keys);
     }
+    for (uint32_t tile = from; tile < to; ++tile) {
+        const int key0 = (int)(tile * kTileKeys);
+        const uint32_t place = (tile - from) & 1;
+        arrived();
+        if (!range.block_all_of(key0)) bad |= clean<kBytes, kThreads>(lds + (kStages + place) * kBytes);
+        meet();
+        load_values(tile + 1);
+        load_keys(tile + 2);
+        s[0] = ahead[0];
+        s[1] = ahead[1];
+        probabilities(key0);
+        if (tile + 1 < to) scores(keys + (place ^ 1) * kBytes);
+        join(values + place * kBytes);
+    }
+
     if (__syncthreads_or(bad))
         for (uint32_t key = from * kTileKeys; key < min(to * kTileKeys, at.lk); ++key) {
             const int key0 = (int)(key / kTileKeys * kTileKeys);
-            if (none_of(key0) || block_all_of(key0)) continue;
-#pragma unroll
-            for (int i = 0; i < kGroups; ++i) spoil<kDim>(o[i], v + (uint64_t)key * p.ld_v, p.dim, (int)key >= seen[i].lo && (int)key < seen[i].hi);
+            if (range.block_all_of(key0)) continue;
+            spoil<kDim>(o, v + (uint64_t)key * p.ld_v, p.dim, (int)key >= seen.lo && (int)key < seen.hi);
         }
-
-#pragma unroll
-    for (int i = 0; i < kGroups; ++i) {
-        sum[i] += across(sum[i]);
-        if (row0 + wave * kRows + 32 * i + r >= rows) continue;
-        const float by = sum[i] == 0.f ? 0.f : 1.f / sum[i];
-        const float lse = sum[i] == 0.f ? -INFINITY : (most[i] * c + __log2f(sum[i])) * kLn2;
-        const uint64_t row = (uint64_t)(at.q0 + token[i]) * p.heads + head[i];
-        if (p.parts == 1) {
-            store_row<kDim>(p.out + (uint64_t)(at.q0 + token[i]) * p.ld_out + head[i] * p.dim, o[i], by, p.dim);
-            if (p.lse && g == 0) p.lse[row] = lse;
-        } else {
-            const uint64_t all = (uint64_t)p.q_rows * p.heads, place = blockIdx.y * all + row;
-            store_row<kDim>(p.scratch + place * p.dim, o[i], by, p.dim);
-            if (g == 0) p.scratch[all * p.parts * p.dim + place] = lse;
-        }
-    }
+    sum += across(sum);
+    const float by = sum == 0.f ? 0.f : 1.f / sum;
+    const float lse = sum == 0.f ? -INFINITY : (most * c + __log2f(sum)) * kLn2;
+    const uint64_t line = (uint64_t)(at.q0 + token) * p.heads + head, all = (uint64_t)p.q_rows * p.heads;
+    if (p.parts == 1)
+        store_rows<kDim>(lds + wave * 64 * kDim, o, by, p.dim, [&](uint32_t i) {
+            const uint32_t row = row0 + wave * 32 + i, t = token_of(row);
+            return row < rows ? p.out + (uint64_t)(at.q0 + t) * p.ld_out + (at.head * p.group.by + row - t * p.group.by) * p.dim : nullptr;
+        });
+    if (row0 + wave * 32 + r >= rows) return;
+    if (p.parts > 1) store_row<kDim>(p.scratch + (blockIdx.y * all + line) * p.dim, o, by, p.dim);
+    float *const to_lse = p.parts > 1 ? p.scratch + all * p.parts * p.dim + blockIdx.y * all : p.lse;
+    if (to_lse && g == 0) to_lse[line] = lse;
 }
 
 // Rows of sequences: what lies before the first and behind the last is let be.
@@ -378,36 +461,53 @@ __device__ __forceinline__ bool belongs(uint32_t row, const uint32_t *starts, ui
     return row < rows && (!starts || (row >= starts[0] && row < starts[sequences]));
 }
 
-// o and lse of the parts' ones: o = sum w_i o_i / sum w_i, w_i = exp(lse_i - the largest).  16 lanes per row and head.
-__global__ __launch_bounds__(kThreads) void k_attention_join(AttentionArgs p) {
-    const uint64_t all = (uint64_t)p.q_rows * p.heads, id = (uint64_t)blockIdx.x * (kThreads / 16) + threadIdx.x / 16;
+// o and lse of the parts' ones: o = sum w_i o_i / sum w_i, w_i = exp(lse_i - the largest).  16 lanes per row and head; eight parts' loads at a time, which is what it waits for.
+__global__ __launch_bounds__(kBlock) void k_attention_join(AttentionArgs p) {
+    const uint32_t all = p.q_rows * p.heads, id = blockIdx.x * (kBlock / 16) + threadIdx.x / 16;   // (below 2^24 / 8, by the room that parts have)
     if (id >= all) return;
-    const uint32_t row = (uint32_t)(id / p.heads), head = (uint32_t)(id - (uint64_t)row * p.heads), from = (threadIdx.x & 15) * 8;
+    const uint32_t row = id / p.heads, head = id - row * p.heads, from = (threadIdx.x & 15) * 8;
     if (!belongs(row, p.q_starts, p.sequences, p.q_rows)) return;
-    const float *const lses = p.scratch + all * p.parts * p.dim + id;
+    const bool mine = from < p.dim;
+    const float *const lses = p.scratch + (uint64_t)all * p.parts * p.dim + id, *const place = p.scratch + (uint64_t)id * p.dim + (mine ? from : 0);
     float most = -INFINITY, total = 0.f, x[8] = {};
-    for (uint32_t i = 0; i < p.parts; ++i) most = fmaxf(most, lses[i * all]);
-    for (uint32_t i = 0; i < p.parts; ++i) {
-        const float lse = lses[i * all], w = lse == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((lse - most) * kLog2e);
-        total += w;
-        if (from < p.dim && w != 0.f) {
-            const f4 *at = (const f4 *)(p.scratch + (i * all + id) * p.dim + from);
+    for (uint32_t i0 = 0; i0 < p.parts; i0 += 8) {
+        float lse[8];
+        f4 part[8][2];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] += w * at[e / 4][e % 4];
+        for (int i = 0; i < 8; ++i) {
+            const uint64_t n = min(i0 + i, p.parts - 1) * (uint64_t)all;
+            lse[i] = lses[n];
+            part[i][0] = *(const f4 *)(place + n * p.dim);
+            part[i][1] = *(const f4 *)(place + n * p.dim + 4);
+        }
+        float next = most;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) next = fmaxf(next, lse[i]);
+        const float by = most == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((most - next) * kLog2e);
+        total *= by;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] *= by;
+        most = next;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float w = i0 + i >= p.parts || lse[i] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((lse[i] - most) * kLog2e);
+            total += w;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = fmaf(w, w == 0.f ? 0.f : part[i][e / 4][e % 4], x[e]);
         }
     }
     const float by = total == 0.f ? 0.f : 1.f / total;
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[e] *= by;
-    if (from < p.dim) store_chunk((Bf16 *)p.out + (uint64_t)row * p.ld_out + head * p.dim + from, 8, x);
+    if (mine) store_chunk((Bf16 *)p.out + (uint64_t)row * p.ld_out + head * p.dim + from, 8, x);
     if (p.lse && from == 0) p.lse[id] = total == 0.f ? -INFINITY : most + __log2f(total) * kLn2;
 }
 
-// dq, and delta for the kernel after it.  As the forward pass, with three products a tile.
-template <int kDim, int kGroups>
-__global__ __launch_bounds__(kThreads, kDim * kGroups >= 128 ? 1 : 2) void k_attention_dq(AttentionArgs p) {
-    constexpr int kSteps = kDim / 16, kWide = kDim / 32, kBytes = kTileKeys * kDim * 2, kRows = 32 * kGroups, kTile = 4 * kRows;
-    __shared__ __align__(16) uint8_t lds[4 * kBytes];
+// dq, and delta for the kernel after it.  As the forward pass, with three products a tile of 64 keys, taken in two halves.
+template <int kDim, int kWaves>
+__global__ __launch_bounds__(64 * kWaves, kDim == 64 ? 3 : 2) void k_attention_dq(AttentionArgs p) {
+    constexpr int kThreads = 64 * kWaves, kTile = 32 * kWaves, kSteps = kDim / 16, kWide = kDim / 32, kBytes = kTileKeys * kDim * 2, kStages = 2;
+    __shared__ __align__(16) uint8_t lds[2 * kStages * kBytes];
     const Place at = place_of(p, false, kTile);
     if (at.none) return;
     const uint32_t rows = at.lq * p.group.by, row0 = at.tile * kTile;
@@ -415,283 +515,282 @@ __global__ __launch_bounds__(kThreads, kDim * kGroups >= 128 ? 1 : 2) void k_att
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), r = lane & 31, g = lane >> 5;
     const float c = p.scale * kLog2e;
 
-    bf8 q[kGroups][kSteps], grad[kGroups][kSteps];
-    Seen seen[kGroups];
-    uint32_t token[kGroups], head[kGroups];
-    float lse[kGroups], delta[kGroups];
+    const uint32_t wanted = row0 + wave * 32 + r, row = min(wanted, rows - 1), token = quotient(row, p.group), head = at.head * p.group.by + row - token * p.group.by;
+    const uint64_t line = at.q0 + token;
+    const uint32_t col = head * p.dim;
+    bf8 q[kSteps], grad[kSteps];
+    float delta = 0.f;
 #pragma unroll
-    for (int i = 0; i < kGroups; ++i) {
-        const uint32_t wanted = row0 + wave * kRows + 32 * i + r, row = min(wanted, rows - 1);
-        token[i] = quotient(row, p.group);
-        head[i] = at.head * p.group.by + row - token[i] * p.group.by;
-        const uint64_t line = at.q0 + token[i];
-        const uint32_t col = head[i] * p.dim;
-        delta[i] = 0.f;
+    for (int s = 0; s < kSteps; ++s) {
+        q[s] = piece_of(p.q + line * p.ld_q + col, 16 * s + 8 * g, p.dim);
+        grad[s] = piece_of(p.grad + line * p.ld_grad + col, 16 * s + 8 * g, p.dim);
+        const bf8 o = piece_of(p.o + line * p.ld_o + col, 16 * s + 8 * g, p.dim);
 #pragma unroll
-        for (int s = 0; s < kSteps; ++s) {
-            q[i][s] = piece_of(p.q + line * p.ld_q + col, 16 * s + 8 * g, p.dim);
-            grad[i][s] = piece_of(p.grad + line * p.ld_grad + col, 16 * s + 8 * g, p.dim);
-            const bf8 o = piece_of(p.o + line * p.ld_o + col, 16 * s + 8 * g, p.dim);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) delta[i] = fmaf((float)grad[i][s][e], (float)o[e], delta[i]);
-        }
-        delta[i] += across(delta[i]);
-        const float l = p.lse[line * p.heads + head[i]];
-        lse[i] = l == -INFINITY ? INFINITY : l * kLog2e;   // a row that sees nothing: p = 0
-        seen[i] = seen_by(p, at, token[i]);
-        if (blockIdx.y == 0 && g == 0 && wanted < rows) p.delta[line * p.heads + head[i]] = delta[i];
+        for (int e = 0; e < 8; ++e) delta = fmaf((float)grad[s][e], (float)o[e], delta);
     }
-    auto token_at = [&](uint32_t row) { return quotient(min(row, rows - 1), p.group); };
-    const Seen block_first = seen_by(p, at, token_at(row0)), block_last = seen_by(p, at, token_at(row0 + kTile - 1));
-    const Seen first = seen_by(p, at, token_at(row0 + wave * kRows)), last = seen_by(p, at, token_at(row0 + wave * kRows + kRows - 1));
-    uint32_t from = (uint32_t)block_first.lo / kTileKeys, to = ((uint32_t)block_last.hi + kTileKeys - 1) / kTileKeys;
-    if (to < from) to = from;
+    delta += across(delta);
+    float lse = p.lse[line * p.heads + head];
+    lse = lse == -INFINITY ? INFINITY : lse * kLog2e;   // a row that sees nothing: p = 0
+    if (blockIdx.y == 0 && g == 0 && wanted < rows) p.delta[line * p.heads + head] = delta;
+    const Range range = range_of(p, at, rows, row0, wave, kTile);
+    const Seen seen = seen_by(p, at, token);
+    uint32_t from = range.from, to = range.to;
     part_of(p.parts, from, to);
 
     const uint16_t *const k = p.k + (uint64_t)at.k0 * p.ld_k + at.head * p.dim, *const v = p.v + (uint64_t)at.k0 * p.ld_v + at.head * p.dim;
-    auto load = [&](uint32_t tile) {
-        uint8_t *const to = lds + (tile & 1) * (2 * kBytes);
-        load_tile<kDim>(to, p.dim, [&](uint32_t row) { const uint32_t key = tile * kTileKeys + row; return key < at.lk ? k + (uint64_t)key * p.ld_k : nullptr; });
-        load_tile<kDim>(to + kBytes, p.dim, [&](uint32_t row) { const uint32_t key = tile * kTileKeys + row; return key < at.lk ? v + (uint64_t)key * p.ld_v : nullptr; });
+    typedef Loader<kDim, kTileKeys, kThreads> Tiles;
+    const Tiles of_keys(k, p.ld_k, at.lk, p.dim), of_values(v, p.ld_v, at.lk, p.dim);
+    const uint32_t keys = address(lds), values = keys + kStages * kBytes, lane_rows_at = lane_rows<kDim>(), lane_columns_at = lane_columns<kDim>();
+    const uint16_t *next_keys = of_keys.tile(from), *next_values = of_values.tile(from);
+    auto load = [&](uint32_t tile, uint32_t stage) {
+        if (tile < min(to, of_keys.whole)) {
+            of_keys.load_whole(keys + stage * kBytes, next_keys);
+            of_values.load_whole(values + stage * kBytes, next_values);
+        } else if (tile < to) {
+            of_keys.load_any(keys + stage * kBytes, tile);
+            of_values.load_any(values + stage * kBytes, tile);
+        }
+        next_keys += kTileKeys * (uint64_t)of_keys.ld;
+        next_values += kTileKeys * (uint64_t)of_values.ld;
     };
 
-    f16 dq[kGroups][kWide] = {};
+    of_keys.pad(lds, 2 * kStages);
+
+    f16 dq[kWide] = {}, s, dp;
+    bf8 ds[2];
+    auto scores = [&](uint32_t stage, int half) {
+        const uint32_t at = anew(lane_rows_at);
+        s = f16{};
+#pragma unroll
+        for (int e = 0; e < 16; ++e) dp[e] = -delta;
+#pragma unroll
+        for (int step = 0; step < kSteps; ++step) {
+            s = product(rows_of<kDim>(keys + stage * kBytes, at, half, step), q[step], s);
+            dp = product(rows_of<kDim>(keys + stage * kBytes, at, half + kStages * kTileKeys / 32, step), grad[step], dp);   // (the values, as far behind the keys)
+        }
+    };
+    auto slopes = [&](int tile_key, int half) {
+        const int key0 = tile_key + 32 * half;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[e] = __builtin_amdgcn_exp2f(fmaf(s[e], c, -lse)) * dp[e];
+        if (!range.all_of(tile_key))
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const int key = key0 + e / 4 * 8 + 4 * (int)g + e % 4;
+                s[e] = key >= seen.lo && key < seen.hi ? s[e] : 0.f;
+            }
+        // ds meets the keys in bf16, as p its values in the forward pass
+#pragma unroll
+        for (int t = 0; t < 2; ++t) ds[t] = eight_of(s, t);
+    };
+    auto join = [&](uint32_t stage, int half) {
+        const uint32_t at = anew(lane_columns_at);
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int d = 0; d < kWide; ++d) dq[d] = product(columns_of<kDim>(keys + stage * kBytes, at, 2 * half + t, d), ds[t], dq[d]);
+    };
+
     bool bad = false;
-    auto work = [&](bool masked, const uint8_t *keys, const uint8_t *values, int key0) {
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            f16 s[kGroups] = {}, dp[kGroups];
-#pragma unroll
-            for (int i = 0; i < kGroups; ++i)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) dp[i][e] = -delta[i];
-#pragma unroll
-            for (int step = 0; step < kSteps; ++step) {
-                const bf8 a = rows_of<kDim>(keys, half, step), b = rows_of<kDim>(values, half, step);
-#pragma unroll
-                for (int i = 0; i < kGroups; ++i) {
-                    s[i] = product(a, q[i][step], s[i]);
-                    dp[i] = product(b, grad[i][step], dp[i]);
-                }
-            }
-            bf8 ds[kGroups][2];
-#pragma unroll
-            for (int i = 0; i < kGroups; ++i) {
-#pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    float x = __builtin_amdgcn_exp2f(fmaf(s[i][e], c, -lse[i])) * dp[i][e];
-                    if (masked) {
-                        const int key = key0 + 32 * half + e / 4 * 8 + 4 * (int)g + e % 4;
-                        x = key >= seen[i].lo && key < seen[i].hi ? x : 0.f;
-                    }
-                    s[i][e] = x;
-                }
-                // ds meets the keys in bf16, as p its values in the forward pass
-#pragma unroll
-                for (int t = 0; t < 2; ++t) ds[i][t] = eight_of(s[i], t);
-            }
-#pragma unroll
-            for (int t = 0; t < 2; ++t)
-#pragma unroll
-                for (int d = 0; d < kWide; ++d) {
-                    const bf8 a = columns_of<kDim>(keys, 2 * half + t, d);
-#pragma unroll
-                    for (int i = 0; i < kGroups; ++i) dq[i][d] = product(a, ds[i][t], dq[i][d]);
-                }
-        }
-    };
-
-    // whether the wavefront's rows see none, or each all, of a tile's keys, and the block's all
-    auto none_of = [&](int key0) { return key0 >= last.hi || key0 + kTileKeys <= first.lo; };
-    auto all_of = [&](int key0) { return key0 >= last.lo && key0 + kTileKeys <= first.hi; };
-    auto block_all_of = [&](int key0) { return key0 >= block_last.lo && key0 + kTileKeys <= block_first.hi; };
-    if (from < to) load(from);
-    for (uint32_t tile = from; tile < to; ++tile) {
-        meet();
-        if (tile + 1 < to) load(tile + 1);
+    if (from < to) load(from, 0);
+    for (uint32_t tile = from, stage = 0; tile < to; ++tile, stage ^= 1) {
         const int key0 = (int)(tile * kTileKeys);
-        uint8_t *const keys = lds + (tile & 1) * (2 * kBytes);
-        if (!block_all_of(key0)) {
-            bad |= clean<kDim>(keys);
-            meet_in_lds();
-        }
-        if (none_of(key0)) continue;
-        work(!all_of(key0), keys, keys + kBytes, key0);
+        arrived();
+        if (!range.block_all_of(key0)) bad |= clean<kBytes, kThreads>(lds + stage * kBytes);
+        meet();
+        load(tile + 1, stage ^ 1);
+        scores(stage, 0);
+        slopes(key0, 0);
+        scores(stage, 1);
+        join(stage, 0);
+        slopes(key0, 1);
+        join(stage, 1);
     }
+
     if (__syncthreads_or(bad))   // a row that sees such a key (whose scores were made without them): NaNs
         for (uint32_t key = from * kTileKeys; key < min(to * kTileKeys, at.lk); ++key) {
             const int key0 = (int)(key / kTileKeys * kTileKeys);
-            if (none_of(key0) || block_all_of(key0)) continue;
+            if (range.block_all_of(key0)) continue;
             bool bad_key = false;
             for (uint32_t d = lane; d < p.dim; d += 64) bad_key |= (k[(uint64_t)key * p.ld_k + d] & 0x7f80u) == 0x7f80u;
             if (!__ballot(bad_key)) continue;
+            if ((int)key >= seen.lo && (int)key < seen.hi)
 #pragma unroll
-            for (int i = 0; i < kGroups; ++i)
-                if ((int)key >= seen[i].lo && (int)key < seen[i].hi)
+                for (int d = 0; d < kWide; ++d)
 #pragma unroll
-                    for (int d = 0; d < kWide; ++d)
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) dq[i][d][e] = NAN;
+                    for (int e = 0; e < 16; ++e) dq[d][e] = NAN;
         }
-#pragma unroll
-    for (int i = 0; i < kGroups; ++i) {
-        if (row0 + wave * kRows + 32 * i + r >= rows) continue;
-        const uint64_t line = at.q0 + token[i];
-        if (p.parts == 1) store_row<kDim>(p.out + line * p.ld_out + head[i] * p.dim, dq[i], p.scale, p.dim);
-        else store_row<kDim>(p.scratch + ((blockIdx.y * (uint64_t)p.q_rows + line) * p.heads + head[i]) * p.dim, dq[i], p.scale, p.dim);
-    }
+    if (p.parts == 1)
+        store_rows<kDim>(lds + wave * 64 * kDim, dq, p.scale, p.dim, [&](uint32_t i) {
+            const uint32_t row = row0 + wave * 32 + i, t = quotient(min(row, rows - 1), p.group);
+            return row < rows ? p.out + (uint64_t)(at.q0 + t) * p.ld_out + (at.head * p.group.by + row - t * p.group.by) * p.dim : nullptr;
+        });
+    else if (wanted < rows) store_row<kDim>(p.scratch + (blockIdx.y * (uint64_t)p.q_rows + line) * p.heads * p.dim + col, dq, p.scale, p.dim);
 }
 
-// dk and dv.  A wavefront has 32 keys, a block 128; rows of q and of the gradient come in tiles of 64.
-template <int kDim>
-__global__ __launch_bounds__(kThreads, kDim > 64 ? 1 : 2) void k_attention_dkv(AttentionArgs p) {
-    constexpr int kSteps = kDim / 16, kWide = kDim / 32, kBytes = kTileKeys * kDim * 2, kTile = 128, kStats = 2 * kTileKeys * 4;
-    __shared__ __align__(16) uint8_t lds[4 * kBytes + 2 * kStats];
+// dk and dv.  A block has 256 keys, a wavefront 32; rows of q and of the gradient come in tiles of 32, one head of the group after the other, and the wavefronts of a SIMD take turns as in the
+// forward pass.  The block's values lie in LDS (in registers, with the keys, there would be room for one wavefront per SIMD).
+template <int kDim, int kWaves>
+__global__ __launch_bounds__(64 * kWaves, kDim == 64 ? 3 : 2) void k_attention_dkv(AttentionArgs p) {
+    constexpr int kThreads = 64 * kWaves, kTile = 32 * kWaves, kSteps = kDim / 16, kWide = kDim / 32, kRows = kDim == 64 || kWaves == 8 ? 64 : 32, kHalves = kRows / 32, kBytes = kRows * kDim * 2, kStats = 2 * kRows, kStages = 2, kValues = kTile * kDim * 2;
+    __shared__ __align__(16) uint8_t lds[kStages * (2 * kBytes + kStats * 4) + kValues];
     const Place at = place_of(p, true, kTile);
     if (at.none || at.tile * kTile >= at.lk) return;
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), r = lane & 31, g = lane >> 5;
-    const uint32_t rows = at.lq * p.group.by, block_key = at.tile * kTile, wave_key = block_key + wave * 32, key = wave_key + r;
+    const uint32_t block_key = at.tile * kTile, wave_key = block_key + wave * 32, key = wave_key + r;
     const float c = p.scale * kLog2e;
-    const int64_t off = (int64_t)at.lk - at.lq;   // a query's number and this are its position
+    const int off = (int)at.lk - (int)at.lq;   // a query's number and this are its position
 
-    bf8 k[kSteps], v[kSteps];
+    bf8 k[kSteps];
     {
-        const bool there = key < at.lk;
-        const uint16_t *const from_k = there ? p.k + (uint64_t)(at.k0 + key) * p.ld_k + at.head * p.dim : nullptr;
-        const uint16_t *const from_v = there ? p.v + (uint64_t)(at.k0 + key) * p.ld_v + at.head * p.dim : nullptr;
+        const uint16_t *const from = key < at.lk ? p.k + (uint64_t)(at.k0 + key) * p.ld_k + at.head * p.dim : nullptr;
 #pragma unroll
-        for (int s = 0; s < kSteps; ++s) { k[s] = piece_of(from_k, 16 * s + 8 * g, p.dim); v[s] = piece_of(from_v, 16 * s + 8 * g, p.dim); }
+        for (int s = 0; s < kSteps; ++s) k[s] = piece_of(from, 16 * s + 8 * g, p.dim);
     }
-    // queries [first, end) that see some of the keys from `key` to the one before `last`
-    auto first_query = [&](uint32_t from) { return p.causal ? (uint32_t)min((int64_t)at.lq, max((int64_t)0, (int64_t)from - off)) : 0u; };
-    auto end_query = [&](uint32_t to) { return p.window ? (uint32_t)min((int64_t)at.lq, max((int64_t)0, (int64_t)to - 1 + p.window - off)) : at.lq; };
-    const uint32_t block_end = min(block_key + kTile, at.lk), wave_end = min(wave_key + 32, at.lk);
-    uint32_t from = first_query(block_key) * p.group.by / kTileKeys, to = (end_query(block_end) * p.group.by + kTileKeys - 1) / kTileKeys;
-    if (to < from) to = from;
-    part_of(p.parts, from, to);
-    const uint32_t wave_first = first_query(wave_key) * p.group.by, wave_last = wave_key < at.lk ? end_query(wave_end) * p.group.by : 0;   // rows
-    // rows from which, and up to which, all keys from `lo` to the one before `hi` are seen
-    auto whole_from = [&](uint32_t hi) { return p.causal ? (uint32_t)min((int64_t)at.lq, max((int64_t)0, (int64_t)hi - 1 - off)) * p.group.by : 0u; };
-    auto whole_to = [&](uint32_t lo, uint32_t hi) {
-        return hi > at.lk ? 0u : p.window ? (uint32_t)min((int64_t)at.lq, max((int64_t)0, (int64_t)lo + p.window - off)) * p.group.by : rows;
-    };
+    // queries from the first that sees one of the keys from `lo` to `hi` - 1, up to the last; and those that see all of them
+    auto query = [&](int key, int further) { return (uint32_t)max(0, min((int)at.lq, key - off + further)); };
+    auto first_query = [&](uint32_t lo) { return p.causal ? query(lo, 0) : 0u; };
+    auto end_query = [&](uint32_t hi) { return p.window ? query(hi - 1, p.window) : at.lq; };
+    auto whole_from = [&](uint32_t hi) { return p.causal ? query(hi - 1, 0) : 0u; };
+    auto whole_to = [&](uint32_t lo, uint32_t hi) { return hi > at.lk ? 0u : p.window ? query(lo, p.window) : at.lq; };
+    const uint32_t seen_from = first_query(key), seen_to = key < at.lk ? end_query(key + 1) : 0u;   // those that see the lane's
     const uint32_t whole_first = whole_from(wave_key + 32), whole_last = whole_to(wave_key, wave_key + 32);
     const uint32_t block_first = whole_from(block_key + kTile), block_last = whole_to(block_key, block_key + kTile);
+    const uint32_t tile0 = first_query(block_key) / kRows, tile1 = (end_query(min(block_key + kTile, at.lk)) + kRows - 1) / kRows, tiles = tile1 > tile0 ? tile1 - tile0 : 0u;
+    // whether all of 32 queries see all of the wavefront's keys, and a tile's all of the block's
+    auto all_of = [&](uint32_t lo) { return lo >= whole_first && lo + 32 <= whole_last; };
+    auto block_all_of = [&](uint32_t lo) { return lo >= block_first && lo + kRows <= block_last; };
 
-    auto load = [&](uint32_t tile) {
-        uint8_t *const to = lds + (tile & 1) * (2 * kBytes);
-        auto row_of = [&](const uint16_t *base, uint64_t ld, uint32_t row) {
-            row += tile * kTileKeys;
-            const uint32_t t = quotient(row, p.group);
-            return row < rows ? base + (uint64_t)(at.q0 + t) * ld + (at.head * p.group.by + row - t * p.group.by) * p.dim : nullptr;
-        };
-        load_tile<kDim>(to, p.dim, [&](uint32_t row) { return row_of(p.q, p.ld_q, row); });
-        load_tile<kDim>(to + kBytes, p.dim, [&](uint32_t row) { return row_of(p.grad, p.ld_grad, row); });
-    };
-    // lse (in powers of two) and -delta of a tile's rows: one per thread of the first two wavefronts
-    float *const stats = (float *)(lds + 4 * kBytes);
-    auto stat = [&](uint32_t tile) {
-        if (threadIdx.x >= 2 * kTileKeys) return 0.f;
-        const uint32_t row = tile * kTileKeys + (threadIdx.x & 63), t = quotient(min(row, rows - 1), p.group);
-        const uint64_t place = (uint64_t)(at.q0 + t) * p.heads + at.head * p.group.by + min(row, rows - 1) - t * p.group.by;
-        if (threadIdx.x < kTileKeys) {
-            const float l = p.lse[place];
-            return row >= rows || l == -INFINITY ? INFINITY : l * kLog2e;
+    uint32_t from = 0, to = tiles * p.group.by;
+    part_of(p.parts, from, to);
+    const uint64_t head0 = (uint64_t)at.head * p.group.by;
+    const uint16_t *const q = p.q + at.q0 * p.ld_q + head0 * p.dim, *const grad = p.grad + at.q0 * p.ld_grad + head0 * p.dim;
+    const uint32_t queries = address(lds), grads = queries + kStages * kBytes, values = grads + kStages * kBytes, lane_rows_at = lane_rows<kDim>(), lane_columns_at = lane_columns<kDim>();
+    float *const stats = (float *)(lds + 2 * kStages * kBytes + kValues);
+    // What comes next: tile `number` of a head of the group.  lse (in powers of two) and -delta of its rows come by one of the first wavefronts' lanes, and go to LDS when they have arrived.
+    uint32_t head = tiles ? from / tiles : 0u, number = tile0 + from - head * tiles;
+    Loader<kDim, kRows, kThreads> of_queries(q + head * p.dim, p.ld_q, at.lq, p.dim), of_grads(grad + head * p.dim, p.ld_grad, at.lq, p.dim);
+    const uint16_t *next_queries = of_queries.tile(number), *next_grads = of_grads.tile(number);
+    of_queries.pad(lds, 2 * kStages);
+    float stat = 0.f;
+    auto load = [&](uint32_t stage) {
+        if (threadIdx.x < kStats) {
+            const uint32_t row = number * kRows + threadIdx.x % kRows;
+            const uint64_t place = (uint64_t)(at.q0 + min(row, at.lq - 1)) * p.heads + head0 + head;
+            stat = threadIdx.x < kRows ? p.lse[place] : p.delta[place];
+            if (threadIdx.x < kRows) stat = row >= at.lq || stat == -INFINITY ? INFINITY : stat * kLog2e;
+            else stat = row < at.lq ? -stat : 0.f;
         }
-        return row < rows ? -p.delta[place] : 0.f;
+        if (number < of_queries.whole) {
+            of_queries.load_whole(queries + stage * kBytes, next_queries);
+            of_grads.load_whole(grads + stage * kBytes, next_grads);
+        } else {
+            of_queries.load_any(queries + stage * kBytes, number);
+            of_grads.load_any(grads + stage * kBytes, number);
+        }
+        next_queries += kRows * (uint64_t)of_queries.ld;
+        next_grads += kRows * (uint64_t)of_grads.ld;
+        if (++number == tile1) {
+            number = tile0;
+            ++head;
+            of_queries.base += p.dim;
+            of_grads.base += p.dim;
+            next_queries = of_queries.tile(tile0);
+            next_grads = of_grads.tile(tile0);
+        }
     };
-    auto keep = [&](uint32_t tile, float x) { if (threadIdx.x < 2 * kTileKeys) stats[(tile & 1) * 2 * kTileKeys + threadIdx.x] = x; };
+    auto keep = [&](uint32_t stage) { if (threadIdx.x < kStats) stats[stage * kStats + threadIdx.x] = stat; };
 
-    f16 dk[kWide] = {}, dv[kWide] = {};
-    bool bad = false;
-    auto work = [&](bool masked, const uint8_t *queries, const uint8_t *grads, const float *lse, const float *delta, int half, uint32_t row0) {
-        f16 s = {}, dp;
+    f16 dk[kWide] = {}, dv[kWide] = {}, s, dp;
+    bf8 prob[2], ds[2];
+    auto scores = [&](uint32_t stage, int half) {
+        const uint32_t at = anew(lane_rows_at);
+        s = f16{};
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const f4 d = *(const f4 *)(delta + 32 * half + 8 * q + 4 * g);
+        for (int i = 0; i < 4; ++i) {
+            const f4 d = *(const f4 *)(stats + stage * kStats + kRows + 32 * half + 8 * i + 4 * g);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) dp[4 * q + e] = d[e];
+            for (int e = 0; e < 4; ++e) dp[4 * i + e] = d[e];
         }
 #pragma unroll
         for (int step = 0; step < kSteps; ++step) {
-            s = product(rows_of<kDim>(queries, half, step), k[step], s);
-            dp = product(rows_of<kDim>(grads, half, step), v[step], dp);
-        }
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const f4 l = *(const f4 *)(lse + 32 * half + 8 * q + 4 * g);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                float x = __builtin_amdgcn_exp2f(fmaf(s[4 * q + e], c, -l[e]));
-                if (masked) {
-                    const uint32_t row = row0 + 32 * half + 8 * q + 4 * g + e;
-                    const Seen by = seen_by(p, at, quotient(row, p.group));
-                    const bool does = row < rows && (int)key >= by.lo && (int)key < by.hi;
-                    x = does ? x : 0.f;
-                    s[4 * q + e] = x;
-                    dp[4 * q + e] = does ? x * dp[4 * q + e] : 0.f;
-                } else {
-                    s[4 * q + e] = x;
-                    dp[4 * q + e] *= x;
-                }
-            }
-        }
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            const bf8 prob = eight_of(s, t), ds = eight_of(dp, t);
-#pragma unroll
-            for (int d = 0; d < kWide; ++d) {
-                const bf8 a = columns_of<kDim>(grads, 2 * half + t, d), b = columns_of<kDim>(queries, 2 * half + t, d);
-                dv[d] = product(a, prob, dv[d]);
-                dk[d] = product(b, ds, dk[d]);
-            }
+            s = product(rows_of<kDim>(queries + stage * kBytes, at, half, step), k[step], s);
+            dp = product(rows_of<kDim>(queries + stage * kBytes, at, half + kStages * kRows / 32, step), rows_of<kDim>(values + wave * (64 * kDim), at, 0, step), dp);   // (the gradients, as far behind the queries)
         }
     };
-
-    // whether the wavefront's keys are seen by none, or each by all, of 32 rows
-    auto none_of = [&](uint32_t lo) { return lo + 32 <= wave_first || lo >= wave_last; };
-    auto all_of = [&](uint32_t lo) { return lo >= whole_first && lo + 32 <= whole_last; };
-    auto block_all_of = [&](uint32_t lo) { return lo >= block_first && lo + kTileKeys <= block_last; };
-    if (from < to) {
-        load(from);
-        keep(from, stat(from));
-    }
-    for (uint32_t tile = from; tile < to; ++tile) {
-        meet();
-        float next = 0.f;
-        if (tile + 1 < to) {
-            next = stat(tile + 1);
-            load(tile + 1);
-        }
-        uint8_t *const queries = lds + (tile & 1) * (2 * kBytes);
-        if (!block_all_of(tile * kTileKeys)) {   // (a key that is seen by a query that is not finite has a NaN by its lse)
-            clean<kDim>(queries);
-            bad |= clean<kDim>(queries + kBytes);
-            meet_in_lds();
-        }
-        const float *const lse = stats + (tile & 1) * 2 * kTileKeys;
-        const uint32_t row0 = tile * kTileKeys;
+    auto slopes = [&](uint32_t stage, int half, uint32_t first) {
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            const uint32_t lo = row0 + 32 * half;
-            if (none_of(lo)) continue;
-            work(!all_of(lo), queries, queries + kBytes, lse, lse + kTileKeys, half, row0);
+        for (int i = 0; i < 4; ++i) {
+            const f4 l = *(const f4 *)(stats + stage * kStats + 32 * half + 8 * i + 4 * g);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                s[4 * i + e] = __builtin_amdgcn_exp2f(fmaf(s[4 * i + e], c, -l[e]));
+                dp[4 * i + e] *= s[4 * i + e];
+            }
         }
-        if (tile + 1 < to) keep(tile + 1, next);
+        if (!all_of(first))
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const uint32_t i = first + e / 4 * 8 + 4 * g + e % 4;
+                const bool does = i >= seen_from && i < seen_to;
+                s[e] = does ? s[e] : 0.f;
+                dp[e] = does ? dp[e] : 0.f;
+            }
+#pragma unroll
+        for (int t = 0; t < 2; ++t) { prob[t] = eight_of(s, t); ds[t] = eight_of(dp, t); }
+    };
+    auto join = [&](uint32_t stage, int half) {
+        const uint32_t at = anew(lane_columns_at);
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int d = 0; d < kWide; ++d) {
+                dv[d] = product(columns_of<kDim>(queries + stage * kBytes, at, 2 * half + t + kStages * kRows / 16, d), prob[t], dv[d]);
+                dk[d] = product(columns_of<kDim>(queries + stage * kBytes, at, 2 * half + t, d), ds[t], dk[d]);
+            }
+    };
+
+    uint32_t now = number;   // the tile that is worked on
+    bool bad = false;
+    if (from < to) {
+        Loader<kDim, kTile, kThreads>(p.v + (uint64_t)at.k0 * p.ld_v + at.head * p.dim, p.ld_v, at.lk, p.dim).load_any(values, at.tile);
+        load(0);
     }
-    if (__syncthreads_or(bad))
-        for (uint32_t row = from * kTileKeys; row < min(to * kTileKeys, rows); ++row) {
-            if (none_of(row / 32 * 32) || block_all_of(row / kTileKeys * kTileKeys)) continue;
-            const uint32_t t = quotient(row, p.group);
-            const Seen by = seen_by(p, at, t);
-            spoil<kDim>(dv, p.grad + (uint64_t)(at.q0 + t) * p.ld_grad + (at.head * p.group.by + row - t * p.group.by) * p.dim, p.dim, (int)key >= by.lo && (int)key < by.hi);
+    for (uint32_t it = from, stage = 0; it < to; ++it, stage ^= 1) {
+        const uint32_t first = now * kRows;
+        arrived();
+        keep(stage);
+        if (!block_all_of(first)) {   // (a key that is seen by a query that is not finite has a NaN by its lse)
+            clean<kBytes, kThreads>(lds + stage * kBytes);
+            bad |= clean<kBytes, kThreads>(lds + (kStages + stage) * kBytes);
         }
-    if (key >= at.lk) return;
-    const uint64_t line = at.k0 + key;
+        meet();
+        if (it + 1 < to) load(stage ^ 1);
+        scores(stage, 0);
+        slopes(stage, 0, first);
+        if constexpr (kHalves > 1) {
+            join(stage, 0);
+            scores(stage, 1);
+            pace<4 * kWide, 1, 2, 3>();
+            pace<2 * kSteps, 2, 3, 2>();
+            slopes(stage, 1, first + 32);
+        }
+        join(stage, kHalves - 1);
+        if (++now == tile1) now = tile0;
+    }
+
+    if (__syncthreads_or(bad))
+        for (uint32_t it = from; it < to; ++it)
+            for (uint32_t i = (tile0 + it % tiles) * kRows; i < min((tile0 + it % tiles + 1) * kRows, at.lq); ++i) {
+                if (block_all_of(i / kRows * kRows)) continue;
+                spoil<kDim>(dv, grad + (uint64_t)i * p.ld_grad + it / tiles * p.dim, p.dim, i >= seen_from && i < seen_to);
+            }
     if (p.parts == 1) {
-        store_row<kDim>(p.dk + line * p.ld_dk + at.head * p.dim, dk, p.scale, p.dim);
-        store_row<kDim>(p.dv + line * p.ld_dv + at.head * p.dim, dv, 1.f, p.dim);
-    } else {
+        auto place = [&](uint16_t *base, uint64_t ld, uint32_t i) { return wave_key + i < at.lk ? base + (uint64_t)(at.k0 + wave_key + i) * ld + at.head * p.dim : nullptr; };
+        store_rows<kDim>(lds + wave * 64 * kDim, dk, p.scale, p.dim, [&](uint32_t i) { return place(p.dk, p.ld_dk, i); });
+        store_rows<kDim>(lds + wave * 64 * kDim, dv, 1.f, p.dim, [&](uint32_t i) { return place(p.dv, p.ld_dv, i); });
+    } else if (key < at.lk) {
+        const uint64_t line = at.k0 + key;
         const uint64_t wide = (uint64_t)p.kv_heads * p.dim, half = (uint64_t)p.parts * p.kv_rows * wide;
         float *const to = p.scratch + (blockIdx.y * (uint64_t)p.kv_rows + line) * wide + at.head * p.dim;
         store_row<kDim>(to, dk, p.scale, p.dim);
@@ -699,19 +798,34 @@ __global__ __launch_bounds__(kThreads, kDim > 64 ? 1 : 2) void k_attention_dkv(A
     }
 }
 
-// The sum of `parts` arrays [rows][cols], in their order, where rows belong to sequences.
-__global__ __launch_bounds__(kThreads) void k_attention_add(const float *part, uint32_t parts, uint32_t rows, uint32_t cols, const uint32_t *starts, uint32_t sequences, uint16_t *out,
-                                                            uint64_t ld) {
-    const uint64_t id = (uint64_t)blockIdx.x * kThreads + threadIdx.x;
-    const uint32_t chunks = cols / 8, row = (uint32_t)min(id / chunks, (uint64_t)rows), col = (uint32_t)(id % chunks) * 8;
-    if (!belongs(row, starts, sequences, rows)) return;
+// Sums of `parts` arrays [rows][cols], in their order, where rows belong to sequences: out, and (blockIdx.y) another, whose arrays lie behind the first's
+struct AddArgs {
+    const float *part;
+    uint32_t parts, rows, cols, sequences;
+    const uint32_t *starts;
+    uint16_t *out[2];
+    uint64_t ld[2];
+};
+__global__ __launch_bounds__(kBlock) void k_attention_add(AddArgs p) {
+    const uint32_t id = blockIdx.x * kBlock + threadIdx.x, chunks = p.cols / 8, row = id / chunks, col = (id - row * chunks) * 8;   // (below 2^24 / 8, by the room that parts have)
+    if (!belongs(row, p.starts, p.sequences, p.rows)) return;
+    const uint64_t all = (uint64_t)p.rows * p.cols;
+    const float *const from = p.part + blockIdx.y * (all * p.parts) + (uint64_t)row * p.cols + col;
     float s[8] = {};
-    for (uint32_t i = 0; i < parts; ++i) {
-        const f4 *at = (const f4 *)(part + ((uint64_t)i * rows + row) * cols + col);
+    for (uint32_t i0 = 0; i0 < p.parts; i0 += 8) {
+        f4 part[8][2];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) s[e] += at[e / 4][e % 4];
+        for (int i = 0; i < 8; ++i) {
+            part[i][0] = *(const f4 *)(from + min(i0 + i, p.parts - 1) * all);
+            part[i][1] = *(const f4 *)(from + min(i0 + i, p.parts - 1) * all + 4);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i0 + i < p.parts)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) s[e] += part[i][e / 4][e % 4];
     }
-    store_chunk((Bf16 *)out + (uint64_t)row * ld + col, 8, s);
+    store_chunk((Bf16 *)p.out[blockIdx.y] + (uint64_t)row * p.ld[blockIdx.y] + col, 8, s);
 }
 
 AttentionArgs args_of(const lgc_attention_shape &shape) {
@@ -720,26 +834,39 @@ AttentionArgs args_of(const lgc_attention_shape &shape) {
     p.q_rows = (uint32_t)shape.q_rows; p.kv_rows = (uint32_t)shape.kv_rows; p.sequences = (uint32_t)shape.sequences;
     p.heads = shape.heads; p.kv_heads = shape.kv_heads; p.dim = shape.dim;
     p.lq = (uint32_t)(shape.q_rows / shape.sequences); p.lk = (uint32_t)(shape.kv_rows / shape.sequences);
-    p.causal = shape.causal != 0; p.window = shape.window;
+    p.causal = shape.causal != 0; p.window = (int)std::min(shape.window, 1u << 29);
     p.scale = shape.scale;
     p.group = divide_by(shape.heads / shape.kv_heads);
     return p;
 }
 
-// Tiles of a key head, of `tile` rows (group of them per token) of `tokens`
+// Tiles of `tile` rows (group of them per token) of `tokens`
 void set_tiles(AttentionArgs &p, uint64_t tokens, uint64_t group, uint64_t tile) {
-    const uint64_t each = std::max<uint64_t>(1, (tokens / p.sequences * group + tile - 1) / tile);
-    p.per_sequence = divide_by((uint32_t)each);
-    p.tiles = divide_by((uint32_t)(p.q_starts ? tokens * group / tile + p.sequences : each * p.sequences));
+    p.tiles = (uint32_t)(p.q_starts ? tokens * group / tile + p.sequences : std::max<uint64_t>(1, (tokens / p.sequences * group + tile - 1) / tile));
+    p.pairs = divide_by(p.q_starts ? p.kv_heads : p.kv_heads * p.sequences);
 }
 
-uint64_t grid_of(const AttentionArgs &p) { return (uint64_t)p.tiles.by * p.kv_heads; }
+uint64_t grid_of(const AttentionArgs &p) { return (uint64_t)p.tiles * p.pairs.by; }
 
-// In how many parts to make a block's sum over `tiles` tiles, where blocks are few: two blocks per compute unit, each with four tiles or more, and room for the parts' results
-uint32_t parts_for(uint64_t blocks, uint64_t tiles, uint64_t results, uint64_t room, int cus) {
-    const uint64_t want = std::min(2 * (uint64_t)cus / blocks, tiles / 4);
-    const uint64_t parts = std::min(want, room / std::max<uint64_t>(1, results));
-    return parts > 1 ? (uint32_t)std::min<uint64_t>(parts, 65535) : 1;
+// In how many parts to make blocks' sums, of which the longest has `most` tiles and the average `mean`: where blocks are few, the time is that of the longest (us: some 2 a tile), and what parts
+// save of it they cost by their results, written and read once, and by the launch that adds them.
+uint32_t parts_for(uint64_t blocks, double most, double mean, double tile, uint64_t results, uint64_t room, int cus) {
+    uint32_t best = 1;
+    double least = 0;
+    for (uint32_t n = 1; n <= 64 && (n == 1 || (n <= most / 2 && n * results <= room)); ++n) {
+        const double time = tile * std::max(most / n, mean * (double)blocks / (2 * cus)) + (n > 1 ? 5 + 2e-6 * (double)(n * results) : 0.);
+        if (n == 1 || time < 0.95 * least) { best = n; least = time; }
+    }
+    return best;
+}
+
+// The most and the mean number of tokens that one of `of` tokens sees of `others` (or is seen by), with `width` neighbours who share a block; lengths of sequences that differ are not known here:
+// twice the average for the longest
+struct Extent { double most, mean; };
+Extent extent(const AttentionArgs &p, uint64_t of, uint64_t others, uint64_t width) {
+    const double a = (double)of / p.sequences, b = (double)others / p.sequences, longest = p.q_starts ? std::min(2 * b, (double)others) : b;
+    const double near = p.window ? (double)p.window + (double)width : 1e30;
+    return Extent{std::min(longest, near), std::min(p.causal ? std::max(b - a / 2, b / 2) : b, near)};
 }
 
 template <typename F>
@@ -747,18 +874,6 @@ void with_dim(uint32_t dim, F &&f) {
     if (dim <= 64) f(std::integral_constant<int, 64>());
     else f(std::integral_constant<int, 128>());
 }
-typedef std::integral_constant<int, 1> One;
-typedef std::integral_constant<int, 2> Two;
-
-// Two groups of 32 rows per wavefront where that leaves enough blocks
-template <typename F>
-void with_groups(AttentionArgs &p, int cus, F &&f) {
-    set_tiles(p, p.q_rows, p.group.by, 256);
-    if (grid_of(p) >= (uint64_t)cus) return f(Two());
-    set_tiles(p, p.q_rows, p.group.by, 128);
-    f(One());
-}
-
 }  // namespace
 
 void launch_attention(const lgc_attention_shape &shape, const void *q, uint64_t ld_q, const void *k, uint64_t ld_k, const void *v, uint64_t ld_v, void *o, uint64_t ld_o, float *lse,
@@ -767,12 +882,13 @@ void launch_attention(const lgc_attention_shape &shape, const void *q, uint64_t 
     p.q = (const uint16_t *)q; p.k = (const uint16_t *)k; p.v = (const uint16_t *)v; p.out = (uint16_t *)o;
     p.ld_q = ld_q; p.ld_k = ld_k; p.ld_v = ld_v; p.ld_out = ld_o;
     p.lse = lse; p.scratch = scratch;
-    with_groups(p, cus, [&](auto groups) {
-        const uint64_t rows = (uint64_t)p.q_rows * p.heads;
-        p.parts = parts_for(grid_of(p), p.kv_rows / p.sequences / kTileKeys, rows * (p.dim + 1), scratch_floats, cus);
-        with_dim(p.dim, [&](auto dim) { k_attention<decltype(dim)::value, decltype(groups)::value><<<dim3((uint32_t)grid_of(p), p.parts), kThreads, 0, st>>>(p); });
-        if (p.parts > 1) k_attention_join<<<(uint32_t)((rows + kThreads / 16 - 1) / (kThreads / 16)), kThreads, 0, st>>>(p);
-    });
+    constexpr int kWaves = 4;
+    set_tiles(p, p.q_rows, p.group.by, 32 * kWaves);
+    const uint64_t rows = (uint64_t)p.q_rows * p.heads;
+    const Extent keys = extent(p, p.q_rows, p.kv_rows, 32 * kWaves / p.group.by);
+    p.parts = parts_for(grid_of(p), keys.most / kTileKeys, keys.mean / kTileKeys, p.dim > 64 ? 2 : 1.5, rows * (p.dim + 1), scratch_floats, cus);
+    with_dim(p.dim, [&](auto dim) { k_attention<decltype(dim)::value, kWaves><<<dim3((uint32_t)grid_of(p), p.parts), 64 * kWaves, 0, st>>>(p); });
+    if (p.parts > 1) k_attention_join<<<(uint32_t)((rows + kBlock / 16 - 1) / (kBlock / 16)), kBlock, 0, st>>>(p);
 }
 
 void launch_attention_grad(const lgc_attention_shape &shape, const void *grad, uint64_t ld_grad, const void *q, uint64_t ld_q, const void *k, uint64_t ld_k, const void *v, uint64_t ld_v,
@@ -784,24 +900,39 @@ void launch_attention_grad(const lgc_attention_shape &shape, const void *grad, u
     p.out = (uint16_t *)dq; p.dk = (uint16_t *)dk; p.dv = (uint16_t *)dv;
     p.ld_out = ld_dq; p.ld_dk = ld_dk; p.ld_dv = ld_dv;
     p.lse = const_cast<float *>(lse); p.delta = delta; p.scratch = scratch;
-    auto add = [&](const float *part, uint32_t rows, uint32_t cols, const uint32_t *starts, uint16_t *out, uint64_t ld) {
-        k_attention_add<<<(uint32_t)(((uint64_t)rows * (cols / 8) + kThreads - 1) / kThreads), kThreads, 0, st>>>(part, p.parts, rows, cols, starts, p.sequences, out, ld);
+    auto add = [&](uint32_t rows, uint32_t cols, const uint32_t *starts, uint16_t *one, uint64_t ld_one, uint16_t *two, uint64_t ld_two) {
+        if (p.parts == 1) return;
+        const AddArgs sums{scratch, p.parts, rows, cols, p.sequences, starts, {one, two}, {ld_one, ld_two}};
+        k_attention_add<<<dim3((uint32_t)(((uint64_t)rows * (cols / 8) + kBlock - 1) / kBlock), two ? 2 : 1), kBlock, 0, st>>>(sums);
     };
-    if (p.q_rows)
-        with_groups(p, cus, [&](auto groups) {
-            p.parts = parts_for(grid_of(p), p.kv_rows / p.sequences / kTileKeys, (uint64_t)p.q_rows * p.heads * p.dim, scratch_floats, cus);
-            with_dim(p.dim, [&](auto dim) { k_attention_dq<decltype(dim)::value, decltype(groups)::value><<<dim3((uint32_t)grid_of(p), p.parts), kThreads, 0, st>>>(p); });
-            if (p.parts > 1) add(scratch, p.q_rows, p.heads * p.dim, p.q_starts, p.out, ld_dq);
-        });
+    const uint64_t group = p.group.by;
+    if (p.q_rows) {
+        constexpr int kWaves = 4;
+        set_tiles(p, p.q_rows, group, 32 * kWaves);
+        const Extent keys = extent(p, p.q_rows, p.kv_rows, 32 * kWaves / group);
+        p.parts = parts_for(grid_of(p), keys.most / kTileKeys, keys.mean / kTileKeys, p.dim > 64 ? 3 : 2, (uint64_t)p.q_rows * p.heads * p.dim, scratch_floats, cus);
+        with_dim(p.dim, [&](auto dim) { k_attention_dq<decltype(dim)::value, kWaves><<<dim3((uint32_t)grid_of(p), p.parts), 64 * kWaves, 0, st>>>(p); });
+        add(p.q_rows, p.heads * p.dim, p.q_starts, p.out, ld_dq, nullptr, 0);
+    }
     if (!p.kv_rows) return;
     const uint32_t cols = p.kv_heads * p.dim;
-    set_tiles(p, p.kv_rows, 1, 128);
-    p.parts = parts_for(grid_of(p), (uint64_t)p.q_rows * p.group.by / p.sequences / kTileKeys, 2 * (uint64_t)p.kv_rows * cols, scratch_floats, cus);
-    with_dim(p.dim, [&](auto dim) { k_attention_dkv<decltype(dim)::value><<<dim3((uint32_t)grid_of(p), p.parts), kThreads, 0, st>>>(p); });
-    if (p.parts > 1) {
-        add(scratch, p.kv_rows, cols, p.kv_starts, p.dk, ld_dk);
-        add(scratch + (uint64_t)p.parts * p.kv_rows * cols, p.kv_rows, cols, p.kv_starts, p.dv, ld_dv);
+    auto dkv = [&](auto dim, auto waves) {
+        constexpr int kDim = decltype(dim)::value, kWaves = decltype(waves)::value;
+        const Extent queries = extent(p, p.kv_rows, p.q_rows, 32 * kWaves);
+        p.parts = parts_for(grid_of(p), queries.most * group / 32, queries.mean * group / 32, kDim > 64 ? 2 : 1, 2 * (uint64_t)p.kv_rows * cols, scratch_floats, cus);
+        k_attention_dkv<kDim, kWaves><<<dim3((uint32_t)grid_of(p), p.parts), 64 * kWaves, 0, st>>>(p);
+    };
+    typedef std::integral_constant<int, 4> Four;
+    typedef std::integral_constant<int, 8> Eight;
+    // Heads of 128: eight wavefronts per block, whose 256 keys read q and do half as often, where that leaves a block per compute unit (us, four / eight: 4 x 4096 tokens of 32 / 8 heads
+    // 1290 / 1180); heads of 64: three blocks of four fit a compute unit, but one of eight (16384 tokens of 8 heads 599 / 601)
+    set_tiles(p, p.kv_rows, 1, 256);
+    if (p.dim > 64 && grid_of(p) >= (uint64_t)cus) dkv(std::integral_constant<int, 128>(), Eight());
+    else {
+        set_tiles(p, p.kv_rows, 1, 128);
+        with_dim(p.dim, [&](auto dim) { dkv(dim, Four()); });
     }
+    add(p.kv_rows, cols, p.kv_starts, p.dk, ld_dk, p.dv, ld_dv);
 }
 
 }  // namespace lgc
