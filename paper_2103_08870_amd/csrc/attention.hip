@@ -55,9 +55,10 @@ struct Place {
 };
 
 // Which tile of which sequence and key head a block works on.  Blocks go to the compute units in their order, and to the eight XCDs in turn.  So the heads (and sequences, if they have one length)
-// come in turn too, which gives most XCDs few of them, whose keys its L2 holds; and of each the tile first that has the most to do under a causal mask, so that short ones fill the end (a
-// head's tiles one sequence after the other, XCD by XCD: 4 x 4096 tokens, 32 / 8 heads of 128: forward 604 us, backward 3148).
-// With starts, tile number starts[s] * group / kTile + s is the first of sequence s: that leaves each sequence as many as it can need, and a block finds its sequence without a table.
+// come in turn too, which gives most XCDs few of them, whose keys its L2 holds; and of each the tile first that has the most to do under a causal mask, so that short ones fill the end
+// (4 x 4096 tokens, 32 / 8 heads of 128, one sequence of a head after the other: backward 3148 us, so 2475).  The order across up to 64 sequences of different lengths is found by
+// counting: how many tiles have at least some number in their sequence.  With more of them, tile number starts[s] * group / tile_rows + s is the first of sequence s: that leaves each as many as
+// it can need, and a block finds its sequence without a table.
 __device__ __forceinline__ Place place_of(const AttentionArgs &p, bool by_keys, uint32_t tile_rows) {
     const uint32_t rank = quotient(blockIdx.x, p.pairs), pair = blockIdx.x - rank * p.pairs.by;
     const bool down = !by_keys || !p.causal;   // (of keys, the first are seen by the most queries)
@@ -71,20 +72,42 @@ __device__ __forceinline__ Place place_of(const AttentionArgs &p, bool by_keys, 
         return at;
     }
     at.head = pair;
-    const uint32_t tile = down ? p.tiles - 1 - rank : rank;
-    const uint32_t *starts = by_keys ? p.kv_starts : p.q_starts, rows = by_keys ? p.kv_rows : p.q_rows, group = by_keys ? 1 : p.group.by;
-    auto first = [&](uint32_t s) { return (uint32_t)((uint64_t)min(starts[s], rows) * group / tile_rows) + s; };
-    uint32_t lo = 0, n = p.sequences;   // sequences before lo begin at or before the tile; of the n from lo on it is open
-    while (n) {
-        const uint32_t step = (n + 63) / 64, off = (threadIdx.x & 63) * step;
-        const uint32_t count = __popcll(__ballot(off < n && first(lo + min(off, n - 1)) <= tile));
-        if (!count) break;
-        lo += (count - 1) * step + 1;
-        n = min(n - (count - 1) * step - 1, step - 1);
+    const uint32_t *starts = by_keys ? p.kv_starts : p.q_starts, rows = by_keys ? p.kv_rows : p.q_rows, group = by_keys ? 1 : p.group.by, lane = threadIdx.x & 63;
+    uint32_t s;
+    if (p.sequences <= 64) {   // a lane has a sequence
+        uint32_t tiles = 0;
+        if (lane < p.sequences) {
+            const uint32_t first = min(starts[lane], rows), end = min(starts[lane + 1], rows);
+            tiles = end > first ? (uint32_t)(((uint64_t)(end - first) * group + tile_rows - 1) / tile_rows) : 0u;
+        }
+        auto from = [&](uint32_t number) { return wave_sum(tiles > number ? tiles - number : 0u); };   // tiles of that number in their sequence, and of higher ones
+        if (from(0) <= rank) { at.none = true; return at; }
+        uint32_t lo = 0, hi = p.tiles;   // from(lo) > rank >= from(hi)
+        while (hi - lo > 1) {
+            const uint32_t mid = lo + (hi - lo) / 2;
+            if (from(mid) > rank) lo = mid;
+            else hi = mid;
+        }
+        const uint32_t among = rank - from(lo + 1);   // (made by all lanes) which of the sequences that have a tile of this number
+        const unsigned long long with = __ballot(tiles > lo), its = __ballot(tiles > lo && lanes_below(with) == among);
+        if (!its) { at.none = true; return at; }
+        s = (uint32_t)__ffsll(its) - 1;
+        at.tile = down ? lo : __builtin_amdgcn_readlane(tiles, s) - 1 - lo;
+    } else {
+        const uint32_t tile = p.tiles - 1 - rank;
+        auto first = [&](uint32_t s) { return (uint32_t)((uint64_t)min(starts[s], rows) * group / tile_rows) + s; };
+        uint32_t lo = 0, n = p.sequences;   // sequences before lo begin at or before the tile; of the n from lo on it is open
+        while (n) {
+            const uint32_t step = (n + 63) / 64, off = lane * step;
+            const uint32_t count = __popcll(__ballot(off < n && first(lo + min(off, n - 1)) <= tile));
+            if (!count) break;
+            lo += (count - 1) * step + 1;
+            n = min(n - (count - 1) * step - 1, step - 1);
+        }
+        if (!lo) { at.none = true; return at; }
+        s = __builtin_amdgcn_readfirstlane(lo - 1);
+        at.tile = tile - __builtin_amdgcn_readfirstlane(first(s));
     }
-    if (!lo) { at.none = true; return at; }
-    const uint32_t s = __builtin_amdgcn_readfirstlane(lo - 1);
-    at.tile = tile - __builtin_amdgcn_readfirstlane(first(s));
     at.q0 = min(p.q_starts[s], p.q_rows); at.lq = max(min(p.q_starts[s + 1], p.q_rows), at.q0) - at.q0;
     at.k0 = min(p.kv_starts[s], p.kv_rows); at.lk = max(min(p.kv_starts[s + 1], p.kv_rows), at.k0) - at.k0;
     return at;
