@@ -219,92 +219,98 @@ __global__ __launch_bounds__(64 * kWavesM * kWavesN) void k_product(ProductArgs 
     }
     meet();   // nothing may arrive any more where the rows go
 
-    // With an epilogue, 32 rows of 64 columns at a time go through LDS in fp32, each wavefront's for itself, and a lane takes eight columns of a row on from there.  The exponents of 8-bit
-    // results are found before, from the sums in registers: two wavefronts have the 128 columns that share one.
+    // With an epilogue, 32 rows of 64 columns at a time go through LDS in fp32, each wavefront's for itself, and a lane takes eight columns of a row on from there, whose residual is on its
+    // way by then.  Exponents of 8-bit results are found before, from the registers: two wavefronts have the 128 columns that share one.  8192 x 16384 x 4096 with GELU to bf16 576 us, of which the
+    // non-linearity takes 68 (16 vector instructions an element, with nothing to multiply meanwhile: the compute unit holds one block; two of small tiles 603).
     if constexpr (std::is_same_v<E, Epilogue>) {
-        static_assert(kSideN == 2 && sizeof(f4) * kAll * 32 * 17 + 2 * kAll * kWaveM * 4 <= 2 * kPlace, "room");
+        static_assert(kSideN == 2 && sizeof(f4) * kAll * 32 * 17 + kAll * kWaveM * 4 <= 2 * kPlace, "room");
         float *const out = (float *)places + wave * 32 * 68;
-        uint32_t *const most = (uint32_t *)(places + kAll * 32 * 68 * 4);   // [of t, of z][wavefront][row]
-        f4 bias[2][4];
+        uint32_t *const most = (uint32_t *)(places + kAll * 32 * 68 * 4);   // [wavefront][row]
+        const bool all_cols = n0 + wn + 64 <= p.n;
 #pragma unroll
         for (int j = 0; j < 2; ++j)
 #pragma unroll
-            for (int c = 0; c < 4; ++c) bias[j][c] = *(const f4 *)((const float *)biases + wn + 32 * j + 8 * c + 4 * g);
-        const bool all_cols = n0 + wn + 64 <= p.n;
-        auto sums = [&](int i, int j, int c, float (&t)[4]) {   // columns that do not exist are zeros
-            const f4 q = bias[j][c] + f4{acc[i][j][4 * c], acc[i][j][4 * c + 1], acc[i][j][4 * c + 2], acc[i][j][4 * c + 3]};
+            for (int c = 0; c < 4; ++c) {
+                const f4 bias = *(const f4 *)((const float *)biases + wn + 32 * j + 8 * c + 4 * g);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) t[e] = all_cols || n0 + wn + 32 * j + 8 * c + 4 * g + e < p.n ? q[e] : 0.f;
-        };
-        if (ep.t_codes || ep.z_codes) {
+                for (int i = 0; i < kSideM; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {   // columns that do not exist are zeros
+                        const float t = acc[i][j][4 * c + e] + bias[e];
+                        acc[i][j][4 * c + e] = all_cols || n0 + wn + 32 * j + 8 * c + 4 * g + e < p.n ? t : 0.f;
+                    }
+            }
+        auto find_most = [&] {
+            __syncthreads();   // (those of the results before are read)
 #pragma unroll
             for (int i = 0; i < kSideM; ++i) {
-                uint32_t most_t = 0, most_z = 0;
-                auto larger = [](uint32_t m, float x) { const uint32_t k = key_of(x); return k < kInfKey && k > m ? k : m; };
+                uint32_t m = 0;
 #pragma unroll
-                for (int j = 0; j < 2; ++j)
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        float t[4];
-                        sums(i, j, c, t);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) most_t = larger(most_t, t[e]);
-                        if (ep.z_codes) {
-                            activate(ep.act, t);
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) most_z = larger(most_z, t[e]);
-                        }
-                    }
-                most_t = max(most_t, (uint32_t)__shfl_xor((int)most_t, 32));
-                most_z = max(most_z, (uint32_t)__shfl_xor((int)most_z, 32));
-                if (g == 0) {
-                    most[wave * kWaveM + 32 * i + r] = most_t;
-                    most[(kAll + wave) * kWaveM + 32 * i + r] = most_z;
+                for (int e = 0; e < 32; ++e) {
+                    const uint32_t k = key_of(acc[i][e / 16][e % 16]);
+                    m = k < kInfKey && k > m ? k : m;
                 }
+                m = max(m, (uint32_t)__shfl_xor((int)m, 32));
+                if (g == 0) most[wave * kWaveM + 32 * i + r] = m;
             }
-        }
-        __syncthreads();
+            __syncthreads();
+        };
         const uint32_t row = lane / 8, col = lane % 8 * 8, other = (wave / kWavesM ^ 1) * kWavesM + wave % kWavesM;   // other: the wavefront beside, in the same 128 columns
         const uint32_t n = n0 + wn + col, codes_to = (uint32_t)block_count(p.n) * kBlockCols, code_exps = (uint32_t)exps_stride(p.n);
         const int count = count_at(n, p.n);
+        auto lines = [&](uint8_t *codes, uint8_t *exps, bool plain) {
 #pragma unroll
-        for (int i = 0; i < kSideM; ++i) {
+            for (int i = 0; i < kSideM; ++i) {
+                Chunk<T> residual[4];
+                if (plain && ep.residual && count)
 #pragma unroll
-            for (int j = 0; j < 2; ++j)
+                    for (int s = 0; s < 4; ++s) residual[s] = fetch_chunk((const T *)ep.residual + (uint64_t)min(m0 + wm + 32 * i + 8 * s + row, p.m - 1) * ep.ld_residual, n, p.n);
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    float t[4];
-                    sums(i, j, c, t);
-                    *(f4 *)(out + r * 68 + 32 * j + 8 * c + 4 * g) = f4{t[0], t[1], t[2], t[3]};
+                for (int j = 0; j < 2; ++j)
+#pragma unroll
+                    for (int c = 0; c < 4; ++c)
+                        *(f4 *)(out + r * 68 + 32 * j + 8 * c + 4 * g) = f4{acc[i][j][4 * c], acc[i][j][4 * c + 1], acc[i][j][4 * c + 2], acc[i][j][4 * c + 3]};
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+                for (int s = 0; s < 4; ++s) {
+                    const uint32_t of_wave = 32 * i + 8 * s + row, m = m0 + wm + of_wave;
+                    const f4 lo = *(const f4 *)(out + (8 * s + row) * 68 + col), hi = *(const f4 *)(out + (8 * s + row) * 68 + col + 4);
+                    float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+                    if (codes && m < p.m && n < codes_to) {
+                        const uint32_t e = block_exp(max(most[wave * kWaveM + of_wave], most[other * kWaveM + of_wave]));
+                        *(u2 *)(codes + (uint64_t)m * codes_to + n) = codes_of(v, e);
+                        if (col == 0 && wave / kWavesM % 2 == 0) exps[(uint64_t)m * code_exps + n / kBlockCols] = (uint8_t)e;
+                    }
+                    if (plain && m < p.m && count) {
+                        if (ep.residual) {
+                            float x[8];
+                            unpack(residual[s], n, p.n, x);
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) v[e] += x[e];
+                        }
+                        store_chunk((T *)p.y + (uint64_t)m * p.ld + n, count, v);
+                    }
                 }
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-#pragma clang loop unroll(disable)
-            for (int s = 0; s < 4; ++s) {
-                const uint32_t of_wave = 32 * i + 8 * s + row, m = m0 + wm + of_wave;
-                float v[8];
-                const f4 lo = *(const f4 *)(out + (8 * s + row) * 68 + col), hi = *(const f4 *)(out + (8 * s + row) * 68 + col + 4);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) { v[e] = lo[e]; v[4 + e] = hi[e]; }
-                auto store_codes = [&](uint8_t *codes, uint8_t *exps, const uint32_t *most) {
-                    const uint32_t e = block_exp(max(most[wave * kWaveM + of_wave], most[other * kWaveM + of_wave]));
-                    if (m >= p.m || n >= codes_to) return;
-                    *(u2 *)(codes + (uint64_t)m * codes_to + n) = codes_of(v, e);
-                    if (col == 0 && wave / kWavesM % 2 == 0) exps[(uint64_t)m * code_exps + n / kBlockCols] = (uint8_t)e;
-                };
-                if (ep.t_codes) store_codes(ep.t_codes, ep.t_exps, most);
-                activate(ep.act, v);
-                if (ep.z_codes) store_codes(ep.z_codes, ep.z_exps, most + kAll * kWaveM);
-                if (!p.y || m >= p.m || !count) continue;
-                if (ep.residual) {
-                    float x[8];
-                    load_chunk((const T *)ep.residual + (uint64_t)m * ep.ld_residual, n, p.n, x);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) v[e] += x[e];
-                }
-                store_chunk((T *)p.y + (uint64_t)m * p.ld + n, count, v);
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             }
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        };
+        if (ep.t_codes) {
+            find_most();
+            lines(ep.t_codes, ep.t_exps, false);
         }
+#pragma unroll
+        for (int i = 0; i < kSideM; ++i)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                float z[16];
+#pragma unroll
+                for (int e = 0; e < 16; ++e) z[e] = acc[i][j][e];
+                activate(ep.act, z);   // (f(0) = 0: columns that do not exist stay zeros)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) acc[i][j][e] = z[e];
+            }
+        if (ep.z_codes) find_most();
+        if (ep.z_codes || p.y) lines(ep.z_codes, ep.z_exps, p.y);
         return;
     }
 
@@ -385,6 +391,19 @@ __global__ __launch_bounds__(64 * kFew) void k_product_few(ProductArgs p, E ep) 
     for (int j = 0; j < kN; ++j) b[j] = p.b + min(n0 + 16 * j + r, p.n - 1) * stride + g * 32;
     typedef const __attribute__((address_space(4))) uint32_t *Scalar;
     const Scalar b_exps = (Scalar)(p.b_exps + (uint64_t)(n0 / kBlockCols) * p.exp_stride);
+    // (with an epilogue, whose results the first threads take one each: their bias and residual, on their way before the sums are made)
+    constexpr bool kEarly = std::is_same_v<E, Epilogue> && kM * kN <= kFew;
+    float bias[4] = {}, residual[4] = {};
+    if constexpr (kEarly) {
+        const uint32_t tile = threadIdx.x / 64, m = tile / kN * 16 + r, n = n0 + tile % kN * 16 + 4 * g;
+        if (tile < kM * kN && m < p.m)
+#pragma unroll
+            for (int d = 0; d < 4; ++d)
+                if (n + d < p.n) {
+                    if (p.bias) bias[d] = p.bias[n + d];
+                    if (ep.residual) residual[d] = to_float(((const T *)ep.residual)[(uint64_t)m * ep.ld_residual + n + d]);
+                }
+    }
     f4 acc[kM][kN] = {};
     const uint32_t end = min((blockIdx.y + 1) * p.share, p.blocks);   // (a part's share: whole groups of four)
     for (uint32_t four = blockIdx.y * p.share / 4 + wave; four * 4 < end; four += kFew) {
@@ -436,12 +455,12 @@ __global__ __launch_bounds__(64 * kFew) void k_product_few(ProductArgs p, E ep) 
             float v[4];
             const T *const from = (const T *)ep.residual + (uint64_t)m * ep.ld_residual + n;
 #pragma unroll
-            for (int d = 0; d < 4; ++d) v[d] = s[d] + (p.bias && n + d < p.n ? p.bias[n + d] : 0.f);
+            for (int d = 0; d < 4; ++d) v[d] = s[d] + (kEarly ? bias[d] : p.bias && n + d < p.n ? p.bias[n + d] : 0.f);
             activate(ep.act, v);
             T *const to = (T *)p.y + (uint64_t)m * p.ld + n;
 #pragma unroll
             for (int d = 0; d < 4; ++d)
-                if (n + d < p.n) store_one(to + d, v[d] + (ep.residual ? to_float(from[d]) : 0.f));
+                if (n + d < p.n) store_one(to + d, v[d] + (kEarly ? residual[d] : ep.residual ? to_float(from[d]) : 0.f));
             continue;
         }
         T *at = (T *)p.y + ((gridDim.y > 1 ? (uint64_t)blockIdx.y * p.m : 0) + m) * p.ld + n;
