@@ -1680,6 +1680,7 @@ void check_attention(Check &c, const lgc_attention_shape *s) {
     c.need(s->scale > 0.f && s->scale < INFINITY, "scale = %g", (double)s->scale);
     c.need(!s->q_starts == !s->kv_starts, "one of q_starts and kv_starts is NULL");
     c.need(aligned(s->q_starts, 4) && aligned(s->kv_starts, 4), "starts are not 4-byte aligned");
+    if (c.status != LGC_OK) return;   // (sequences are not none)
     c.need(s->q_starts || (q_rows % sequences == 0 && kv_rows % sequences == 0), "%llu and %llu rows are not %llu equal sequences", q_rows, kv_rows, sequences);
 }
 void check_heads(Check &c, const char *name, const void *p, uint64_t rows, uint64_t cols, uint64_t ld) {
@@ -1700,6 +1701,7 @@ extern "C" lgc_status lgc_attention(lgc_ctx *ctx, const lgc_attention_shape *sha
     check_heads(c, "k", k, shape->kv_rows, narrow, ld_k);
     check_heads(c, "v", v, shape->kv_rows, narrow, ld_v);
     check_heads(c, "o", o, shape->q_rows, wide, ld_o);
+    c.need(!shape->q_rows || (o != q && o != k && o != v), "o lies where an argument does: the arrays of a call must not overlap");
     c.maybe("lse", lse).reserved("lgc_attention");
     return launch(c, [&] {
         if (shape->q_rows) launch_attention(*shape, q, ld_q, k, ld_k, v, ld_v, o, ld_o, lse, ctx->training, kTrainingFloats, ctx->cus, (hipStream_t)stream);
@@ -1721,7 +1723,10 @@ extern "C" lgc_status lgc_attention_grad(lgc_ctx *ctx, const lgc_attention_shape
     check_heads(c, "dq", dq, shape->q_rows, wide, ld_dq);
     check_heads(c, "dk", dk, shape->kv_rows, narrow, ld_dk);
     check_heads(c, "dv", dv, shape->kv_rows, narrow, ld_dv);
-    if (shape->q_rows) c.vector("lse", lse).vector("delta", delta);
+    const void *const inputs[] = {grad, q, k, v, o};
+    for (const void *p : inputs) c.need(!p || (p != dq && p != dk && p != dv), "a gradient lies where an argument does: the arrays of a call must not overlap");
+    c.need((!dq || (dq != dk && dq != dv)) && (!dk || dk != dv), "two of the gradients lie in one place");
+    if (shape->q_rows) c.vector("lse", lse).vector("delta", delta).need(lse != delta, "delta lies where lse does");
     c.reserved("lgc_attention_grad");
     return launch(c, [&] {
         launch_attention_grad(*shape, grad, ld_grad, q, ld_q, k, ld_k, v, ld_v, o, ld_o, lse, dq, ld_dq, dk, ld_dk, dv, ld_dv, delta, ctx->training, kTrainingFloats, ctx->cus,
