@@ -7,6 +7,7 @@ import math
 import torch
 
 U, H = 2.0 ** -24, 2.0 ** -8      # half a unit in the last place of fp32 and of bf16
+LEAST = 2.0 ** -126
 
 
 def lengths_of(starts, rows, sequences):
@@ -43,7 +44,7 @@ def _zeroed(x, seen):
 
 def attention(q, k, v, heads, kv_heads, dim, scale, sequences=1, q_starts=None, kv_starts=None, causal=True, window=0):
     """o, lse and their bounds; rows that belong to no sequence: NaN."""
-    q, k, v = (x.double().view(x.shape[0], -1, dim) for x in (q, k, v))
+    q, k, v = (x.double().view(x.shape[0], x.shape[1] // dim, dim) for x in (q, k, v))
     o, lse = torch.full_like(q, math.nan), torch.full(q.shape[:2], math.nan, dtype=torch.float64, device=q.device)
     off_o, off_lse = torch.zeros_like(o), torch.zeros_like(lse)
     for rq, rk, h, g, seen in _pairs(heads, kv_heads, dim, sequences, q, k, q_starts, kv_starts, causal, window):
@@ -63,7 +64,7 @@ def attention(q, k, v, heads, kv_heads, dim, scale, sequences=1, q_starts=None, 
 
 def attention_grad(do, q, k, v, o, lse, heads, kv_heads, dim, scale, sequences=1, q_starts=None, kv_starts=None, causal=True, window=0):
     """(dq, dk, dv), and their bounds, with the o and lse that are given; rows that belong to no sequence: NaN."""
-    do, q, k, v, o = (x.double().view(x.shape[0], -1, dim) for x in (do, q, k, v, o))
+    do, q, k, v, o = (x.double().view(x.shape[0], x.shape[1] // dim, dim) for x in (do, q, k, v, o))
     lse = lse.double()
     dq, dk, dv = (torch.full_like(x, math.nan) for x in (q, k, v))
     off = [torch.zeros_like(x) for x in (q, k, v)]
@@ -84,8 +85,9 @@ def attention_grad(do, q, k, v, o, lse, heads, kv_heads, dim, scale, sequences=1
         dv[rk, g] += p.t() @ y
         size = scale * a.abs() @ b.abs().t()
         wrong = (dim + 8) * U * (size + l.abs()) + 4 * U
-        wrong_p = p * (H + 2 * wrong)
-        wrong_ds = ds.abs() * (H + 2 * wrong) + p * (dim + 4) * U * (y.abs() @ c.abs().t() + (y.abs() * out.abs()).sum(1, keepdim=True))
+        # (what is below the least normal number, 2^-126 in fp32 as in bf16, may count as nothing: a probability, and its ds)
+        wrong_p = torch.where(seen, p * (H + 2 * wrong) + LEAST, 0.0)
+        wrong_ds = ds.abs() * (H + 2 * wrong) + torch.where(seen, LEAST * ((dp - delta).abs() + 1), 0.0) + p * (dim + 4) * U * (y.abs() @ c.abs().t() + (y.abs() * out.abs()).sum(1, keepdim=True))
         n, m = (lk_terms(s.shape[1]), lk_terms(s.shape[0] * heads // kv_heads))
         off[0][rq, h] = scale * (wrong_ds + n * ds.abs()) @ b.abs() + H * dq[rq, h].abs()
         off[1][rk, g] += scale * (wrong_ds + m * ds.abs()).t() @ a.abs()
