@@ -506,6 +506,8 @@ lgc_status lgc_rotate(lgc_ctx *ctx, const void *x, lgc_type type, uint64_t rows,
  * neither read nor written.  A start past the last row counts as the last row's end.
  * With both NULL all sequences have q_rows / sequences and kv_rows / sequences tokens,
  * without a remainder.
+ * kv_lengths (device array of sequences numbers, NULL: none; lgc_attention only): of a sequence's rows of k and v, only the first
+ * kv_lengths[s] are its keys, as in a cache with room for more; a length past the room counts as the room.  What the others hold is not looked at.
  * Query i of a sequence of lq queries and lk keys is at position i + lk - lq.  It sees
  * all lk keys; if causal != 0, only those at positions up to its own; if window != 0, of
  * these only those at positions above its own less window.  What it does not see has no
@@ -525,6 +527,7 @@ typedef struct {
     float scale;
     int32_t causal;
     uint32_t window;
+    const uint32_t *kv_lengths; /* device, or NULL */
 } lgc_attention_shape;
 
 /*

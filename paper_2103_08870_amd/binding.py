@@ -51,7 +51,8 @@ class _Layer(C.Structure):
 
 class _AttentionShape(C.Structure):
     _fields_ = [("q_rows", C.c_uint64), ("kv_rows", C.c_uint64), ("sequences", C.c_uint64), ("q_starts", C.c_void_p), ("kv_starts", C.c_void_p),
-                ("heads", C.c_uint32), ("kv_heads", C.c_uint32), ("dim", C.c_uint32), ("scale", C.c_float), ("causal", C.c_int32), ("window", C.c_uint32)]
+                ("heads", C.c_uint32), ("kv_heads", C.c_uint32), ("dim", C.c_uint32), ("scale", C.c_float), ("causal", C.c_int32), ("window", C.c_uint32),
+                ("kv_lengths", C.c_void_p)]
 
 
 _lib = None
@@ -683,10 +684,11 @@ def lgc_rotate(ctx: Context, x: torch.Tensor, heads: int, freqs: torch.Tensor, y
 
 class AttentionShape:
     """lgc_attention_shape without its rows: heads, sequences and who sees whom.  `scale` is dim^(-1/2) where it is not given.  q_starts, kv_starts: int32 device
-    tensors of sequences + 1 row numbers, read by every call; without them all sequences are of one length."""
+    tensors of sequences + 1 row numbers, read by every call; without them all sequences are of one length.  kv_lengths: int32, how many of each sequence's rows of k and
+    v are its keys (lgc_attention alone)."""
 
     def __init__(self, heads: int, kv_heads: int, dim: int, sequences: int = 1, q_starts: Optional[torch.Tensor] = None, kv_starts: Optional[torch.Tensor] = None,
-                 scale: Optional[float] = None, causal: bool = True, window: int = 0):
+                 scale: Optional[float] = None, causal: bool = True, window: int = 0, kv_lengths: Optional[torch.Tensor] = None):
         if min(heads, kv_heads, dim, window, sequences) < 0 or max(heads, kv_heads, dim, window) >= 1 << 32:
             _refuse("heads, kv_heads, dim, sequences and window are not negative, and below 2^32")
         if (q_starts is None) != (kv_starts is None):
@@ -694,10 +696,12 @@ class AttentionShape:
         for t in (q_starts, kv_starts):
             if t is not None and (t.numel() != sequences + 1 or not t.is_contiguous()):
                 _refuse(f"starts must be contiguous with {sequences + 1} elements")
-        self._starts = q_starts, kv_starts
+        if kv_lengths is not None and (kv_lengths.numel() != sequences or not kv_lengths.is_contiguous()):
+            _refuse(f"lengths must be contiguous with {sequences} elements")
+        self._starts, self._lengths = (q_starts, kv_starts), kv_lengths
         self._heads, self._kv_heads, self._dim = heads, kv_heads, dim
         self._c = _AttentionShape(0, 0, sequences, _ptr(q_starts, torch.int32), _ptr(kv_starts, torch.int32), heads, kv_heads, dim,
-                                  scale if scale is not None else max(1, dim) ** -0.5, causal, window)
+                                  scale if scale is not None else max(1, dim) ** -0.5, causal, window, _ptr(kv_lengths, torch.int32))
         self._at = C.addressof(self._c)
 
     def _rows(self, q: torch.Tensor, k: torch.Tensor) -> int:
@@ -705,6 +709,8 @@ class AttentionShape:
         c = self._c
         if self._starts[0] is not None:   # (a tensor's memory may have been exchanged since it was looked at)
             c.q_starts, c.kv_starts = self._starts[0].data_ptr(), self._starts[1].data_ptr()
+        if self._lengths is not None:
+            c.kv_lengths = self._lengths.data_ptr()
         c.q_rows, c.kv_rows = q.shape[0], k.shape[0]
         return self._at
 

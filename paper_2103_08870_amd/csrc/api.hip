@@ -1679,7 +1679,7 @@ void check_attention(Check &c, const lgc_attention_shape *s) {
     c.need(kv_rows < (1ull << 29) && kv_rows * kv_heads < (1ull << 29), "kv_rows * kv_heads = %llu * %llu not below 2^29", kv_rows, kv_heads);
     c.need(s->scale > 0.f && s->scale < INFINITY, "scale = %g", (double)s->scale);
     c.need(!s->q_starts == !s->kv_starts, "one of q_starts and kv_starts is NULL");
-    c.need(aligned(s->q_starts, 4) && aligned(s->kv_starts, 4), "starts are not 4-byte aligned");
+    c.need(aligned(s->q_starts, 4) && aligned(s->kv_starts, 4) && aligned(s->kv_lengths, 4), "starts or lengths are not 4-byte aligned");
     if (c.status != LGC_OK) return;   // (sequences are not none)
     c.need(s->q_starts || (q_rows % sequences == 0 && kv_rows % sequences == 0), "%llu and %llu rows are not %llu equal sequences", q_rows, kv_rows, sequences);
 }
@@ -1715,6 +1715,7 @@ extern "C" lgc_status lgc_attention_grad(lgc_ctx *ctx, const lgc_attention_shape
     check_attention(c, shape);
     if (c.status != LGC_OK) return c.status;
     const uint64_t wide = (uint64_t)shape->heads * shape->dim, narrow = (uint64_t)shape->kv_heads * shape->dim;
+    c.need(!shape->kv_lengths, "kv_lengths are the forward pass's: a cache has no gradient");
     check_heads(c, "grad", grad, shape->q_rows, wide, ld_grad);
     check_heads(c, "q", q, shape->q_rows, wide, ld_q);
     check_heads(c, "k", k, shape->kv_rows, narrow, ld_k);

@@ -31,7 +31,7 @@ constexpr float kSlack = 8.f;
 struct AttentionArgs {
     const uint16_t *q, *k, *v, *o, *grad;   // grad: of o
     uint64_t ld_q, ld_k, ld_v, ld_o, ld_grad;
-    const uint32_t *q_starts, *kv_starts;
+    const uint32_t *q_starts, *kv_starts, *kv_lengths;
     uint32_t q_rows, kv_rows, sequences, heads, kv_heads, dim;
     uint32_t lq, lk;              // of every sequence, where there are no starts
     int causal, window;
@@ -64,11 +64,12 @@ __device__ __forceinline__ Place place_of(const AttentionArgs &p, bool by_keys, 
     const bool down = !by_keys || !p.causal;   // (of keys, the first are seen by the most queries)
     Place at;
     at.none = false;
+    auto keys_of = [&](uint32_t s, uint32_t room) { return p.kv_lengths ? min(p.kv_lengths[s], room) : room; };
     if (!p.q_starts) {
         const uint32_t s = pair / p.kv_heads;
         at.head = pair - s * p.kv_heads;
         at.tile = down ? p.tiles - 1 - rank : rank;
-        at.q0 = s * p.lq; at.lq = p.lq; at.k0 = s * p.lk; at.lk = p.lk;
+        at.q0 = s * p.lq; at.lq = p.lq; at.k0 = s * p.lk; at.lk = keys_of(s, p.lk);
         return at;
     }
     at.head = pair;
@@ -109,7 +110,7 @@ __device__ __forceinline__ Place place_of(const AttentionArgs &p, bool by_keys, 
         at.tile = tile - __builtin_amdgcn_readfirstlane(first(s));
     }
     at.q0 = min(p.q_starts[s], p.q_rows); at.lq = max(min(p.q_starts[s + 1], p.q_rows), at.q0) - at.q0;
-    at.k0 = min(p.kv_starts[s], p.kv_rows); at.lk = max(min(p.kv_starts[s + 1], p.kv_rows), at.k0) - at.k0;
+    at.k0 = min(p.kv_starts[s], p.kv_rows); at.lk = keys_of(s, max(min(p.kv_starts[s + 1], p.kv_rows), at.k0) - at.k0);
     return at;
 }
 
@@ -853,7 +854,7 @@ __global__ __launch_bounds__(kBlock) void k_attention_add(AddArgs p) {
 
 AttentionArgs args_of(const lgc_attention_shape &shape) {
     AttentionArgs p{};
-    p.q_starts = shape.q_starts; p.kv_starts = shape.kv_starts;
+    p.q_starts = shape.q_starts; p.kv_starts = shape.kv_starts; p.kv_lengths = shape.kv_lengths;
     p.q_rows = (uint32_t)shape.q_rows; p.kv_rows = (uint32_t)shape.kv_rows; p.sequences = (uint32_t)shape.sequences;
     p.heads = shape.heads; p.kv_heads = shape.kv_heads; p.dim = shape.dim;
     p.lq = (uint32_t)(shape.q_rows / shape.sequences); p.lk = (uint32_t)(shape.kv_rows / shape.sequences);

@@ -28,8 +28,8 @@ class Shape(C.Structure):
                 ("causal", C.c_int32), ("window", u32)]
 
 
-def shape(q_rows=256, kv_rows=256, sequences=1, heads=4, kv_heads=2, dim=64, scale=0.125, causal=1, window=0, q_starts=None, kv_starts=None):
-    return Shape(q_rows, kv_rows, sequences, q_starts, kv_starts, heads, kv_heads, dim, scale, causal, window)
+def shape(q_rows=256, kv_rows=256, sequences=1, heads=4, kv_heads=2, dim=64, scale=0.125, causal=1, window=0, q_starts=None, kv_starts=None, kv_lengths=None):
+    return Shape(q_rows, kv_rows, sequences, q_starts, kv_starts, heads, kv_heads, dim, scale, causal, window, kv_lengths)
 
 
 def attention(l, ctx, s, **change):
@@ -69,6 +69,7 @@ REFUSED = [
     (attention, (shape(scale=0.0),), "scale"), (attention, (shape(scale=-1.0),), "scale"), (attention, (shape(scale=math.nan),), "scale"), (attention, (shape(scale=math.inf),), "scale"),
     (attention, (shape(q_starts=at(11).value),), "starts"), (attention, (shape(kv_starts=at(11).value),), "starts"),
     (attention, (shape(q_starts=ODD.value, kv_starts=at(11).value),), "starts"), (attention, (shape(sequences=3),), "equal"),
+    (attention, (shape(kv_lengths=ODD.value),), "lengths"), (attention_grad, (shape(kv_lengths=at(11).value),), "cache"),
     (attention, (shape(), dict(q=None)), "q is NULL"), (attention, (shape(), dict(k=None)), "k is NULL"), (attention, (shape(), dict(v=None)), "v is NULL"),
     (attention, (shape(), dict(o=None)), "o is NULL"), (attention, (shape(), dict(q=ODD)), "q is not"), (attention, (shape(), dict(ld_k=127)), "k are"),
     (attention, (shape(), dict(ld_v=132)), "v is not"), (attention, (shape(), dict(ld_q=(1 << 24) + 8)), "q is not"), (attention, (shape(), dict(o=at(2))), "overlap"),

@@ -172,6 +172,28 @@ def seen_keys(n, window):
     return ref.visible(n, n, True, window)
 
 
+@pytest.mark.parametrize("starts", [None, [0, 3000, 3000, 6000]])
+def test_caches_with_room(B, ctx, starts):
+    """kv_lengths: of each sequence's rows the first so many, whatever the others hold; a length past the room is the room."""
+    lengths, rooms = [1500, 0, 2500], [2000] * 3 if starts is None else [3000, 0, 3000]
+    for lengths in ([1500, 0, 2500], [1, 7, 9000]):
+        c = Case(6, 6000, 4, 2, 64, 3, None if starts is None else ([0, 2, 4, 6], starts), seed=40)
+        real = [min(n, room) for n, room in zip(lengths, rooms)]
+        firsts = [0, 2000, 4000] if starts is None else starts[:3]
+        for first, n, room in zip(firsts, real, rooms):
+            c.k[first + n:first + room] = math.nan
+            c.v[first + n:first + room] = math.inf
+        how = {} if starts is None else {n: torch.tensor(s, dtype=torch.int32, device="cuda") for n, s in (("q_starts", [0, 2, 4, 6]), ("kv_starts", starts))}
+        shape = B.AttentionShape(4, 2, 64, sequences=3, kv_lengths=torch.tensor(lengths, dtype=torch.int32, device="cuda"), **how)
+        o, lse = torch.full_like(c.q, KEEP), torch.full((6, 4), KEEP, device="cuda")
+        B.lgc_attention(ctx, shape, c.q, c.k, c.v, o, lse)
+        k, v = (torch.cat([x[first:first + n] for first, n in zip(firsts, real)]) for x in (c.k, c.v))
+        packed = [0, real[0], real[0] + real[1], sum(real)]
+        want_o, want_lse, off_o, off_lse = ref.attention(c.q, k, v, 4, 2, 64, c.scale, 3, [0, 2, 4, 6], packed)
+        near(o, want_o, off_o, "o")
+        near(lse, want_lse, off_lse, "lse")
+
+
 def test_garbage_around_sequences(B, ctx):
     """Rows of no sequence may hold anything, in front, behind and between what is read together."""
     starts = ([5, 90, 200], [8, 100, 260])
@@ -331,6 +353,7 @@ def test_the_binding_s_checks(B, ctx):
              lambda: B.lgc_attention(ctx, c.shape(B), c.q.cpu(), c.k, c.v, o), lambda: B.AttentionShape(4, 2, 64, q_starts=torch.zeros(2, dtype=torch.int32, device="cuda")),
              lambda: B.AttentionShape(4, 2, 64, q_starts=torch.zeros(3, dtype=torch.int32, device="cuda"), kv_starts=torch.zeros(2, dtype=torch.int32, device="cuda")),
              lambda: B.AttentionShape(4, 2, 64, q_starts=torch.zeros(2, device="cuda"), kv_starts=torch.zeros(2, device="cuda")), lambda: B.AttentionShape(4, 2, -64),
+             lambda: B.AttentionShape(4, 2, 64, sequences=2, kv_lengths=torch.zeros(1, dtype=torch.int32, device="cuda")),
              lambda: B.lgc_attention_grad(ctx, c.shape(B), c.do, c.q, c.k, c.v, o, lse, torch.empty_like(c.k), torch.empty_like(c.k), torch.empty_like(c.v), lse.clone())]
     for call in wrong:
         with pytest.raises(ValueError):
