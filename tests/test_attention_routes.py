@@ -25,7 +25,7 @@ def at(i):
 
 class Shape(C.Structure):
     _fields_ = [("q_rows", u64), ("kv_rows", u64), ("sequences", u64), ("q_starts", p), ("kv_starts", p), ("heads", u32), ("kv_heads", u32), ("dim", u32), ("scale", f32),
-                ("causal", C.c_int32), ("window", u32)]
+                ("causal", C.c_int32), ("window", u32), ("kv_lengths", p)]
 
 
 def shape(q_rows=256, kv_rows=256, sequences=1, heads=4, kv_heads=2, dim=64, scale=0.125, causal=1, window=0, q_starts=None, kv_starts=None, kv_lengths=None):
