@@ -23,7 +23,7 @@ typedef __bf16 bf8 __attribute__((ext_vector_type(8)));
 typedef float f16 __attribute__((ext_vector_type(16)));
 typedef __attribute__((address_space(3))) void *Lds;
 
-constexpr int kTileKeys = 64;     // keys (forward, dq) or rows (dk, dv) that are in LDS at a time
+constexpr int kTileKeys = 64;     // keys of a tile in LDS (forward, dq)
 constexpr float kLn2 = 0.69314718055994530942f;
 // The running maximum is followed only when it grows by more than this many powers of two: p up to 2^8 loses nothing in fp32 or bf16, and sums are rarely scaled anew.
 constexpr float kSlack = 8.f;
@@ -56,7 +56,7 @@ struct Place {
 
 // Which tile of which sequence and key head a block works on.  Blocks go to the compute units in their order, and to the eight XCDs in turn.  So the heads (and sequences, if they have one length)
 // come in turn too, which gives most XCDs few of them, whose keys its L2 holds; and of each the tile first that has the most to do under a causal mask, so that short ones fill the end
-// (4 x 4096 tokens, 32 / 8 heads of 128, one sequence of a head after the other: backward 3148 us, so 2475).  The order across up to 64 sequences of different lengths is found by
+// (backward of 4 x 4096 tokens, 32 / 8 heads of 128, as the kernels then were: one sequence of a head after the other 3148 us, so 2475).  The order across up to 64 sequences of different lengths is found by
 // counting: how many tiles have at least some number in their sequence.  With more of them, tile number starts[s] * group / tile_rows + s is the first of sequence s: that leaves each as many as
 // it can need, and a block finds its sequence without a table.
 __device__ __forceinline__ Place place_of(const AttentionArgs &p, bool by_keys, uint32_t tile_rows) {
@@ -145,9 +145,9 @@ __device__ __forceinline__ uint32_t exchange(uint32_t row) { return (kDim == 128
 // 16 bytes per lane from memory straight to LDS, `to` (the same for all lanes) on.  The compiler, which cannot tell what is under way from what is read, would wait for such loads of its own before
 // every turned read of LDS; here arrived() waits for them, in its place.  No register waits for them.
 __device__ __forceinline__ void bring(uint32_t to, const void *base, uint32_t offset) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(to), "v"(offset), "s"(base));
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(to), "v"(offset), "s"(base) : "m0", "memory");
 }
-__device__ __forceinline__ void bring(uint32_t to, const void *at) { asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(to), "v"(at)); }
+__device__ __forceinline__ void bring(uint32_t to, const void *at) { asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(to), "v"(at) : "m0", "memory"); }
 
 // How a block loads tiles of kRows rows to LDS: a lane takes one piece of every kPass-th row.  Tiles whose rows all exist, of which there are `whole`, cost it three instructions a load; columns
 // that the head does not have are zeroed in LDS once, and left by lanes that are switched off.
@@ -159,9 +159,10 @@ struct Loader {
     uint32_t ld, rows, whole, row, piece, offset, wave;
     bool there;   // the head has the piece's columns
     __device__ __forceinline__ Loader(const uint16_t *base_, uint64_t ld_, uint32_t rows_, uint32_t dim) : base(base_), ld((uint32_t)ld_), rows(rows_) {
-        wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64) * 1024;
-        row = threadIdx.x / kPieces;
-        piece = (threadIdx.x % kPieces ^ exchange<kDim>(row)) * 8;
+        const uint32_t thread = threadIdx.x % kThreads;
+        wave = __builtin_amdgcn_readfirstlane(thread / 64) * 1024;
+        row = thread / kPieces;
+        piece = (thread % kPieces ^ exchange<kDim>(row)) * 8;
         offset = (row * ld + piece) * 2;
         there = piece < dim;
         whole = rows / kRows;
@@ -169,7 +170,7 @@ struct Loader {
     // The zeros, in `stages` places that lie one after the other
     __device__ __forceinline__ void pad(uint8_t *place, int stages) const {
         if (!there)
-            for (int i = 0; i < stages * kLoads; ++i) *((u4 *)place + i * kThreads + threadIdx.x) = u4{};
+            for (int i = 0; i < stages * kLoads; ++i) *((u4 *)place + i * kThreads + threadIdx.x % kThreads) = u4{};
     }
     __device__ __forceinline__ const uint16_t *tile(uint32_t number) const { return base + (uint64_t)number * kRows * ld; }
     // A whole tile's, from its place in memory on
@@ -262,7 +263,7 @@ __device__ __forceinline__ bool clean(uint8_t *tile) {
     uint32_t bad = 0;
 #pragma unroll
     for (int i = 0; i < kBytes / (kThreads * 16); ++i) {
-        u4 *const at = (u4 *)tile + i * kThreads + threadIdx.x, v = *at;
+        u4 *const at = (u4 *)tile + i * kThreads + threadIdx.x % kThreads, v = *at;
         u4 w = v;
 #pragma unroll
         for (int j = 0; j < 4; ++j) w[j] &= ~(((v[j] & 0x7f80u) == 0x7f80u ? 0xffffu : 0u) | ((v[j] & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u));
@@ -339,21 +340,51 @@ __device__ __forceinline__ void part_of(uint32_t parts, uint32_t &from, uint32_t
     to = min(from + share, end);
 }
 
-// o and lse.  A block has 256 rows, a wavefront 32; keys and values come in tiles of 64.  The two wavefronts of a SIMD take turns: while one makes scores and joins values on the matrix cores, the
-// other makes probabilities of its scores, and all change places at a barrier.  A tile's keys are loaded two tiles ahead of their use, its values, which are used a tile later, one ahead.
-template <int kDim, int kWaves>
-__global__ __launch_bounds__(64 * kWaves, kDim == 64 ? 3 : 2) void k_attention(AttentionArgs p) {
-    constexpr int kThreads = 64 * kWaves, kTile = 32 * kWaves, kSteps = kDim / 16, kWide = kDim / 32, kBytes = kTileKeys * kDim * 2, kStages = 2;
-    __shared__ __align__(16) uint8_t lds[2 * kStages * kBytes];
+// What a team takes of its block's tiles, one half; how many turns both have
+template <int kTeams>
+__device__ __forceinline__ uint32_t team_of(uint32_t team, uint32_t &from, uint32_t &to) {
+    if constexpr (kTeams == 1) return to - from;
+    const uint32_t turns = (to - from + 1) / 2;
+    if (team) from += turns;
+    else to = min(to, from + turns);
+    return turns;
+}
+
+// A lane's results to LDS, from where the first team's lane takes them
+template <int kWide>
+__device__ __forceinline__ void hand_over(f4 *to, const f16 (&x)[kWide]) {
+#pragma unroll
+    for (int d = 0; d < kWide; ++d)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) to[(4 * d + e) * 64] = f4{x[d][4 * e], x[d][4 * e + 1], x[d][4 * e + 2], x[d][4 * e + 3]};
+}
+
+// o and lse, in one pass over the keys with a running maximum and sum.  A block has 128 rows, a wavefront 32, whose queries stay in registers; keys and values come in tiles of 64, straight to LDS,
+// the keys two tiles ahead of their use and the values one: they are used a tile later than the keys, because the next tile's scores are made on the matrix cores while this one's probabilities are
+// made by the vector units.  One barrier a tile; three blocks fit a compute unit (heads of 128: two), so that one's barrier and loads hide behind another's work.
+//
+// Two teams: eight wavefronts, of which four take the first half of the block's tiles and four the second, in LDS of their own; their sums meet in LDS at the end.  It halves the chain of tiles that
+// a block goes through one after the other, with no partial results in memory, but a compute unit holds one such block.
+//
+// Bound: per 32 rows and 64 keys of a head of 128, 32 products of 33 cycles on the matrix cores, and 900 cycles of vector instructions (five an element, the exponential 8.5 cycles) beside them, which the
+// same SIMD's other wavefront can fill only in part, at a clock that falls to 1.9 GHz.  4 x 4096 tokens, causal, 32 / 8 heads of 128: 570 us, 0.96 PFLOP/s; 8 x 1 tokens after 4096: 25 us and 4.5 for the join
+// of eight parts, 5.4 TB/s of keys and values.  Taken back: two groups of rows per wavefront, one wavefront per SIMD (680 us, so 921, as the kernel then was); a SIMD's two wavefronts in turn between barriers,
+// 256 rows (565 / 575); eight wavefronts without teams (586); loads among the products (650); three tiles under way (no change).
+template <int kDim, int kTeams>
+__global__ __launch_bounds__(256 * kTeams, kDim == 64 && kTeams == 1 ? 3 : 2) void k_attention(AttentionArgs p) {
+    constexpr int kThreads = 256, kTile = 128, kSteps = kDim / 16, kWide = kDim / 32, kBytes = kTileKeys * kDim * 2, kStages = 2;
+    __shared__ __align__(16) uint8_t all_lds[kTeams * 2 * kStages * kBytes];
     const Place at = place_of(p, false, kTile);
     if (at.none) return;
     const uint32_t rows = at.lq * p.group.by, row0 = at.tile * kTile;
     if (row0 >= rows) return;
-    const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), r = lane & 31, g = lane >> 5;
+    const uint32_t lane = threadIdx.x & 63, all_wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), wave = kTeams == 1 ? all_wave : all_wave % 4, team = kTeams == 1 ? 0 : all_wave / 4, r = lane & 31, g = lane >> 5;
+    uint8_t *const lds = all_lds + team * (2 * kStages * kBytes);
     const float c = p.scale * kLog2e;
     const Range range = range_of(p, at, rows, row0, wave, kTile);
     uint32_t from = range.from, to = range.to;
     part_of(p.parts, from, to);
+    const uint32_t turns = team_of<kTeams>(team, from, to);
 
     const uint16_t *const k = p.k + (uint64_t)at.k0 * p.ld_k + at.head * p.dim, *const v = p.v + (uint64_t)at.k0 * p.ld_v + at.head * p.dim;
     typedef Loader<kDim, kTileKeys, kThreads> Tiles;
@@ -443,6 +474,8 @@ __global__ __launch_bounds__(64 * kWaves, kDim == 64 ? 3 : 2) void k_attention(A
         load_values(from);
         load_keys(from + 1);
         scores(keys);
+    } else if (turns) {
+        meet();
     }
     for (uint32_t tile = from; tile < to; ++tile) {
         const int key0 = (int)(tile * kTileKeys);
@@ -459,6 +492,8 @@ __global__ __launch_bounds__(64 * kWaves, kDim == 64 ? 3 : 2) void k_attention(A
         join(values + place * kBytes);
     }
 
+    if constexpr (kTeams == 2)
+        for (uint32_t turn = to - from; turn < turns; ++turn) meet();   // (the other team's)
     if (__syncthreads_or(bad))
         for (uint32_t key = from * kTileKeys; key < min(to * kTileKeys, at.lk); ++key) {
             const int key0 = (int)(key / kTileKeys * kTileKeys);
@@ -466,11 +501,30 @@ __global__ __launch_bounds__(64 * kWaves, kDim == 64 ? 3 : 2) void k_attention(A
             spoil<kDim>(o, v + (uint64_t)key * p.ld_v, p.dim, (int)key >= seen.lo && (int)key < seen.hi);
         }
     sum += across(sum);
+    if constexpr (kTeams == 2) {   // the second team's results are added to the first's, whose lanes have the same rows and columns
+        f4 *const theirs = (f4 *)all_lds + wave * (kWide * 4 * 64) + lane;
+        float *const ends = (float *)(all_lds + kDim * 512) + wave * 128;
+        if (team) {
+            hand_over(theirs, o);
+            ends[lane] = most;
+            ends[64 + lane] = sum;
+        }
+        __syncthreads();
+        if (team) return;
+        const float other = ends[lane], both = fmaxf(most, other);
+        const float mine = both == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((most - both) * c), its = both == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((other - both) * c);
+        most = both;
+        sum = sum * mine + ends[64 + lane] * its;
+#pragma unroll
+        for (int d = 0; d < kWide; ++d)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) o[d][e] = o[d][e] * mine + theirs[(4 * d + e / 4) * 64][e % 4] * its;
+    }
     const float by = sum == 0.f ? 0.f : 1.f / sum;
     const float lse = sum == 0.f ? -INFINITY : (most * c + __log2f(sum)) * kLn2;
     const uint64_t line = (uint64_t)(at.q0 + token) * p.heads + head, all = (uint64_t)p.q_rows * p.heads;
     if (p.parts == 1)
-        store_rows<kDim>(lds + wave * 64 * kDim, o, by, p.dim, [&](uint32_t i) {
+        store_rows<kDim>(all_lds + wave * (kTeams * 64 * kDim), o, by, p.dim, [&](uint32_t i) {   // (of two teams: where its own were read from)
             const uint32_t row = row0 + wave * 32 + i, t = token_of(row);
             return row < rows ? p.out + (uint64_t)(at.q0 + t) * p.ld_out + (at.head * p.group.by + row - t * p.group.by) * p.dim : nullptr;
         });
@@ -514,10 +568,11 @@ __global__ __launch_bounds__(kBlock) void k_attention_join(AttentionArgs p) {
         most = next;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const float w = i0 + i >= p.parts || lse[i] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((lse[i] - most) * kLog2e);
+            const bool counts = i0 + i < p.parts && lse[i] != -INFINITY;   // (a weight that is 0 by its size keeps a NaN of the part's)
+            const float w = counts ? __builtin_amdgcn_exp2f((lse[i] - most) * kLog2e) : 0.f;
             total += w;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = fmaf(w, w == 0.f ? 0.f : part[i][e / 4][e % 4], x[e]);
+            for (int e = 0; e < 8; ++e) x[e] = fmaf(w, counts ? part[i][e / 4][e % 4] : 0.f, x[e]);
         }
     }
     const float by = total == 0.f ? 0.f : 1.f / total;
@@ -527,16 +582,20 @@ __global__ __launch_bounds__(kBlock) void k_attention_join(AttentionArgs p) {
     if (p.lse && from == 0) p.lse[id] = total == 0.f ? -INFINITY : most + __log2f(total) * kLn2;
 }
 
-// dq, and delta for the kernel after it.  As the forward pass, with three products a tile of 64 keys, taken in two halves.
-template <int kDim, int kWaves>
-__global__ __launch_bounds__(64 * kWaves, kDim == 64 ? 3 : 2) void k_attention_dq(AttentionArgs p) {
-    constexpr int kThreads = 64 * kWaves, kTile = 32 * kWaves, kSteps = kDim / 16, kWide = kDim / 32, kBytes = kTileKeys * kDim * 2, kStages = 2;
-    __shared__ __align__(16) uint8_t lds[2 * kStages * kBytes];
+// dq, and delta for the kernel after it (in this kernel a row's o and do are needed once, by the lanes that have the row).  Blocks, tiles and teams as in the forward pass; three products a tile, which
+// is taken in two halves of 32 keys, so that scores and slopes of one fit the registers beside q and do: a half's scores are made before the join of the half before, between whose products its slopes
+// lie.  Bound as the forward pass, with 48 products and half as many vector instructions for each: 4 x 4096 tokens, causal, 32 / 8 heads of 128: 760 us, 1.08 PFLOP/s; 16384 tokens of 8 heads of 64: 390 us.
+template <int kDim, int kTeams>
+__global__ __launch_bounds__(256 * kTeams, kDim == 64 && kTeams == 1 ? 3 : 2) void k_attention_dq(AttentionArgs p) {
+    constexpr int kThreads = 256, kTile = 128, kSteps = kDim / 16, kWide = kDim / 32, kBytes = kTileKeys * kDim * 2, kStages = 2;
+    __shared__ __align__(16) uint8_t all_lds[kTeams * 2 * kStages * kBytes];
     const Place at = place_of(p, false, kTile);
     if (at.none) return;
     const uint32_t rows = at.lq * p.group.by, row0 = at.tile * kTile;
     if (row0 >= rows) return;
-    const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), r = lane & 31, g = lane >> 5;
+    const uint32_t lane = threadIdx.x & 63, all_wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), wave = kTeams == 1 ? all_wave : all_wave % 4, team = kTeams == 1 ? 0 : all_wave / 4;
+    const uint32_t r = lane & 31, g = lane >> 5;
+    uint8_t *const lds = all_lds + team * (2 * kStages * kBytes);
     const float c = p.scale * kLog2e;
 
     const uint32_t wanted = row0 + wave * 32 + r, row = min(wanted, rows - 1), token = quotient(row, p.group), head = at.head * p.group.by + row - token * p.group.by;
@@ -555,11 +614,12 @@ __global__ __launch_bounds__(64 * kWaves, kDim == 64 ? 3 : 2) void k_attention_d
     delta += across(delta);
     float lse = p.lse[line * p.heads + head];
     lse = lse == -INFINITY ? INFINITY : lse * kLog2e;   // a row that sees nothing: p = 0
-    if (blockIdx.y == 0 && g == 0 && wanted < rows) p.delta[line * p.heads + head] = delta;
+    if (blockIdx.y == 0 && team == 0 && g == 0 && wanted < rows) p.delta[line * p.heads + head] = delta;
     const Range range = range_of(p, at, rows, row0, wave, kTile);
     const Seen seen = seen_by(p, at, token);
     uint32_t from = range.from, to = range.to;
     part_of(p.parts, from, to);
+    const uint32_t turns = team_of<kTeams>(team, from, to);
 
     const uint16_t *const k = p.k + (uint64_t)at.k0 * p.ld_k + at.head * p.dim, *const v = p.v + (uint64_t)at.k0 * p.ld_v + at.head * p.dim;
     typedef Loader<kDim, kTileKeys, kThreads> Tiles;
@@ -631,6 +691,8 @@ __global__ __launch_bounds__(64 * kWaves, kDim == 64 ? 3 : 2) void k_attention_d
         join(stage, 1);
     }
 
+    if constexpr (kTeams == 2)
+        for (uint32_t turn = to - from; turn < turns; ++turn) meet();   // (the other team's)
     if (__syncthreads_or(bad))   // a row that sees such a key (whose scores were made without them): NaNs
         for (uint32_t key = from * kTileKeys; key < min(to * kTileKeys, at.lk); ++key) {
             const int key0 = (int)(key / kTileKeys * kTileKeys);
@@ -644,23 +706,42 @@ __global__ __launch_bounds__(64 * kWaves, kDim == 64 ? 3 : 2) void k_attention_d
 #pragma unroll
                     for (int e = 0; e < 16; ++e) dq[d][e] = NAN;
         }
+    if constexpr (kTeams == 2) {
+        f4 *const theirs = (f4 *)all_lds + wave * (kWide * 4 * 64) + lane;
+        if (team) hand_over(theirs, dq);
+        __syncthreads();
+        if (team) return;
+#pragma unroll
+        for (int d = 0; d < kWide; ++d)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) dq[d][e] += theirs[(4 * d + e / 4) * 64][e % 4];
+    }
     if (p.parts == 1)
-        store_rows<kDim>(lds + wave * 64 * kDim, dq, p.scale, p.dim, [&](uint32_t i) {
+        store_rows<kDim>(all_lds + wave * (kTeams * 64 * kDim), dq, p.scale, p.dim, [&](uint32_t i) {
             const uint32_t row = row0 + wave * 32 + i, t = quotient(min(row, rows - 1), p.group);
             return row < rows ? p.out + (uint64_t)(at.q0 + t) * p.ld_out + (at.head * p.group.by + row - t * p.group.by) * p.dim : nullptr;
         });
     else if (wanted < rows) store_row<kDim>(p.scratch + (blockIdx.y * (uint64_t)p.q_rows + line) * p.heads * p.dim + col, dq, p.scale, p.dim);
 }
 
-// dk and dv.  A block has 256 keys, a wavefront 32; rows of q and of the gradient come in tiles of 32, one head of the group after the other, and the wavefronts of a SIMD take turns as in the
-// forward pass.  The block's values lie in LDS (in registers, with the keys, there would be room for one wavefront per SIMD).
-template <int kDim, int kWaves>
-__global__ __launch_bounds__(64 * kWaves, kDim == 64 ? 3 : 2) void k_attention_dkv(AttentionArgs p) {
-    constexpr int kThreads = 64 * kWaves, kTile = 32 * kWaves, kSteps = kDim / 16, kWide = kDim / 32, kRows = kDim == 64 || kWaves == 8 ? 64 : 32, kHalves = kRows / 32, kBytes = kRows * kDim * 2, kStats = 2 * kRows, kStages = 2, kValues = kTile * kDim * 2;
-    __shared__ __align__(16) uint8_t lds[kStages * (2 * kBytes + kStats * 4) + kValues];
+// dk and dv.  A block has 32 keys for each wavefront of a team, which stay in registers; its values lie in LDS (in registers beside the keys, they would leave room for nothing else), and its rows of q
+// and do come in tiles, one head of the group after the other, straight to LDS, one tile ahead, with lse and -delta by way of a register of one lane each; -delta is what the sum of do . v begins with.
+// Four products for 32 rows and keys: q and do are each read from LDS as rows (scores) and turned (the sums over rows).  Tiles of 64 rows, in two halves: the second half's scores lie between the products of
+// the first half's join; of 32 rows for heads of 128 in teams of four, where LDS holds two such teams, or two such blocks.
+//
+// Eight wavefronts in one team have 256 keys, which read q and do half as often as two blocks of four; two teams of four share 128 keys, and each has half of the rows.
+// Bound: the products (64 of them for 32 rows and 64 keys of a head of 128, 54 % of the time on the matrix cores) and, beside them, LDS, which gives 16 reads of 1 KB for every eight products.
+// 4 x 4096 tokens, causal, 32 / 8 heads of 128: 1130 us, 0.97 PFLOP/s; 16384 tokens of 8 heads of 64: 590 us.
+template <int kDim, int kWaves, int kTeams>
+__global__ __launch_bounds__(64 * kWaves * kTeams, kDim == 64 && kTeams == 1 ? 3 : 2) void k_attention_dkv(AttentionArgs p) {
+    constexpr int kThreads = 64 * kWaves, kTile = 32 * kWaves, kSteps = kDim / 16, kWide = kDim / 32;
+    constexpr int kRows = kDim == 64 || kWaves == 8 ? 64 : 32, kHalves = kRows / 32, kBytes = kRows * kDim * 2, kStats = 2 * kRows, kStages = 2, kValues = kTile * kDim * 2;
+    __shared__ __align__(16) uint8_t all_lds[kTeams * kStages * (2 * kBytes + kStats * 4) + kValues];
     const Place at = place_of(p, true, kTile);
     if (at.none || at.tile * kTile >= at.lk) return;
-    const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), r = lane & 31, g = lane >> 5;
+    const uint32_t lane = threadIdx.x & 63, all_wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), wave = kTeams == 1 ? all_wave : all_wave % kWaves, team = kTeams == 1 ? 0 : all_wave / kWaves;
+    const uint32_t thread = threadIdx.x % kThreads, r = lane & 31, g = lane >> 5;
+    uint8_t *const lds = all_lds + team * (2 * kStages * kBytes);
     const uint32_t block_key = at.tile * kTile, wave_key = block_key + wave * 32, key = wave_key + r;
     const float c = p.scale * kLog2e;
     const int off = (int)at.lk - (int)at.lq;   // a query's number and this are its position
@@ -687,10 +768,11 @@ __global__ __launch_bounds__(64 * kWaves, kDim == 64 ? 3 : 2) void k_attention_d
 
     uint32_t from = 0, to = tiles * p.group.by;
     part_of(p.parts, from, to);
+    const uint32_t turns = team_of<kTeams>(team, from, to);
     const uint64_t head0 = (uint64_t)at.head * p.group.by;
     const uint16_t *const q = p.q + at.q0 * p.ld_q + head0 * p.dim, *const grad = p.grad + at.q0 * p.ld_grad + head0 * p.dim;
-    const uint32_t queries = address(lds), grads = queries + kStages * kBytes, values = grads + kStages * kBytes, lane_rows_at = lane_rows<kDim>(), lane_columns_at = lane_columns<kDim>();
-    float *const stats = (float *)(lds + 2 * kStages * kBytes + kValues);
+    const uint32_t queries = address(lds), grads = queries + kStages * kBytes, values = address(all_lds) + kTeams * 2 * kStages * kBytes, lane_rows_at = lane_rows<kDim>(), lane_columns_at = lane_columns<kDim>();
+    float *const stats = (float *)(all_lds + kTeams * 2 * kStages * kBytes + kValues) + team * (kStages * kStats);
     // What comes next: tile `number` of a head of the group.  lse (in powers of two) and -delta of its rows come by one of the first wavefronts' lanes, and go to LDS when they have arrived.
     uint32_t head = tiles ? from / tiles : 0u, number = tile0 + from - head * tiles;
     Loader<kDim, kRows, kThreads> of_queries(q + head * p.dim, p.ld_q, at.lq, p.dim), of_grads(grad + head * p.dim, p.ld_grad, at.lq, p.dim);
@@ -698,11 +780,11 @@ __global__ __launch_bounds__(64 * kWaves, kDim == 64 ? 3 : 2) void k_attention_d
     of_queries.pad(lds, 2 * kStages);
     float stat = 0.f;
     auto load = [&](uint32_t stage) {
-        if (threadIdx.x < kStats) {
-            const uint32_t row = number * kRows + threadIdx.x % kRows;
+        if (thread < kStats) {
+            const uint32_t row = number * kRows + thread % kRows;
             const uint64_t place = (uint64_t)(at.q0 + min(row, at.lq - 1)) * p.heads + head0 + head;
-            stat = threadIdx.x < kRows ? p.lse[place] : p.delta[place];
-            if (threadIdx.x < kRows) stat = row >= at.lq || stat == -INFINITY ? INFINITY : stat * kLog2e;
+            stat = thread < kRows ? p.lse[place] : p.delta[place];
+            if (thread < kRows) stat = row >= at.lq || stat == -INFINITY ? INFINITY : stat * kLog2e;
             else stat = row < at.lq ? -stat : 0.f;
         }
         if (number < of_queries.whole) {
@@ -723,7 +805,7 @@ __global__ __launch_bounds__(64 * kWaves, kDim == 64 ? 3 : 2) void k_attention_d
             next_grads = of_grads.tile(tile0);
         }
     };
-    auto keep = [&](uint32_t stage) { if (threadIdx.x < kStats) stats[stage * kStats + threadIdx.x] = stat; };
+    auto keep = [&](uint32_t stage) { if (thread < kStats) stats[stage * kStats + thread] = stat; };
 
     f16 dk[kWide] = {}, dv[kWide] = {}, s, dp;
     bf8 prob[2], ds[2];
@@ -777,7 +859,7 @@ __global__ __launch_bounds__(64 * kWaves, kDim == 64 ? 3 : 2) void k_attention_d
     uint32_t now = number;   // the tile that is worked on
     bool bad = false;
     if (from < to) {
-        Loader<kDim, kTile, kThreads>(p.v + (uint64_t)at.k0 * p.ld_v + at.head * p.dim, p.ld_v, at.lk, p.dim).load_any(values, at.tile);
+        if (team == 0) Loader<kDim, kTile, kThreads>(p.v + (uint64_t)at.k0 * p.ld_v + at.head * p.dim, p.ld_v, at.lk, p.dim).load_any(values, at.tile);
         load(0);
     }
     for (uint32_t it = from, stage = 0; it < to; ++it, stage ^= 1) {
@@ -803,16 +885,34 @@ __global__ __launch_bounds__(64 * kWaves, kDim == 64 ? 3 : 2) void k_attention_d
         if (++now == tile1) now = tile0;
     }
 
+    if constexpr (kTeams == 2)
+        for (uint32_t turn = to - from; turn < turns; ++turn) meet();   // (the other team's)
     if (__syncthreads_or(bad))
         for (uint32_t it = from; it < to; ++it)
             for (uint32_t i = (tile0 + it % tiles) * kRows; i < min((tile0 + it % tiles + 1) * kRows, at.lq); ++i) {
                 if (block_all_of(i / kRows * kRows)) continue;
                 spoil<kDim>(dv, grad + (uint64_t)i * p.ld_grad + it / tiles * p.dim, p.dim, i >= seen_from && i < seen_to);
             }
+    if constexpr (kTeams == 2) {
+        f4 *const theirs = (f4 *)all_lds + wave * (kWide * 4 * 64) + lane;
+        auto add = [&](f16 (&x)[kWide]) {
+            if (team) hand_over(theirs, x);
+            __syncthreads();
+            if (team == 0)
+#pragma unroll
+                for (int d = 0; d < kWide; ++d)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) x[d][e] += theirs[(4 * d + e / 4) * 64][e % 4];
+        };
+        add(dk);
+        __syncthreads();
+        add(dv);
+        if (team) return;
+    }
     if (p.parts == 1) {
         auto place = [&](uint16_t *base, uint64_t ld, uint32_t i) { return wave_key + i < at.lk ? base + (uint64_t)(at.k0 + wave_key + i) * ld + at.head * p.dim : nullptr; };
-        store_rows<kDim>(lds + wave * 64 * kDim, dk, p.scale, p.dim, [&](uint32_t i) { return place(p.dk, p.ld_dk, i); });
-        store_rows<kDim>(lds + wave * 64 * kDim, dv, 1.f, p.dim, [&](uint32_t i) { return place(p.dv, p.ld_dv, i); });
+        store_rows<kDim>(all_lds + wave * (kTeams * 64 * kDim), dk, p.scale, p.dim, [&](uint32_t i) { return place(p.dk, p.ld_dk, i); });
+        store_rows<kDim>(all_lds + wave * (kTeams * 64 * kDim), dv, 1.f, p.dim, [&](uint32_t i) { return place(p.dv, p.ld_dv, i); });
     } else if (key < at.lk) {
         const uint64_t line = at.k0 + key;
         const uint64_t wide = (uint64_t)p.kv_heads * p.dim, half = (uint64_t)p.parts * p.kv_rows * wide;
@@ -873,13 +973,13 @@ void set_tiles(AttentionArgs &p, uint64_t tokens, uint64_t group, uint64_t tile)
 uint64_t grid_of(const AttentionArgs &p) { return (uint64_t)p.tiles * p.pairs.by; }
 
 // In how many parts to make blocks' sums, of which the longest has `most` tiles and the average `mean`: where blocks are few, the time is that of the longest (us: some 2 a tile), and what parts
-// save of it they cost by their results, written and read once, and by the launch that adds them.
-uint32_t parts_for(uint64_t blocks, double most, double mean, double tile, uint64_t results, uint64_t room, int cus) {
-    uint32_t best = 1;
-    double least = 0;
+// save of it they cost by their results, written and read once, and by the launch that adds them; where a compute unit holds one block at a time, each further one begins anew (`round` us).
+struct Split { uint32_t parts; double time; };
+Split parts_for(uint64_t blocks, double most, double mean, double tile, uint64_t results, uint64_t room, int cus, double round = 0.) {
+    Split best{1, 0.};
     for (uint32_t n = 1; n <= 64 && (n == 1 || (n <= most / 2 && n * results <= room)); ++n) {
-        const double time = tile * std::max(most / n, mean * (double)blocks / (2 * cus)) + (n > 1 ? 5 + 2e-6 * (double)(n * results) : 0.);
-        if (n == 1 || time < 0.95 * least) { best = n; least = time; }
+        const double time = tile * std::max({most / n, 1., mean * (double)blocks / (2 * cus)}) + (n > 1 ? 5 + 2e-6 * (double)(n * results) : 0.) + round * (double)((n * blocks - 1) / cus);
+        if (n == 1 || time < 0.95 * best.time) best = Split{n, time};
     }
     return best;
 }
@@ -891,6 +991,21 @@ Extent extent(const AttentionArgs &p, uint64_t of, uint64_t others, uint64_t wid
     const double a = (double)of / p.sequences, b = (double)others / p.sequences, longest = p.q_starts ? std::min(2 * b, (double)others) : b;
     const double near = p.window ? (double)p.window + (double)width : 1e30;
     return Extent{std::min(longest, near), std::min(p.causal ? std::max(b - a / 2, b / 2) : b, near)};
+}
+
+// Whether two teams work on a block's tiles, and in how many parts, set in p: where blocks are few enough for a compute unit to hold its share at once, and the longest has as much to do as a compute unit
+// has altogether, so that the chain of its tiles is what takes the time.  One team / two, us, causal: forward 1024 tokens of 16 heads of 64 23.1 / 17.0, 4096 of them 75 / 60, 1024 of 32 / 8 heads of 128 28 / 25;
+// 9 sequences of 4 to 2348 tokens of 12 / 4 heads of 64 42 / 37; and not taken: 8192 of 16 heads of 64 176 / 197, 8 x 512 of 32 / 8 of 128 36 / 53, 4 x 1024 of 16 of 64 (a longest of 16 tiles) 23.3 / 25.6.
+// Backward: 1024 of 16 heads of 64 55 / 44, 4096 of 32 / 8 of 128 713 / 555, 2 x 4096 of them 1258 / 1024 (dk and dv by blocks of 256 keys / two teams), and not taken: 4 x 4096 1926 / 2044.
+bool two_teams(AttentionArgs &p, uint64_t most_blocks, double round, double most, double mean, double tile, uint64_t results, uint64_t room, int cus) {
+    const uint64_t blocks = grid_of(p);
+    const Split one = parts_for(blocks, most, mean, tile, results, room, cus);
+    p.parts = one.parts;
+    if (blocks > most_blocks * cus || most < 0.95 * mean * (double)blocks / cus || (blocks > (uint64_t)cus && most < 20)) return false;
+    const Split two = parts_for(blocks, most / 2, mean, tile, results, room, cus, round);
+    if (two.time >= one.time) return false;
+    p.parts = two.parts;
+    return true;
 }
 
 template <typename F>
@@ -906,12 +1021,15 @@ void launch_attention(const lgc_attention_shape &shape, const void *q, uint64_t 
     p.q = (const uint16_t *)q; p.k = (const uint16_t *)k; p.v = (const uint16_t *)v; p.out = (uint16_t *)o;
     p.ld_q = ld_q; p.ld_k = ld_k; p.ld_v = ld_v; p.ld_out = ld_o;
     p.lse = lse; p.scratch = scratch;
-    constexpr int kWaves = 4;
-    set_tiles(p, p.q_rows, p.group.by, 32 * kWaves);
+    set_tiles(p, p.q_rows, p.group.by, 128);
     const uint64_t rows = (uint64_t)p.q_rows * p.heads;
-    const Extent keys = extent(p, p.q_rows, p.kv_rows, 32 * kWaves / p.group.by);
-    p.parts = parts_for(grid_of(p), keys.most / kTileKeys, keys.mean / kTileKeys, p.dim > 64 ? 2 : 1.5, rows * (p.dim + 1), scratch_floats, cus);
-    with_dim(p.dim, [&](auto dim) { k_attention<decltype(dim)::value, kWaves><<<dim3((uint32_t)grid_of(p), p.parts), 64 * kWaves, 0, st>>>(p); });
+    const Extent keys = extent(p, p.q_rows, p.kv_rows, 128 / p.group.by);
+    const bool two = two_teams(p, p.dim > 64 ? 2 : 3, 3., keys.most / kTileKeys, keys.mean / kTileKeys, p.dim > 64 ? 2 : 1.5, rows * (p.dim + 1), scratch_floats, cus);
+    with_dim(p.dim, [&](auto dim) {
+        const dim3 grid((uint32_t)grid_of(p), p.parts);
+        if (two) k_attention<decltype(dim)::value, 2><<<grid, 512, 0, st>>>(p);
+        else k_attention<decltype(dim)::value, 1><<<grid, 256, 0, st>>>(p);
+    });
     if (p.parts > 1) k_attention_join<<<(uint32_t)((rows + kBlock / 16 - 1) / (kBlock / 16)), kBlock, 0, st>>>(p);
 }
 
@@ -931,11 +1049,14 @@ void launch_attention_grad(const lgc_attention_shape &shape, const void *grad, u
     };
     const uint64_t group = p.group.by;
     if (p.q_rows) {
-        constexpr int kWaves = 4;
-        set_tiles(p, p.q_rows, group, 32 * kWaves);
-        const Extent keys = extent(p, p.q_rows, p.kv_rows, 32 * kWaves / group);
-        p.parts = parts_for(grid_of(p), keys.most / kTileKeys, keys.mean / kTileKeys, p.dim > 64 ? 3 : 2, (uint64_t)p.q_rows * p.heads * p.dim, scratch_floats, cus);
-        with_dim(p.dim, [&](auto dim) { k_attention_dq<decltype(dim)::value, kWaves><<<dim3((uint32_t)grid_of(p), p.parts), 64 * kWaves, 0, st>>>(p); });
+        set_tiles(p, p.q_rows, group, 128);
+        const Extent keys = extent(p, p.q_rows, p.kv_rows, 128 / group);
+        const bool two = two_teams(p, p.dim > 64 ? 2 : 3, 3., keys.most / kTileKeys, keys.mean / kTileKeys, p.dim > 64 ? 3 : 2, (uint64_t)p.q_rows * p.heads * p.dim, scratch_floats, cus);
+        with_dim(p.dim, [&](auto dim) {
+            const dim3 grid((uint32_t)grid_of(p), p.parts);
+            if (two) k_attention_dq<decltype(dim)::value, 2><<<grid, 512, 0, st>>>(p);
+            else k_attention_dq<decltype(dim)::value, 1><<<grid, 256, 0, st>>>(p);
+        });
         add(p.q_rows, p.heads * p.dim, p.q_starts, p.out, ld_dq, nullptr, 0);
     }
     if (!p.kv_rows) return;
@@ -943,15 +1064,22 @@ void launch_attention_grad(const lgc_attention_shape &shape, const void *grad, u
     auto dkv = [&](auto dim, auto waves) {
         constexpr int kDim = decltype(dim)::value, kWaves = decltype(waves)::value;
         const Extent queries = extent(p, p.kv_rows, p.q_rows, 32 * kWaves);
-        p.parts = parts_for(grid_of(p), queries.most * group / 32, queries.mean * group / 32, kDim > 64 ? 2 : 1, 2 * (uint64_t)p.kv_rows * cols, scratch_floats, cus);
-        k_attention_dkv<kDim, kWaves><<<dim3((uint32_t)grid_of(p), p.parts), 64 * kWaves, 0, st>>>(p);
+        const double most = queries.most * group / 32, mean = queries.mean * group / 32, tile = kDim > 64 ? 2 : 1;
+        if constexpr (kWaves == 4)
+            if (two_teams(p, p.dim > 64 ? 4 : 3, 8., most, mean, tile, 2 * (uint64_t)p.kv_rows * cols, scratch_floats, cus)) {
+                k_attention_dkv<kDim, 4, 2><<<dim3((uint32_t)grid_of(p), p.parts), 512, 0, st>>>(p);
+                return;
+            }
+        p.parts = parts_for(grid_of(p), most, mean, tile, 2 * (uint64_t)p.kv_rows * cols, scratch_floats, cus).parts;
+        k_attention_dkv<kDim, kWaves, 1><<<dim3((uint32_t)grid_of(p), p.parts), 64 * kWaves, 0, st>>>(p);
     };
     typedef std::integral_constant<int, 4> Four;
     typedef std::integral_constant<int, 8> Eight;
-    // Heads of 128: eight wavefronts per block, whose 256 keys read q and do half as often, where that leaves a block per compute unit (us, four / eight: 4 x 4096 tokens of 32 / 8 heads
-    // 1290 / 1180); heads of 64: three blocks of four fit a compute unit, but one of eight (16384 tokens of 8 heads 599 / 601)
+    // Heads of 128: eight wavefronts in one team where that leaves two blocks per compute unit, one after the other (2 x 4096 tokens of 32 / 8 heads, one of them: 1258, two teams 1024), and where keys have a thousand
+    // rows and more to go through, among which the loads of 256 keys and values count less (backward, us, eight / four: 4 x 4096 tokens of 32 / 8 heads 1930 / 2050, 8 x 2048 1107 / 1154, 20 sequences, 16000 tokens
+    // 1033 / 1066, 16 x 1024 of 16 heads 414 / 410, one new token after each of 8 x 4096 168 / 131).  Heads of 64: three blocks of four fit a compute unit, one of eight (16384 tokens of 8 heads 599 / 601).
     set_tiles(p, p.kv_rows, 1, 256);
-    if (p.dim > 64 && grid_of(p) >= (uint64_t)cus) dkv(std::integral_constant<int, 128>(), Eight());
+    if (p.dim > 64 && grid_of(p) >= 2 * (uint64_t)cus && extent(p, p.kv_rows, p.q_rows, 256).mean * (double)group >= 1024.) dkv(std::integral_constant<int, 128>(), Eight());
     else {
         set_tiles(p, p.kv_rows, 1, 128);
         with_dim(p.dim, [&](auto dim) { dkv(dim, Four()); });

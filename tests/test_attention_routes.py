@@ -99,14 +99,17 @@ def call_of(f, args):
 BIG = dict(q_rows=16384, kv_rows=16384, sequences=4, heads=32, kv_heads=8, dim=128)
 LONG = dict(q_rows=16384, kv_rows=16384, heads=8, kv_heads=8, dim=64)
 ROUTES = [
-    (attention, (shape(**BIG),), ["k_attention 128 4"]), (attention, (shape(**LONG),), ["k_attention 64 4"]), (attention, (shape(dim=8),), ["k_attention 64 4"]),
-    (attention, (shape(dim=72),), ["k_attention 128 4"]), (attention, (shape(q_rows=8, kv_rows=32768, sequences=8, heads=32, kv_heads=8, dim=128),), ["k_attention 128 4", "k_attention_join"]),
-    (attention, (shape(q_rows=0),), []), (attention, (shape(kv_rows=0),), ["k_attention 64 4"]),
-    (attention_grad, (shape(**BIG),), ["k_attention_dq 128 4", "k_attention_dkv 128 8"]), (attention_grad, (shape(**LONG),), ["k_attention_dq 64 4", "k_attention_dkv 64 4"]),
-    (attention_grad, (shape(q_rows=64, kv_rows=64, dim=128),), ["k_attention_dq 128 4", "k_attention_dkv 128 4"]), (attention_grad, (shape(q_rows=0),), ["k_attention_dkv 64 4"]),
-    (attention_grad, (shape(kv_rows=0),), ["k_attention_dq 64 4"]), (attention_grad, (shape(q_rows=0, kv_rows=0),), []),
-    (attention_grad, (shape(q_rows=1, kv_rows=65536, heads=1, kv_heads=1),), ["k_attention_dq 64 4", "k_attention_add", "k_attention_dkv 64 4"]),
-    (attention_grad, (shape(q_rows=65536, kv_rows=100, heads=1, kv_heads=1, causal=0),), ["k_attention_dq 64 4", "k_attention_dkv 64 4", "k_attention_add"]),
+    (attention, (shape(**BIG),), ["k_attention 128 1"]), (attention, (shape(**LONG),), ["k_attention 64 1"]), (attention, (shape(dim=8),), ["k_attention 64 2"]),
+    (attention, (shape(dim=72),), ["k_attention 128 2"]), (attention, (shape(q_rows=8, kv_rows=32768, sequences=8, heads=32, kv_heads=8, dim=128),), ["k_attention 128 2", "k_attention_join"]),
+    (attention, (shape(q_rows=0),), []), (attention, (shape(kv_rows=0),), ["k_attention 64 1"]), (attention, (shape(q_rows=60, kv_rows=60),), ["k_attention 64 1"]),
+    (attention, (shape(q_rows=8192, kv_rows=8192, heads=16, kv_heads=16, sequences=2),), ["k_attention 64 1"]),
+    (attention_grad, (shape(**BIG),), ["k_attention_dq 128 1", "k_attention_dkv 128 8 1"]), (attention_grad, (shape(**LONG),), ["k_attention_dq 64 1", "k_attention_dkv 64 4 1"]),
+    (attention_grad, (shape(q_rows=64, kv_rows=64, dim=128),), ["k_attention_dq 128 1", "k_attention_dkv 128 4 2"]), (attention_grad, (shape(q_rows=0),), ["k_attention_dkv 64 4 1"]),
+    (attention_grad, (shape(kv_rows=0),), ["k_attention_dq 64 1"]), (attention_grad, (shape(q_rows=0, kv_rows=0),), []),
+    (attention_grad, (shape(q_rows=8, kv_rows=32768, sequences=8, heads=32, kv_heads=8, dim=128),), ["k_attention_dq 128 2", "k_attention_add", "k_attention_dkv 128 4 1"]),
+    (attention_grad, (shape(q_rows=8192, kv_rows=8192, sequences=2, heads=32, kv_heads=8, dim=128),), ["k_attention_dq 128 1", "k_attention_dkv 128 4 2"]),
+    (attention_grad, (shape(q_rows=1, kv_rows=65536, heads=1, kv_heads=1),), ["k_attention_dq 64 2", "k_attention_add", "k_attention_dkv 64 4 1"]),
+    (attention_grad, (shape(q_rows=65536, kv_rows=100, heads=1, kv_heads=1, causal=0),), ["k_attention_dq 64 1", "k_attention_dkv 64 4 2", "k_attention_add"]),
     (rotate, ((), dict(rows=8)), ["k_rotate 1 1"]), (rotate, ((), dict(rows=8, pairs=1)), ["k_rotate 0 1"]), (rotate, ((), dict(rows=100000)), ["k_rotate 1 4"]), (rotate, ((), dict(rows=0)), []),
     (epilogue, ((), dict(m=1, n=4096, k=16384)), ["k_product_few 1 1 8 0"]), (epilogue, ((), dict(m=1, n=4096, k=16384, t=(at(6), at(6)))), ["k_product_few 1 1 8 0", "k_epilogue"]),
     (epilogue, ((), dict(m=1, n=300, k=16384)), ["k_product_few 1 1 8 0", "k_epilogue"]), (epilogue, ((), dict(m=8192, n=16384, k=4096)), ["k_product 4 2 2 4 0"]),

@@ -94,7 +94,9 @@ SHAPES = {
     "65 starts": (900, 900, 2, 1, 64, 65, ([i * (i + 1) // 5 for i in range(66)], [i * (i + 1) // 5 for i in range(66)])),
     "many starts": (3000, 3000, 1, 1, 64, 1500, (list(range(0, 3001, 2)), list(range(0, 3001, 2)))),
     "keys in parts": (4, 8192, 8, 2, 128, 2), "queries in parts": (6000, 100, 4, 2, 128, 1, None, False), "parts of starts": (9, 7000, 2, 2, 64, 3, ([1, 2, 5, 8], [100, 3000, 3001, 6900])),
-    "eight wavefronts": (4096, 4096, 8, 8, 128, 2), "half a head": (2048, 2048, 8, 2, 64, 2),
+    "eight wavefronts": (2048, 2048, 64, 64, 128), "half a head": (2048, 2048, 8, 2, 64, 2), "long": (4096, 4096, 8, 8, 128, 2),
+    "many blocks": (1400, 1400, 80, 80, 40, 7), "many blocks, wide heads": (1400, 1400, 80, 80, 104, 7), "many blocks of starts": (1400, 1500, 160, 80, 64, 7, ([0, 3, 400, 400, 800, 1000, 1300, 1399],
+                                                                                                                                                              [7, 300, 301, 301, 900, 1000, 1100, 1500]), True, 150),
 }
 
 
@@ -122,12 +124,13 @@ def test_extremes(B, ctx):
 
 @pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
 @pytest.mark.parametrize("window", [0, 70])
-def test_what_is_hidden_has_no_influence(B, ctx, bad, window):
+@pytest.mark.parametrize("heads,dim", [(4, 64), (280, 64), (280, 128)])     # (few blocks, many)
+def test_what_is_hidden_has_no_influence(B, ctx, bad, window, heads, dim):
     """Infinities and NaNs in keys, values, queries and gradients: what does not see them is as if they were zeros, what does is not finite (where all of it is bad)."""
     n, at = 400, 250
     for which in "kvq":
-        c = Case(n, n, 4, 2, 64, window=window, seed=11)
-        clean = Case(n, n, 4, 2, 64, window=window, seed=11)
+        c = Case(n, n, heads, heads // 2, dim, window=window, seed=11)
+        clean = Case(n, n, heads, heads // 2, dim, window=window, seed=11)
         getattr(c, which)[at] = bad
         getattr(clean, which)[at] = 0.0
         o, lse = c.forward(B, ctx)
@@ -156,7 +159,7 @@ def test_what_is_hidden_has_no_influence(B, ctx, bad, window):
                 assert torch.equal(got[i][~keys], want[i][~keys]), (which, i)
                 if which == "q":
                     assert not bool(got[i][keys].isfinite().any())
-    c, clean = Case(n, n, 4, 2, 64, window=window, seed=12), Case(n, n, 4, 2, 64, window=window, seed=12)
+    c, clean = Case(n, n, heads, heads // 2, dim, window=window, seed=12), Case(n, n, heads, heads // 2, dim, window=window, seed=12)
     c.do[at] = bad
     clean.do[at] = 0.0
     o, lse = c.forward(B, ctx)
