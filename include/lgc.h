@@ -371,8 +371,9 @@ uint64_t lgc_codes_stride(uint64_t cols);
 uint64_t lgc_exps_stride(uint64_t cols);
 
 /*
- * Reserves the scratch (64 MB) where lgc_layer_norm_grad, lgc_product and
- * lgc_weight_grad put partial sums, whatever their sizes.  Without it they return
+ * Reserves the scratch (64 MB) where lgc_layer_norm_grad, lgc_product,
+ * lgc_product_activate, lgc_weight_grad, lgc_attention and lgc_attention_grad put
+ * partial sums, whatever their sizes.  Without it they return
  * LGC_EINVAL and say so; the other calls need none.  May allocate; a second call
  * does nothing.  The context's max_n, max_k and max_batch do not limit these
  * calls, and none of them touches the state of the selection.

@@ -366,10 +366,10 @@ __device__ __forceinline__ void hand_over(f4 *to, const f16 (&x)[kWide]) {
 // Two teams: eight wavefronts, of which four take the first half of the block's tiles and four the second, in LDS of their own; their sums meet in LDS at the end.  It halves the chain of tiles that
 // a block goes through one after the other, with no partial results in memory, but a compute unit holds one such block.
 //
-// Bound: per 32 rows and 64 keys of a head of 128, 32 products of 33 cycles on the matrix cores, and 900 cycles of vector instructions (five an element, the exponential 8.5 cycles) beside them, which the
-// same SIMD's other wavefront can fill only in part, at a clock that falls to 1.9 GHz.  4 x 4096 tokens, causal, 32 / 8 heads of 128: 570 us, 0.96 PFLOP/s; 8 x 1 tokens after 4096: 25 us and 4.5 for the join
-// of eight parts, 5.4 TB/s of keys and values.  Taken back: two groups of rows per wavefront, one wavefront per SIMD (680 us, so 921, as the kernel then was); a SIMD's two wavefronts in turn between barriers,
-// 256 rows (565 / 575); eight wavefronts without teams (586); loads among the products (650); three tiles under way (no change).
+// Bound: by the matrix cores and the vector units (five instructions a score; an exponential is 8.5 cycles), which two wavefronts of a SIMD overlap in part: busy 51 % and 55 % of the time, LDS 27 %, at a clock
+// that power holds to 1.75 GHz of 2.4.  4 x 4096 tokens, causal, 32 / 8 heads of 128: 570 us, 0.96 PFLOP/s; 8 x 1 tokens after 4096: 25 us and 4 for the join
+// of four parts, 5.4 TB/s of keys and values.  Taken back: two groups of rows per wavefront, one wavefront per SIMD (680 us, so 921, as the kernel then was); a SIMD's two wavefronts in turn between barriers,
+// 256 rows (no gain); eight wavefronts without teams (586); loads among the products (650); three tiles under way (no change).
 template <int kDim, int kTeams>
 __global__ __launch_bounds__(256 * kTeams, kDim == 64 && kTeams == 1 ? 3 : 2) void k_attention(AttentionArgs p) {
     constexpr int kThreads = 256, kTile = 128, kSteps = kDim / 16, kWide = kDim / 32, kBytes = kTileKeys * kDim * 2, kStages = 2;
@@ -584,7 +584,7 @@ __global__ __launch_bounds__(kBlock) void k_attention_join(AttentionArgs p) {
 
 // dq, and delta for the kernel after it (in this kernel a row's o and do are needed once, by the lanes that have the row).  Blocks, tiles and teams as in the forward pass; three products a tile, which
 // is taken in two halves of 32 keys, so that scores and slopes of one fit the registers beside q and do: a half's scores are made before the join of the half before, between whose products its slopes
-// lie.  Bound as the forward pass, with 48 products and half as many vector instructions for each: 4 x 4096 tokens, causal, 32 / 8 heads of 128: 760 us, 1.08 PFLOP/s; 16384 tokens of 8 heads of 64: 390 us.
+// lie.  Bound as the forward pass (matrix cores 60 %, vector units 45 %, LDS 31 %): 4 x 4096 tokens, causal, 32 / 8 heads of 128: 760 us, 1.08 PFLOP/s; 16384 tokens of 8 heads of 64: 390 us.
 template <int kDim, int kTeams>
 __global__ __launch_bounds__(256 * kTeams, kDim == 64 && kTeams == 1 ? 3 : 2) void k_attention_dq(AttentionArgs p) {
     constexpr int kThreads = 256, kTile = 128, kSteps = kDim / 16, kWide = kDim / 32, kBytes = kTileKeys * kDim * 2, kStages = 2;
@@ -730,7 +730,7 @@ __global__ __launch_bounds__(256 * kTeams, kDim == 64 && kTeams == 1 ? 3 : 2) vo
 // the first half's join; of 32 rows for heads of 128 in teams of four, where LDS holds two such teams, or two such blocks.
 //
 // Eight wavefronts in one team have 256 keys, which read q and do half as often as two blocks of four; two teams of four share 128 keys, and each has half of the rows.
-// Bound: the products (64 of them for 32 rows and 64 keys of a head of 128, 54 % of the time on the matrix cores) and, beside them, LDS, which gives 16 reads of 1 KB for every eight products.
+// Bound: matrix cores 50 % of the time, vector units 33 %, LDS 39 % (24 reads of 1 KB and 32 of 512 bytes for 32 products), waits for LDS between them, one block per compute unit, at 1.73 GHz.
 // 4 x 4096 tokens, causal, 32 / 8 heads of 128: 1130 us, 0.97 PFLOP/s; 16384 tokens of 8 heads of 64: 590 us.
 template <int kDim, int kWaves, int kTeams>
 __global__ __launch_bounds__(64 * kWaves * kTeams, kDim == 64 && kTeams == 1 ? 3 : 2) void k_attention_dkv(AttentionArgs p) {

@@ -220,7 +220,7 @@ __global__ __launch_bounds__(64 * kWavesM * kWavesN) void k_product(ProductArgs 
     meet();   // nothing may arrive any more where the rows go
 
     // With an epilogue, 32 rows of 64 columns at a time go through LDS in fp32, each wavefront's for itself, and a lane takes eight columns of a row on from there, whose residual is on its
-    // way by then.  Exponents of 8-bit results are found before, from the registers: two wavefronts have the 128 columns that share one.  8192 x 16384 x 4096 with GELU to bf16 576 us, of which the
+    // way by then.  Exponents of 8-bit results are found before, from the registers: two wavefronts have the 128 columns that share one.  8192 x 16384 x 4096 with GELU to bf16 549 us, of which the
     // non-linearity takes 68 (16 vector instructions an element, with nothing to multiply meanwhile: the compute unit holds one block; two of small tiles 603).
     if constexpr (std::is_same_v<E, Epilogue>) {
         static_assert(kSideN == 2 && sizeof(f4) * kAll * 32 * 17 + kAll * kWaveM * 4 <= 2 * kPlace, "room");
