@@ -700,25 +700,27 @@ class AttentionShape:
             _refuse(f"lengths must be contiguous with {sequences} elements")
         self._starts, self._lengths = (q_starts, kv_starts), kv_lengths
         self._heads, self._kv_heads, self._dim = heads, kv_heads, dim
-        self._c = _AttentionShape(0, 0, sequences, _ptr(q_starts, torch.int32), _ptr(kv_starts, torch.int32), heads, kv_heads, dim,
+        self._made = None, _AttentionShape(0, 0, sequences, _ptr(q_starts, torch.int32), _ptr(kv_starts, torch.int32), heads, kv_heads, dim,
                                   scale if scale is not None else max(1, dim) ** -0.5, causal, window, _ptr(kv_lengths, torch.int32))
-        self._at = C.addressof(self._c)
 
-    def _rows(self, q: torch.Tensor, k: torch.Tensor) -> int:
-        """The structure's address, with the rows that a call's matrices have."""
-        c = self._c
-        if self._starts[0] is not None:   # (a tensor's memory may have been exchanged since it was looked at)
-            c.q_starts, c.kv_starts = self._starts[0].data_ptr(), self._starts[1].data_ptr()
-        if self._lengths is not None:
-            c.kv_lengths = self._lengths.data_ptr()
-        c.q_rows, c.kv_rows = q.shape[0], k.shape[0]
-        return self._at
+    def _of(self, q: torch.Tensor, k: torch.Tensor) -> _AttentionShape:
+        """The structure with the rows that a call's matrices have: another one where they are others, as a call of another thread may be under way with it."""
+        starts, of_keys = self._starts
+        lengths = self._lengths
+        at = (None if starts is None else starts.data_ptr(), None if of_keys is None else of_keys.data_ptr(), None if lengths is None else lengths.data_ptr(), q.shape[0], k.shape[0])
+        was, c = self._made
+        if at != was:   # (a tensor's memory may have been exchanged, too, since it was looked at)
+            c = _AttentionShape.from_buffer_copy(c)
+            c.q_starts, c.kv_starts, c.kv_lengths, c.q_rows, c.kv_rows = at
+            self._made = at, c
+        return c
 
 
 def lgc_attention(ctx: Context, shape: AttentionShape, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, o: torch.Tensor, lse: Optional[torch.Tensor] = None) -> None:
     """o [q_rows][heads * dim], lse [q_rows][heads] <- attention of q over k, v [kv_rows][kv_heads * dim], all but lse in bfloat16."""
     rows, keys, wide, narrow = q.shape[0], k.shape[0], shape._heads * shape._dim, shape._kv_heads * shape._dim
-    _check(lib().lgc_attention(ctx.h, shape._rows(q, k), *_matrix(q, rows, wide, _BF16, "q"), *_matrix(k, keys, narrow, _BF16, "k"), *_matrix(v, keys, narrow, _BF16, "v"),
+    c = shape._of(q, k)
+    _check(lib().lgc_attention(ctx.h, C.addressof(c), *_matrix(q, rows, wide, _BF16, "q"), *_matrix(k, keys, narrow, _BF16, "k"), *_matrix(v, keys, narrow, _BF16, "v"),
                                *_matrix(o, rows, wide, _BF16, "o"), _vector(lse, rows * shape._heads, "lse"), _stream()), ctx.h)
 
 
@@ -728,5 +730,6 @@ def lgc_attention_grad(ctx: Context, shape: AttentionShape, do: torch.Tensor, q:
     rows, keys, wide, narrow = q.shape[0], k.shape[0], shape._heads * shape._dim, shape._kv_heads * shape._dim
     of_q = lambda t, what: _matrix(t, rows, wide, _BF16, what)  # noqa: E731
     of_k = lambda t, what: _matrix(t, keys, narrow, _BF16, what)  # noqa: E731
-    _check(lib().lgc_attention_grad(ctx.h, shape._rows(q, k), *of_q(do, "do"), *of_q(q, "q"), *of_k(k, "k"), *of_k(v, "v"), *of_q(o, "o"), _vector(lse, rows * shape._heads, "lse"),
+    c = shape._of(q, k)
+    _check(lib().lgc_attention_grad(ctx.h, C.addressof(c), *of_q(do, "do"), *of_q(q, "q"), *of_k(k, "k"), *of_k(v, "v"), *of_q(o, "o"), _vector(lse, rows * shape._heads, "lse"),
                                     *of_q(dq, "dq"), *of_k(dk, "dk"), *of_k(dv, "dv"), _vector(delta, rows * shape._heads, "delta"), _stream()), ctx.h)

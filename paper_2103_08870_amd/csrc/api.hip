@@ -1613,6 +1613,9 @@ extern "C" lgc_status lgc_product_activate(lgc_ctx *ctx, const uint8_t *a_codes,
     if (m) c.blocks("a", a_codes, a_exps).blocks("b", b_codes, b_exps).maybe("residual", residual, type, n, ld_residual).maybe("z", z, type, n, ld)
         .maybe_blocks("t", t_codes, t_exps).maybe_blocks("z", z_codes, z_exps)
         .need(!residual || z, "a residual, and no z to which it goes")
+        .need(!residual || residual != z || ld_residual == ld || m == 1, "the residual lies where z does, with rows another distance apart")
+        .need((!t_codes || (t_codes != a_codes && t_codes != b_codes && t_codes != z_codes)) && (!z_codes || (z_codes != a_codes && z_codes != b_codes)),
+              "t or z in 8 bits lies where an argument or the other does")
         .need(!residual || !(z_codes || z_exps), "z in 8 bits is not made with a residual");
     c.reserved("lgc_product_activate");
     return launch(c, [&] {

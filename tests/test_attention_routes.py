@@ -86,6 +86,8 @@ REFUSED = [
     (epilogue, ((), dict(act=4)), "non-linearity"), (epilogue, ((), dict(act=-1)), "non-linearity"), (epilogue, ((), dict(type=5)), "type"), (epilogue, ((), dict(n=0)), "n ="),
     (epilogue, ((), dict(k=(1 << 20) + 1)), "k ="), (epilogue, ((), dict(m=1 << 31)), "m ="), (epilogue, ((), dict(ld=299)), "apart"),
     (epilogue, ((), dict(t=(at(6), None))), "codes"), (epilogue, ((), dict(z8=(p((1 << 40) + 8), at(6)))), "codes"), (epilogue, ((), dict(residual=at(7), z=None, t=(at(6), at(6)))), "residual"),
+    (epilogue, ((), dict(residual=at(5), ld=308)), "distance"), (epilogue, ((), dict(t=(at(1), at(6)))), "lies where"), (epilogue, ((), dict(t=(at(6), at(6)), z8=(at(6), at(7)))), "lies where"),
+    (epilogue, ((), dict(z8=(at(2), at(7)))), "lies where"),
     (epilogue, ((), dict(residual=at(7), z8=(at(6), at(6)))), "residual"), (epilogue, ((), dict(residual=p((1 << 40) + 1))), "aligned"),
 ]
 

@@ -1,6 +1,7 @@
 """Attention and its gradient against their definitions in 64 bits, within bounds that follow from where numbers are rounded (attention_reference.py); gradients against differences; what is hidden
 without influence, whatever it is; rows of no sequence let be; strides, far places, streams and graphs."""
 import math
+import threading
 
 import pytest
 import torch
@@ -309,6 +310,36 @@ def test_on_another_stream_and_another_context(B, ctx):
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) and torch.equal(a, m) for a, b, m in zip(want, got, mine))
     other.close()
+
+
+def test_one_shape_in_two_threads(B, ctx):
+    """The structure of heads and sequences serves calls of other lengths at once, each on a context and stream of its own."""
+    cases = [Case(n, n, 2, 2, 64, seed=60 + n) for n in (100, 900)]
+    shape = cases[0].shape(B)
+    want = [c.forward(B, ctx)[0] for c in cases]
+    got, wrong = [torch.full_like(c.q, KEEP) for c in cases], []
+    contexts = [B.Context(1, 1, 1) for _ in cases]
+    for c in contexts:
+        B.lgc_reserve_training(c)
+    torch.cuda.synchronize()
+
+    def work(i):
+        try:
+            with torch.cuda.stream(torch.cuda.Stream()):
+                for _ in range(200):
+                    B.lgc_attention(contexts[i], shape, cases[i].q, cases[i].k, cases[i].v, got[i])
+        except Exception as e:  # noqa: BLE001
+            wrong.append(e)
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert not wrong and all(torch.equal(a, b) for a, b in zip(got, want))
+    for c in contexts:
+        c.close()
 
 
 def test_in_graphs(B, ctx):

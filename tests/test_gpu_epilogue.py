@@ -202,14 +202,14 @@ def test_strides_streams_graphs_and_bits(B, ctx):
 
 def test_the_binding_s_checks(B, ctx):
     a, b, _, _, bias = made(B, ctx, 10, 256, 128, 4)
-    z, r = torch.empty((10, 256), device="cuda"), torch.empty((10, 256), device="cuda")
+    z, r, same = torch.empty((10, 256), device="cuda"), torch.empty((10, 256), device="cuda"), B.Blocks(10, 256)
     for call in (lambda: B.lgc_product_activate(ctx, a, b, bias, "tanh", z=z), lambda: B.lgc_product_activate(ctx, a, b, bias, z=z[:, :200]), lambda: B.lgc_product_activate(ctx, a, a, bias, z=z),
                  lambda: B.lgc_product_activate(ctx, a, b, bias[:100], z=z), lambda: B.lgc_product_activate(ctx, a, b, bias, residual=r.to(torch.bfloat16), z=z),
                  lambda: B.lgc_product_activate(ctx, a, b, bias, z=z, t_blocks=B.Blocks(10, 128)), lambda: B.lgc_product_activate(ctx, a, b, bias, residual=r[:5], z=z)):
         with pytest.raises(ValueError):
             call()
     for call in (lambda: B.lgc_product_activate(ctx, a, b, bias, residual=r.to(torch.bfloat16), t_blocks=B.Blocks(10, 256)),
-                 lambda: B.lgc_product_activate(ctx, a, b, bias, residual=r, z=z, z_blocks=B.Blocks(10, 256))):
+                 lambda: B.lgc_product_activate(ctx, a, b, bias, residual=r, z=z, z_blocks=B.Blocks(10, 256)), lambda: B.lgc_product_activate(ctx, a, b, bias, t_blocks=same, z_blocks=same)):
         with pytest.raises(B.LgcError):
             call()
     B.lgc_product_activate(ctx, a, b, bias)        # nothing is wanted

@@ -112,7 +112,7 @@ def far(got, want):
 
 
 @pytest.mark.parametrize("rows,width,heads,kv_heads,dim,hidden,how", [(300, 256, 4, 2, 64, 640, dict(sequences=2)), (257, 200, 6, 2, 40, 333, dict(act="silu", window=60)),
-                                                                      (1, 128, 2, 1, 64, 512, {}), (512, 512, 4, 4, 128, 1024, dict(act="relu"))])
+                                                                      (70, 131, 3, 1, 8, 77, {}), (1, 128, 2, 1, 64, 512, {}), (512, 512, 4, 4, 128, 1024, dict(act="relu"))])
 def test_layer(T, rows, width, heads, kv_heads, dim, hidden, how):
     layer = made(T, rows, width, heads, kv_heads, dim, hidden, seed=3, **how)
     x, dy = rand((rows, width), 1).to(torch.bfloat16).cuda(), rand((rows, width), 2, 1e-3).to(torch.bfloat16).cuda()
