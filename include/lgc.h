@@ -518,7 +518,7 @@ lgc_status lgc_rotate(lgc_ctx *ctx, const void *x, lgc_type type, uint64_t rows,
  *
  * Limits: dim a multiple of 8, 8 to 128; heads a multiple of kv_heads, heads * dim at
  * most 2^20; sequences 1 to 2^20, sequences * kv_heads at most 2^22; q_rows * heads and kv_rows * kv_heads below 2^29;
- * scale > 0 and finite.  Matrices are bf16, 16-byte aligned, rows a multiple of
+ * scale 2^-100 to 2^100.  Matrices are bf16, 16-byte aligned, rows a multiple of
  * 8 elements apart, 2^24 at most.  q_rows == 0 and kv_rows == 0 are valid.
  */
 typedef struct {

@@ -1680,7 +1680,7 @@ void check_attention(Check &c, const lgc_attention_shape *s) {
     c.need(sequences >= 1 && sequences <= kMostCols && sequences * kv_heads <= 4 * kMostCols, "%llu sequences: none, above 2^20, or with their key heads above 2^22", sequences);
     c.need(q_rows < (1ull << 29) && q_rows * heads < (1ull << 29), "q_rows * heads = %llu * %llu not below 2^29", q_rows, heads);
     c.need(kv_rows < (1ull << 29) && kv_rows * kv_heads < (1ull << 29), "kv_rows * kv_heads = %llu * %llu not below 2^29", kv_rows, kv_heads);
-    c.need(s->scale > 0.f && s->scale < INFINITY, "scale = %g", (double)s->scale);
+    c.need(s->scale >= 0x1p-100f && s->scale <= 0x1p100f, "scale = %g outside [2^-100, 2^100]", (double)s->scale);
     c.need(!s->q_starts == !s->kv_starts, "one of q_starts and kv_starts is NULL");
     c.need(aligned(s->q_starts, 4) && aligned(s->kv_starts, 4) && aligned(s->kv_lengths, 4), "starts or lengths are not 4-byte aligned");
     if (c.status != LGC_OK) return;   // (sequences are not none)

@@ -448,16 +448,18 @@ __global__ __launch_bounds__(256 * kTeams, kDim == 64 && kTeams == 1 ? 3 : 2) vo
                 for (int e = 0; e < 16; ++e) o[d][e] *= by;
         }
         const float off = most == -INFINITY ? 0.f : most * c;
+        float of_tile = 0.f;   // added up by itself: a row may have a million keys, whose sum would lose what each adds
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
 #pragma unroll
             for (int e = 8 * t; e < 8 * t + 8; ++e) {
                 const float x = __builtin_amdgcn_exp2f(fmaf(s[e / 16][e % 16], c, -off));
                 s[e / 16][e % 16] = x;
-                sum += x;
+                of_tile += x;
             }
             prob[t] = eight_of(s[t / 2], t & 1);   // probabilities meet the values in bf16: 2^-9 of each, as the values have them themselves
         }
+        sum += of_tile;
     };
     auto join = [&](uint32_t tile) {
         const uint32_t at = anew(lane_columns_at);

@@ -66,7 +66,7 @@ REFUSED = [
     (attention, (shape(heads=1 << 14, kv_heads=1, dim=128),), "2^20"), (attention, (shape(sequences=0),), "sequences"), (attention, (shape(sequences=(1 << 20) + 1),), "sequences"),
     (attention, (shape(q_rows=1 << 20, kv_rows=1 << 20, sequences=1 << 20, heads=8, kv_heads=8, dim=8),), "sequences"),
     (attention, (shape(q_rows=1 << 28),), "q_rows"), (attention, (shape(q_rows=1 << 40),), "q_rows"), (attention, (shape(kv_rows=1 << 29),), "kv_rows"),
-    (attention, (shape(scale=0.0),), "scale"), (attention, (shape(scale=-1.0),), "scale"), (attention, (shape(scale=math.nan),), "scale"), (attention, (shape(scale=math.inf),), "scale"),
+    (attention, (shape(scale=0.0),), "scale"), (attention, (shape(scale=-1.0),), "scale"), (attention, (shape(scale=math.nan),), "scale"), (attention, (shape(scale=math.inf),), "scale"), (attention, (shape(scale=1e-38),), "scale"),
     (attention, (shape(q_starts=at(11).value),), "starts"), (attention, (shape(kv_starts=at(11).value),), "starts"),
     (attention, (shape(q_starts=ODD.value, kv_starts=at(11).value),), "starts"), (attention, (shape(sequences=3),), "equal"),
     (attention, (shape(kv_lengths=ODD.value),), "lengths"), (attention_grad, (shape(kv_lengths=at(11).value),), "cache"),

@@ -123,6 +123,22 @@ def test_extremes(B, ctx):
     c.check(B, ctx)
 
 
+def test_a_million_keys(B, ctx):
+    """Rows enough that nothing is split: a lane adds up 2^14 tiles, whose rounding is at most U / 2 of the whole for each, and within a tile 32 terms."""
+    keys, rows = 1 << 20, 1 << 17
+    q, k = torch.ones((rows, 8), dtype=BF16, device="cuda"), torch.full((keys, 8), 0.0433, dtype=BF16, device="cuda")
+    k[0] = 0.0                                                  # the maximum stays here: the others are 2^0.5 of it
+    v = torch.ones_like(k)
+    o, lse = torch.full_like(q, KEEP), torch.full((rows, 1), KEEP, device="cuda")
+    B.lgc_attention(ctx, B.AttentionShape(1, 1, 8, scale=1.0, causal=False), q, k, v, o, lse)
+    want = math.log1p((keys - 1) * math.exp(8 * float(k[1, 0])))
+    off = (2 ** 14 / 2 + 32 + 16) * ref.U
+    assert float((lse.double() - want).abs().max()) <= off
+    # p meets the values in bf16: all of them with one and the same rounding; the products' sums add 16 keys at a time
+    p, rounded = math.exp(8 * float(k[1, 0])), float(torch.tensor(math.exp(8 * float(k[1, 0]))).to(BF16))
+    assert float((o.double() - (1 + (keys - 1) * rounded) / (1 + (keys - 1) * p)).abs().max()) <= off + 2 ** 16 / 2 * ref.U + ref.H
+
+
 @pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
 @pytest.mark.parametrize("window", [0, 70])
 @pytest.mark.parametrize("heads,dim", [(4, 64), (280, 64), (280, 128)])     # (few blocks, many)
