@@ -137,6 +137,9 @@ __device__ __forceinline__ Range range_of(const AttentionArgs &p, const Place &a
     return x;
 }
 
+// Kernels are made for heads of up to 64, 96 and 128 columns (kDim); a row in LDS has room for 64 or 128.  (Heads of 72 to 96 as 128, and as 96: 4 x 4096 tokens of 32 / 8 heads of 96 553 us, so 498,
+// backward 1834, so 1577; 2048 tokens of 80 50 and 45, backward 193 and 172.)
+constexpr int pitch_of(int dim) { return dim <= 64 ? 64 : 128; }
 // A tile of rows of kDim elements in LDS.  A row's pieces of 16 bytes are exchanged by its number, so that 16 neighbouring rows' pieces of one column (a plain read) and four rows' four
 // neighbouring pieces (a turned one) meet all 64 banks.
 template <int kDim>
@@ -301,12 +304,12 @@ __device__ __forceinline__ bf8 piece_of(const uint16_t *row, uint32_t from, uint
 }
 // Stores a wavefront's 32 rows of results, of which a lane has columns 32 d + 8 c + 4 g + 0 .. 3 of row lane % 32, times `by`: through LDS (`room`, of the wavefront's own), in whole lines.
 // where(row): the row's place, or null.
-template <int kDim, typename F>
-__device__ __forceinline__ void store_rows(uint8_t *room, const f16 (&x)[kDim / 32], float by, uint32_t dim, F &&where) {
+template <int kDim, int kWide, typename F>
+__device__ __forceinline__ void store_rows(uint8_t *room, const f16 (&x)[kWide], float by, uint32_t dim, F &&where) {
     constexpr int kPieces = kDim / 8, kPass = 64 / kPieces;
     const uint32_t lane = threadIdx.x & 63, r = lane & 31, g = lane >> 5;
 #pragma unroll
-    for (int d = 0; d < kDim / 32; ++d)
+    for (int d = 0; d < kWide; ++d)
 #pragma unroll
         for (int c = 0; c < 4; ++c)
             *(u2 *)(room + r * (2 * kDim) + ((4 * d + c) ^ (r & (kPieces - 1))) * 16 + 8 * g) = u2{bf16_pair(x[d][4 * c] * by, x[d][4 * c + 1] * by), bf16_pair(x[d][4 * c + 2] * by, x[d][4 * c + 3] * by)};
@@ -372,7 +375,7 @@ __device__ __forceinline__ void hand_over(f4 *to, const f16 (&x)[kWide]) {
 // 256 rows (no gain); eight wavefronts without teams (586); loads among the products (650); three tiles under way (no change).
 template <int kDim, int kTeams>
 __global__ __launch_bounds__(256 * kTeams, kDim == 64 && kTeams == 1 ? 3 : 2) void k_attention(AttentionArgs p) {
-    constexpr int kThreads = 256, kTile = 128, kSteps = kDim / 16, kWide = kDim / 32, kBytes = kTileKeys * kDim * 2, kStages = 2;
+    constexpr int kThreads = 256, kTile = 128, kSteps = kDim / 16, kWide = kDim / 32, kPitch = pitch_of(kDim), kBytes = kTileKeys * kPitch * 2, kStages = 2;
     __shared__ __align__(16) uint8_t all_lds[kTeams * 2 * kStages * kBytes];
     const Place at = place_of(p, false, kTile);
     if (at.none) return;
@@ -387,10 +390,10 @@ __global__ __launch_bounds__(256 * kTeams, kDim == 64 && kTeams == 1 ? 3 : 2) vo
     const uint32_t turns = team_of<kTeams>(team, from, to);
 
     const uint16_t *const k = p.k + (uint64_t)at.k0 * p.ld_k + at.head * p.dim, *const v = p.v + (uint64_t)at.k0 * p.ld_v + at.head * p.dim;
-    typedef Loader<kDim, kTileKeys, kThreads> Tiles;
+    typedef Loader<kPitch, kTileKeys, kThreads> Tiles;
     const Tiles of_keys(k, p.ld_k, at.lk, p.dim), of_values(v, p.ld_v, at.lk, p.dim);
     const uint16_t *next_keys = of_keys.tile(from), *next_values = of_values.tile(from);
-    const uint32_t keys = address(lds), values = keys + kStages * kBytes, lane_rows_at = lane_rows<kDim>(), lane_columns_at = lane_columns<kDim>();
+    const uint32_t keys = address(lds), values = keys + kStages * kBytes, lane_rows_at = lane_rows<kPitch>(), lane_columns_at = lane_columns<kPitch>();
     auto load_keys = [&](uint32_t tile) {
         const uint32_t place = keys + ((tile - from) & 1) * kBytes;
         if (tile < min(to, of_keys.whole))
@@ -424,7 +427,7 @@ __global__ __launch_bounds__(256 * kTeams, kDim == 64 && kTeams == 1 ? 3 : 2) vo
 #pragma unroll
         for (int step = 0; step < kSteps; ++step)
 #pragma unroll
-            for (int half = 0; half < 2; ++half) ahead[half] = product(rows_of<kDim>(tile, at, half, step), q[step], ahead[half]);
+            for (int half = 0; half < 2; ++half) ahead[half] = product(rows_of<kPitch>(tile, at, half, step), q[step], ahead[half]);
     };
     auto probabilities = [&](int key0) {
         if (!range.all_of(key0))
@@ -466,7 +469,7 @@ __global__ __launch_bounds__(256 * kTeams, kDim == 64 && kTeams == 1 ? 3 : 2) vo
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
-            for (int d = 0; d < kWide; ++d) o[d] = product(columns_of<kDim>(tile, at, t, d), prob[t], o[d]);
+            for (int d = 0; d < kWide; ++d) o[d] = product(columns_of<kPitch>(tile, at, t, d), prob[t], o[d]);
     };
 
     bool bad = false;
@@ -526,7 +529,7 @@ __global__ __launch_bounds__(256 * kTeams, kDim == 64 && kTeams == 1 ? 3 : 2) vo
     const float lse = sum == 0.f ? -INFINITY : (most * c + __log2f(sum)) * kLn2;
     const uint64_t line = (uint64_t)(at.q0 + token) * p.heads + head, all = (uint64_t)p.q_rows * p.heads;
     if (p.parts == 1)
-        store_rows<kDim>(all_lds + wave * (kTeams * 64 * kDim), o, by, p.dim, [&](uint32_t i) {   // (of two teams: where its own were read from)
+        store_rows<kPitch>(all_lds + wave * (kTeams == 1 ? 64 * kPitch : 128 * kDim), o, by, p.dim, [&](uint32_t i) {   // (of two teams: where its own were read from)
             const uint32_t row = row0 + wave * 32 + i, t = token_of(row);
             return row < rows ? p.out + (uint64_t)(at.q0 + t) * p.ld_out + (at.head * p.group.by + row - t * p.group.by) * p.dim : nullptr;
         });
@@ -589,7 +592,7 @@ __global__ __launch_bounds__(kBlock) void k_attention_join(AttentionArgs p) {
 // lie.  Bound as the forward pass (matrix cores 60 %, vector units 45 %, LDS 31 %): 4 x 4096 tokens, causal, 32 / 8 heads of 128: 760 us, 1.08 PFLOP/s; 16384 tokens of 8 heads of 64: 390 us.
 template <int kDim, int kTeams>
 __global__ __launch_bounds__(256 * kTeams, kDim == 64 && kTeams == 1 ? 3 : 2) void k_attention_dq(AttentionArgs p) {
-    constexpr int kThreads = 256, kTile = 128, kSteps = kDim / 16, kWide = kDim / 32, kBytes = kTileKeys * kDim * 2, kStages = 2;
+    constexpr int kThreads = 256, kTile = 128, kSteps = kDim / 16, kWide = kDim / 32, kPitch = pitch_of(kDim), kBytes = kTileKeys * kPitch * 2, kStages = 2;
     __shared__ __align__(16) uint8_t all_lds[kTeams * 2 * kStages * kBytes];
     const Place at = place_of(p, false, kTile);
     if (at.none) return;
@@ -624,9 +627,9 @@ __global__ __launch_bounds__(256 * kTeams, kDim == 64 && kTeams == 1 ? 3 : 2) vo
     const uint32_t turns = team_of<kTeams>(team, from, to);
 
     const uint16_t *const k = p.k + (uint64_t)at.k0 * p.ld_k + at.head * p.dim, *const v = p.v + (uint64_t)at.k0 * p.ld_v + at.head * p.dim;
-    typedef Loader<kDim, kTileKeys, kThreads> Tiles;
+    typedef Loader<kPitch, kTileKeys, kThreads> Tiles;
     const Tiles of_keys(k, p.ld_k, at.lk, p.dim), of_values(v, p.ld_v, at.lk, p.dim);
-    const uint32_t keys = address(lds), values = keys + kStages * kBytes, lane_rows_at = lane_rows<kDim>(), lane_columns_at = lane_columns<kDim>();
+    const uint32_t keys = address(lds), values = keys + kStages * kBytes, lane_rows_at = lane_rows<kPitch>(), lane_columns_at = lane_columns<kPitch>();
     const uint16_t *next_keys = of_keys.tile(from), *next_values = of_values.tile(from);
     auto load = [&](uint32_t tile, uint32_t stage) {
         if (tile < min(to, of_keys.whole)) {
@@ -651,8 +654,8 @@ __global__ __launch_bounds__(256 * kTeams, kDim == 64 && kTeams == 1 ? 3 : 2) vo
         for (int e = 0; e < 16; ++e) dp[e] = -delta;
 #pragma unroll
         for (int step = 0; step < kSteps; ++step) {
-            s = product(rows_of<kDim>(keys + stage * kBytes, at, half, step), q[step], s);
-            dp = product(rows_of<kDim>(keys + stage * kBytes, at, half + kStages * kTileKeys / 32, step), grad[step], dp);   // (the values, as far behind the keys)
+            s = product(rows_of<kPitch>(keys + stage * kBytes, at, half, step), q[step], s);
+            dp = product(rows_of<kPitch>(keys + stage * kBytes, at, half + kStages * kTileKeys / 32, step), grad[step], dp);   // (the values, as far behind the keys)
         }
     };
     auto slopes = [&](int tile_key, int half) {
@@ -674,7 +677,7 @@ __global__ __launch_bounds__(256 * kTeams, kDim == 64 && kTeams == 1 ? 3 : 2) vo
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
-            for (int d = 0; d < kWide; ++d) dq[d] = product(columns_of<kDim>(keys + stage * kBytes, at, 2 * half + t, d), ds[t], dq[d]);
+            for (int d = 0; d < kWide; ++d) dq[d] = product(columns_of<kPitch>(keys + stage * kBytes, at, 2 * half + t, d), ds[t], dq[d]);
     };
 
     bool bad = false;
@@ -719,7 +722,7 @@ __global__ __launch_bounds__(256 * kTeams, kDim == 64 && kTeams == 1 ? 3 : 2) vo
             for (int e = 0; e < 16; ++e) dq[d][e] += theirs[(4 * d + e / 4) * 64][e % 4];
     }
     if (p.parts == 1)
-        store_rows<kDim>(all_lds + wave * (kTeams * 64 * kDim), dq, p.scale, p.dim, [&](uint32_t i) {
+        store_rows<kPitch>(all_lds + wave * (kTeams == 1 ? 64 * kPitch : 128 * kDim), dq, p.scale, p.dim, [&](uint32_t i) {
             const uint32_t row = row0 + wave * 32 + i, t = quotient(min(row, rows - 1), p.group);
             return row < rows ? p.out + (uint64_t)(at.q0 + t) * p.ld_out + (at.head * p.group.by + row - t * p.group.by) * p.dim : nullptr;
         });
@@ -736,8 +739,8 @@ __global__ __launch_bounds__(256 * kTeams, kDim == 64 && kTeams == 1 ? 3 : 2) vo
 // 4 x 4096 tokens, causal, 32 / 8 heads of 128: 1130 us, 0.97 PFLOP/s; 16384 tokens of 8 heads of 64: 590 us.
 template <int kDim, int kWaves, int kTeams>
 __global__ __launch_bounds__(64 * kWaves * kTeams, kDim == 64 && kTeams == 1 ? 3 : 2) void k_attention_dkv(AttentionArgs p) {
-    constexpr int kThreads = 64 * kWaves, kTile = 32 * kWaves, kSteps = kDim / 16, kWide = kDim / 32;
-    constexpr int kRows = kDim == 64 || kWaves == 8 ? 64 : 32, kHalves = kRows / 32, kBytes = kRows * kDim * 2, kStats = 2 * kRows, kStages = 2, kValues = kTile * kDim * 2;
+    constexpr int kThreads = 64 * kWaves, kTile = 32 * kWaves, kSteps = kDim / 16, kWide = kDim / 32, kPitch = pitch_of(kDim);
+    constexpr int kRows = kDim == 64 || kWaves == 8 ? 64 : 32, kHalves = kRows / 32, kBytes = kRows * kPitch * 2, kStats = 2 * kRows, kStages = 2, kValues = kTile * kPitch * 2;
     __shared__ __align__(16) uint8_t all_lds[kTeams * kStages * (2 * kBytes + kStats * 4) + kValues];
     const Place at = place_of(p, true, kTile);
     if (at.none || at.tile * kTile >= at.lk) return;
@@ -773,11 +776,11 @@ __global__ __launch_bounds__(64 * kWaves * kTeams, kDim == 64 && kTeams == 1 ? 3
     const uint32_t turns = team_of<kTeams>(team, from, to);
     const uint64_t head0 = (uint64_t)at.head * p.group.by;
     const uint16_t *const q = p.q + at.q0 * p.ld_q + head0 * p.dim, *const grad = p.grad + at.q0 * p.ld_grad + head0 * p.dim;
-    const uint32_t queries = address(lds), grads = queries + kStages * kBytes, values = address(all_lds) + kTeams * 2 * kStages * kBytes, lane_rows_at = lane_rows<kDim>(), lane_columns_at = lane_columns<kDim>();
+    const uint32_t queries = address(lds), grads = queries + kStages * kBytes, values = address(all_lds) + kTeams * 2 * kStages * kBytes, lane_rows_at = lane_rows<kPitch>(), lane_columns_at = lane_columns<kPitch>();
     float *const stats = (float *)(all_lds + kTeams * 2 * kStages * kBytes + kValues) + team * (kStages * kStats);
     // What comes next: tile `number` of a head of the group.  lse (in powers of two) and -delta of its rows come by one of the first wavefronts' lanes, and go to LDS when they have arrived.
     uint32_t head = tiles ? from / tiles : 0u, number = tile0 + from - head * tiles;
-    Loader<kDim, kRows, kThreads> of_queries(q + head * p.dim, p.ld_q, at.lq, p.dim), of_grads(grad + head * p.dim, p.ld_grad, at.lq, p.dim);
+    Loader<kPitch, kRows, kThreads> of_queries(q + head * p.dim, p.ld_q, at.lq, p.dim), of_grads(grad + head * p.dim, p.ld_grad, at.lq, p.dim);
     const uint16_t *next_queries = of_queries.tile(number), *next_grads = of_grads.tile(number);
     of_queries.pad(lds, 2 * kStages);
     float stat = 0.f;
@@ -822,8 +825,8 @@ __global__ __launch_bounds__(64 * kWaves * kTeams, kDim == 64 && kTeams == 1 ? 3
         }
 #pragma unroll
         for (int step = 0; step < kSteps; ++step) {
-            s = product(rows_of<kDim>(queries + stage * kBytes, at, half, step), k[step], s);
-            dp = product(rows_of<kDim>(queries + stage * kBytes, at, half + kStages * kRows / 32, step), rows_of<kDim>(values + wave * (64 * kDim), at, 0, step), dp);   // (the gradients, as far behind the queries)
+            s = product(rows_of<kPitch>(queries + stage * kBytes, at, half, step), k[step], s);
+            dp = product(rows_of<kPitch>(queries + stage * kBytes, at, half + kStages * kRows / 32, step), rows_of<kPitch>(values + wave * (64 * kPitch), at, 0, step), dp);   // (the gradients, as far behind the queries)
         }
     };
     auto slopes = [&](uint32_t stage, int half, uint32_t first) {
@@ -853,15 +856,15 @@ __global__ __launch_bounds__(64 * kWaves * kTeams, kDim == 64 && kTeams == 1 ? 3
         for (int t = 0; t < 2; ++t)
 #pragma unroll
             for (int d = 0; d < kWide; ++d) {
-                dv[d] = product(columns_of<kDim>(queries + stage * kBytes, at, 2 * half + t + kStages * kRows / 16, d), prob[t], dv[d]);
-                dk[d] = product(columns_of<kDim>(queries + stage * kBytes, at, 2 * half + t, d), ds[t], dk[d]);
+                dv[d] = product(columns_of<kPitch>(queries + stage * kBytes, at, 2 * half + t + kStages * kRows / 16, d), prob[t], dv[d]);
+                dk[d] = product(columns_of<kPitch>(queries + stage * kBytes, at, 2 * half + t, d), ds[t], dk[d]);
             }
     };
 
     uint32_t now = number;   // the tile that is worked on
     bool bad = false;
     if (from < to) {
-        if (team == 0) Loader<kDim, kTile, kThreads>(p.v + (uint64_t)at.k0 * p.ld_v + at.head * p.dim, p.ld_v, at.lk, p.dim).load_any(values, at.tile);
+        if (team == 0) Loader<kPitch, kTile, kThreads>(p.v + (uint64_t)at.k0 * p.ld_v + at.head * p.dim, p.ld_v, at.lk, p.dim).load_any(values, at.tile);
         load(0);
     }
     for (uint32_t it = from, stage = 0; it < to; ++it, stage ^= 1) {
@@ -913,8 +916,8 @@ __global__ __launch_bounds__(64 * kWaves * kTeams, kDim == 64 && kTeams == 1 ? 3
     }
     if (p.parts == 1) {
         auto place = [&](uint16_t *base, uint64_t ld, uint32_t i) { return wave_key + i < at.lk ? base + (uint64_t)(at.k0 + wave_key + i) * ld + at.head * p.dim : nullptr; };
-        store_rows<kDim>(all_lds + wave * (kTeams * 64 * kDim), dk, p.scale, p.dim, [&](uint32_t i) { return place(p.dk, p.ld_dk, i); });
-        store_rows<kDim>(all_lds + wave * (kTeams * 64 * kDim), dv, 1.f, p.dim, [&](uint32_t i) { return place(p.dv, p.ld_dv, i); });
+        store_rows<kPitch>(all_lds + wave * (kTeams == 1 ? 64 * kPitch : 128 * kDim), dk, p.scale, p.dim, [&](uint32_t i) { return place(p.dk, p.ld_dk, i); });
+        store_rows<kPitch>(all_lds + wave * (kTeams == 1 ? 64 * kPitch : 128 * kDim), dv, 1.f, p.dim, [&](uint32_t i) { return place(p.dv, p.ld_dv, i); });
     } else if (key < at.lk) {
         const uint64_t line = at.k0 + key;
         const uint64_t wide = (uint64_t)p.kv_heads * p.dim, half = (uint64_t)p.parts * p.kv_rows * wide;
@@ -1013,6 +1016,7 @@ bool two_teams(AttentionArgs &p, uint64_t most_blocks, double round, double most
 template <typename F>
 void with_dim(uint32_t dim, F &&f) {
     if (dim <= 64) f(std::integral_constant<int, 64>());
+    else if (dim <= 96) f(std::integral_constant<int, 96>());
     else f(std::integral_constant<int, 128>());
 }
 }  // namespace
@@ -1081,7 +1085,10 @@ void launch_attention_grad(const lgc_attention_shape &shape, const void *grad, u
     // rows and more to go through, among which the loads of 256 keys and values count less (backward, us, eight / four: 4 x 4096 tokens of 32 / 8 heads 1930 / 2050, 8 x 2048 1107 / 1154, 20 sequences, 16000 tokens
     // 1033 / 1066, 16 x 1024 of 16 heads 414 / 410, one new token after each of 8 x 4096 168 / 131).  Heads of 64: three blocks of four fit a compute unit, one of eight (16384 tokens of 8 heads 599 / 601).
     set_tiles(p, p.kv_rows, 1, 256);
-    if (p.dim > 64 && grid_of(p) >= 2 * (uint64_t)cus && extent(p, p.kv_rows, p.q_rows, 256).mean * (double)group >= 1024.) dkv(std::integral_constant<int, 128>(), Eight());
+    if (p.dim > 64 && grid_of(p) >= 2 * (uint64_t)cus && extent(p, p.kv_rows, p.q_rows, 256).mean * (double)group >= 1024.) {
+        if (p.dim <= 96) dkv(std::integral_constant<int, 96>(), Eight());
+        else dkv(std::integral_constant<int, 128>(), Eight());
+    }
     else {
         set_tiles(p, p.kv_rows, 1, 128);
         with_dim(p.dim, [&](auto dim) { dkv(dim, Four()); });

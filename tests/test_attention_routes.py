@@ -102,10 +102,11 @@ BIG = dict(q_rows=16384, kv_rows=16384, sequences=4, heads=32, kv_heads=8, dim=1
 LONG = dict(q_rows=16384, kv_rows=16384, heads=8, kv_heads=8, dim=64)
 ROUTES = [
     (attention, (shape(**BIG),), ["k_attention 128 1"]), (attention, (shape(**LONG),), ["k_attention 64 1"]), (attention, (shape(dim=8),), ["k_attention 64 2"]),
-    (attention, (shape(dim=72),), ["k_attention 128 2"]), (attention, (shape(q_rows=8, kv_rows=32768, sequences=8, heads=32, kv_heads=8, dim=128),), ["k_attention 128 2", "k_attention_join"]),
+    (attention, (shape(dim=72),), ["k_attention 96 2"]), (attention, (shape(dim=96),), ["k_attention 96 2"]), (attention, (shape(dim=104),), ["k_attention 128 2"]), (attention, (shape(q_rows=8, kv_rows=32768, sequences=8, heads=32, kv_heads=8, dim=128),), ["k_attention 128 2", "k_attention_join"]),
     (attention, (shape(q_rows=0),), []), (attention, (shape(kv_rows=0),), ["k_attention 64 1"]), (attention, (shape(q_rows=60, kv_rows=60),), ["k_attention 64 1"]),
     (attention, (shape(q_rows=8192, kv_rows=8192, heads=16, kv_heads=16, sequences=2),), ["k_attention 64 1"]),
     (attention_grad, (shape(**BIG),), ["k_attention_dq 128 1", "k_attention_dkv 128 8 1"]), (attention_grad, (shape(**LONG),), ["k_attention_dq 64 1", "k_attention_dkv 64 4 1"]),
+    (attention_grad, (shape(**(BIG | dict(dim=96))),), ["k_attention_dq 96 1", "k_attention_dkv 96 8 1"]), (attention_grad, (shape(dim=80),), ["k_attention_dq 96 2", "k_attention_dkv 96 4 2", "k_attention_add"]),
     (attention_grad, (shape(q_rows=64, kv_rows=64, dim=128),), ["k_attention_dq 128 1", "k_attention_dkv 128 4 2"]), (attention_grad, (shape(q_rows=0),), ["k_attention_dkv 64 4 1"]),
     (attention_grad, (shape(kv_rows=0),), ["k_attention_dq 64 1"]), (attention_grad, (shape(q_rows=0, kv_rows=0),), []),
     (attention_grad, (shape(q_rows=8, kv_rows=32768, sequences=8, heads=32, kv_heads=8, dim=128),), ["k_attention_dq 128 2", "k_attention_add", "k_attention_dkv 128 4 1"]),

@@ -95,7 +95,7 @@ SHAPES = {
     "65 starts": (900, 900, 2, 1, 64, 65, ([i * (i + 1) // 5 for i in range(66)], [i * (i + 1) // 5 for i in range(66)])),
     "many starts": (3000, 3000, 1, 1, 64, 1500, (list(range(0, 3001, 2)), list(range(0, 3001, 2)))),
     "keys in parts": (4, 8192, 8, 2, 128, 2), "queries in parts": (6000, 100, 4, 2, 128, 1, None, False), "parts of starts": (9, 7000, 2, 2, 64, 3, ([1, 2, 5, 8], [100, 3000, 3001, 6900])),
-    "eight wavefronts": (2048, 2048, 64, 64, 128), "half a head": (2048, 2048, 8, 2, 64, 2), "long": (4096, 4096, 8, 8, 128, 2),
+    "eight wavefronts": (2048, 2048, 64, 64, 128), "half a head": (2048, 2048, 8, 2, 64, 2), "eight wavefronts of 88": (2048, 2048, 64, 64, 88), "many blocks of 72": (1400, 1400, 80, 80, 72, 7), "long": (4096, 4096, 8, 8, 128, 2),
     "many blocks": (1400, 1400, 80, 80, 40, 7), "many blocks, wide heads": (1400, 1400, 80, 80, 104, 7), "many blocks of starts": (1400, 1500, 160, 80, 64, 7, ([0, 3, 400, 400, 800, 1000, 1300, 1399],
                                                                                                                                                               [7, 300, 301, 301, 900, 1000, 1100, 1500]), True, 150),
 }
@@ -141,7 +141,7 @@ def test_a_million_keys(B, ctx):
 
 @pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
 @pytest.mark.parametrize("window", [0, 70])
-@pytest.mark.parametrize("heads,dim", [(4, 64), (280, 64), (280, 128)])     # (few blocks, many)
+@pytest.mark.parametrize("heads,dim", [(4, 64), (280, 64), (280, 128), (4, 80), (280, 96)])     # (few blocks, many)
 def test_what_is_hidden_has_no_influence(B, ctx, bad, window, heads, dim):
     """Infinities and NaNs in keys, values, queries and gradients: what does not see them is as if they were zeros, what does is not finite (where all of it is bad)."""
     n, at = 400, 250
