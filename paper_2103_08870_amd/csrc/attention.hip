@@ -369,8 +369,8 @@ __device__ __forceinline__ void hand_over(f4 *to, const f16 (&x)[kWide]) {
 // Two teams: eight wavefronts, of which four take the first half of the block's tiles and four the second, in LDS of their own; their sums meet in LDS at the end.  It halves the chain of tiles that
 // a block goes through one after the other, with no partial results in memory, but a compute unit holds one such block.
 //
-// Bound: by the matrix cores and the vector units (five instructions a score; an exponential is 8.5 cycles), which two wavefronts of a SIMD overlap in part: busy 51 % and 55 % of the time, LDS 27 %, at a clock
-// that power holds to 1.75 GHz of 2.4.  4 x 4096 tokens, causal, 32 / 8 heads of 128: 570 us, 0.96 PFLOP/s; 8 x 1 tokens after 4096: 25 us and 4 for the join
+// Bound: by the matrix cores and the vector units (five instructions a score; an exponential is 8.5 cycles), which two wavefronts of a SIMD overlap in part: busy 54 % and 56 % of the time, LDS 29 %, at a clock
+// that power holds to 1.7 GHz of 2.4.  4 x 4096 tokens, causal, 32 / 8 heads of 128: 550 us, 1.0 PFLOP/s; 8 x 1 tokens after 4096: 25 us and 4 for the join
 // of four parts, 5.4 TB/s of keys and values.  Taken back: two groups of rows per wavefront, one wavefront per SIMD (680 us, so 921, as the kernel then was); a SIMD's two wavefronts in turn between barriers,
 // 256 rows (no gain); eight wavefronts without teams (586); loads among the products (650); three tiles under way (no change).
 template <int kDim, int kTeams>
@@ -493,7 +493,8 @@ __global__ __launch_bounds__(256 * kTeams, kDim == 64 && kTeams == 1 ? 3 : 2) vo
         s[0] = ahead[0];
         s[1] = ahead[1];
         probabilities(key0);
-        if (tile + 1 < to) scores(keys + (place ^ 1) * kBytes);
+        // behind the last tile too, of what lies there, for nothing: without a branch these products stand among the exponentials (4 x 4096 tokens, 32 / 8 heads of 128 594 us with it, 567 without)
+        scores(keys + (place ^ 1) * kBytes);
         join(values + place * kBytes);
     }
 
